@@ -50,7 +50,7 @@
 extern "C" {
 #endif
 
-#define LUQ_ABI_VERSION 9
+#define LUQ_ABI_VERSION 10
 
 typedef int luq_status;
 enum {
@@ -101,7 +101,11 @@ enum {
   LUQ_OP_GEMM_FWD = 4,      /* d0 = M, d1 = N, d2 = K                        */
   LUQ_OP_CONV_WGRAD = 5,    /* d0 = B*H*W, d1 = C, d2 = Cout                 */
   LUQ_OP_GEMM_DGRAD_FP6 = 6, /* luq_gemm_dgrad with LUQ_CARRIER_FP6: M, N, K  */
-  LUQ_OP_GEMM_WGRAD_FP6 = 7  /* luq_gemm_wgrad with LUQ_CARRIER_FP6: T, Nout, Kin */
+  LUQ_OP_GEMM_WGRAD_FP6 = 7, /* luq_gemm_wgrad with LUQ_CARRIER_FP6: T, Nout, Kin */
+  /* operators of luq_lm.h */
+  LUQ_OP_GROUP_IDS = 8,     /* d0 = n, d1 = groups                           */
+  LUQ_OP_EMBEDDING_GRAD = 9, /* d0 = n, d1 = dim                             */
+  LUQ_OP_LAYERNORM_BWD = 10 /* d0 = rows, d1 = cols                          */
 };
 
 /* ABI version of the loaded library (LUQ_ABI_VERSION of its build). */

@@ -2,8 +2,9 @@
 
 Argument marshalling only: torch tensors supply device memory and the
 current HIP stream; every step runs in the HIP kernels of libluq.so.  The
-functions carry the names of the C ABI in include/luq.h.  Outputs that are
-not passed in are allocated with torch on the input's device.
+functions carry the names of the C ABI in include/luq.h and include/luq_lm.h
+(the operators of language models around the 4-bit products).  Outputs that
+are not passed in are allocated with torch on the input's device.
 
 The library must have been built (``python -m paper_2112_10769_amd._build``
 or ``__graft_entry__.build()``); importing the binding without it raises.
@@ -19,17 +20,24 @@ LIB_PATH = os.path.join(_HERE, "libluq.so")
 LUQ_OK = 0
 LUQ_ERR_NONFINITE = 8
 LUQ_F32, LUQ_BF16 = 0, 1
+LUQ_I32, LUQ_I64 = 0, 1
 ALPHA_PW2 = 0x100  # or-ed into R: power-of-two alpha
 SMP_SUM = 0x10     # or-ed into n_samples = 2: the two samples as int8 sums
 CARRIER_FP6 = 0x40  # or-ed into n_samples = 1 of the backward GEMMs: FP6 MFMA carrier
 OP_QUANTIZE_GRAD, OP_INT4_QUANTIZE, OP_GEMM_DGRAD, OP_GEMM_WGRAD, OP_GEMM_FWD, OP_CONV_WGRAD = 0, 1, 2, 3, 4, 5
 OP_GEMM_DGRAD_FP6, OP_GEMM_WGRAD_FP6 = 6, 7
+OP_GROUP_IDS, OP_EMBEDDING_GRAD, OP_LAYERNORM_BWD = 8, 9, 10
 
 EXPORTS = (
     "luq_abi_version", "luq_status_string", "luq_last_error", "luq_plane_bytes",
     "luq_workspace_size", "luq_query_status", "luq_quantize_grad", "luq_quantize_grad_noalloc", "luq_quantize_grad_hindsight", "int4_quantize",
     "luq_gemm_dgrad", "luq_gemm_wgrad", "int4_gemm_fwd", "int4_im2col3x3_t", "luq_conv3x3_dgrad",
     "luq_conv3x3_wgrad",
+)
+# of include/luq_lm.h
+EXPORTS_LM = (
+    "luq_group_ids", "luq_embedding_fwd", "luq_embedding_grad", "luq_layernorm_fwd", "luq_layernorm_bwd",
+    "int4_gemm_fwd_grouped", "luq_gemm_dgrad_grouped", "luq_grouped_wgrad_workspace", "luq_gemm_wgrad_grouped",
 )
 
 
@@ -76,6 +84,24 @@ def _load():
     lib.luq_conv3x3_dgrad.argtypes = [vp, vp, i32, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp]
     lib.luq_conv3x3_wgrad.restype = i32
     lib.luq_conv3x3_wgrad.argtypes = [vp, vp, i32, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, sz, vp]
+    lib.luq_group_ids.restype = i32
+    lib.luq_group_ids.argtypes = [vp, i32, i64, i64, vp, vp, vp, sz, vp]
+    lib.luq_embedding_fwd.restype = i32
+    lib.luq_embedding_fwd.argtypes = [vp, i32, i64, vp, i32, i64, i64, f32, vp, i32, vp]
+    lib.luq_embedding_grad.restype = i32
+    lib.luq_embedding_grad.argtypes = [vp, i32, vp, i32, vp, vp, i64, i64, i64, f32, i32, vp, vp, sz, vp]
+    lib.luq_layernorm_fwd.restype = i32
+    lib.luq_layernorm_fwd.argtypes = [vp, i32, i64, i64, vp, vp, f32, vp, vp, vp, vp]
+    lib.luq_layernorm_bwd.restype = i32
+    lib.luq_layernorm_bwd.argtypes = [vp, i32, vp, i32, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.int4_gemm_fwd_grouped.restype = i32
+    lib.int4_gemm_fwd_grouped.argtypes = [vp, vp, i32, vp, i64, i64, vp, i64, i32, vp, i64, i64, i64, i64, vp, vp]
+    lib.luq_gemm_dgrad_grouped.restype = i32
+    lib.luq_gemm_dgrad_grouped.argtypes = [vp, vp, i32, vp, i64, i64, vp, i64, i32, vp, i64, i64, i64, i64, vp, vp]
+    lib.luq_grouped_wgrad_workspace.restype = sz
+    lib.luq_grouped_wgrad_workspace.argtypes = [i64, i64, i64, i64]
+    lib.luq_gemm_wgrad_grouped.restype = i32
+    lib.luq_gemm_wgrad_grouped.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i64, i64, i64, vp, vp, sz, vp]
     return lib
 
 
@@ -317,4 +343,207 @@ def luq_conv3x3_wgrad(g_codes_t, alpha, a_codes_t, a_scale, a_signed, B, H, W, C
     st = LIB.luq_conv3x3_wgrad(_ptr(g_codes_t), _ptr(alpha), n_samples, _ptr(a_codes_t), _ptr(a_scale),
                                1 if a_signed else 0, B, H, W, C, Cout, _ptr(dw), _ptr(ws), ws.numel(), _stream(dev))
     _check(st, "luq_conv3x3_wgrad")
+    return dw
+
+
+# ---- operators of language models (include/luq_lm.h) ---------------------------------
+
+
+def _index(t):
+    if t.dtype == torch.int64:
+        return LUQ_I64
+    if t.dtype == torch.int32:
+        return LUQ_I32
+    raise TypeError(f"unsupported index dtype {t.dtype}")
+
+
+def _buffer(t, shape, dtype, dev, name):
+    """The output buffer t, checked, or a new one: the kernels write shape elements of dtype."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    n = 1
+    for v in shape:
+        n *= v
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name} must be contiguous, {tuple(shape)} of {dtype} on {dev}")
+    return t
+
+
+def _input(t, n, dtype, dev, name):
+    """The input t (None stays None), checked: the kernels read n elements of dtype."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or t.device != dev:
+        raise ValueError(f"{name} must hold {n} elements of {dtype} on {dev}")
+    return t.contiguous()
+
+
+def _codes(t, nbytes, dev, name):
+    """A code operand, checked: the kernels read nbytes from it."""
+    if t.element_size() != 1 or t.numel() < nbytes or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name} must be contiguous, at least {nbytes} bytes on {dev}")
+    return t.data_ptr()
+
+
+def luq_group_ids(ids, groups, order=None, offsets=None, ws=None):
+    """Positions of ids grouped by id (a stable sort), and the groups' offsets: (order [n] int32,
+    offsets [groups + 1] int32).  Ids outside [0, groups) come last and belong to no group."""
+    n, dev = ids.numel(), ids.device
+    it = _index(ids)
+    order = _buffer(order, (n,), torch.int32, dev, "order")
+    offsets = _buffer(offsets, (groups + 1,), torch.int32, dev, "offsets")
+    if ws is None:
+        ws = _bytes(workspace_size(OP_GROUP_IDS, n, groups), dev)
+    ids = ids.contiguous()
+    st = LIB.luq_group_ids(_ptr(ids), it, n, groups, _ptr(order), _ptr(offsets), _ptr(ws), ws.numel(), _stream(dev))
+    _check(st, "luq_group_ids")
+    return order, offsets
+
+
+def luq_embedding_fwd(ids, table, scale=1.0, out_dtype=None, out=None):
+    """scale * table[ids] of shape [*ids.shape, dim], in table's dtype or out_dtype.  Ids below 0 (padding) give
+    rows of zeros, ids at or above the table's rows rows of NaN."""
+    if table.dim() != 2 or table.device != ids.device:
+        raise ValueError("table must be [vocab, dim] on the ids' device")
+    n, dev = ids.numel(), ids.device
+    vocab, dim = table.shape
+    it, tt = _index(ids), _dtype(table)
+    if out is not None and out_dtype is None:
+        out_dtype = out.dtype
+    out = _buffer(out, (*ids.shape, dim), out_dtype or table.dtype, dev, "out")
+    ids, table = ids.contiguous(), table.contiguous()
+    st = LIB.luq_embedding_fwd(_ptr(ids), it, n, _ptr(table), tt, vocab, dim, float(scale), _ptr(out), _dtype(out),
+                               _stream(dev))
+    _check(st, "luq_embedding_fwd")
+    return out
+
+
+def luq_embedding_grad(dout, ids, order, offsets, scale=1.0, accumulate=False, dtable=None, ws=None):
+    """Gradient [vocab, dim] (float32) of luq_embedding_fwd's table from dout [*ids.shape, dim], with order and
+    offsets of luq_group_ids(ids, vocab).  accumulate adds to the rows of the dtable passed in."""
+    n, dev = ids.numel(), ids.device
+    vocab = offsets.numel() - 1
+    dim = dout.shape[-1]
+    if dout.numel() != n * dim or dout.device != dev:
+        raise ValueError("dout must be [*ids.shape, dim] on the ids' device")
+    if accumulate and dtable is None:
+        raise ValueError("accumulate adds to a dtable that is passed in")
+    it, gt = _index(ids), _dtype(dout)
+    order = _input(order, n, torch.int32, dev, "order")
+    offsets = _input(offsets, vocab + 1, torch.int32, dev, "offsets")
+    dtable = _buffer(dtable, (vocab, dim), torch.float32, dev, "dtable")
+    if ws is None:
+        ws = _bytes(workspace_size(OP_EMBEDDING_GRAD, n, dim), dev)
+    dout, ids = dout.contiguous(), ids.contiguous()
+    st = LIB.luq_embedding_grad(_ptr(dout), gt, _ptr(ids), it, _ptr(order), _ptr(offsets), n, vocab, dim, float(scale),
+                                1 if accumulate else 0, _ptr(dtable), _ptr(ws), ws.numel(), _stream(dev))
+    _check(st, "luq_embedding_grad")
+    return dtable
+
+
+def luq_layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rstd=None):
+    """Layer norm over the last dimension of x: (y, mean, rstd), y in x's dtype, the statistics float32 of
+    x.shape[:-1].  gamma and beta are float32 [cols]; y may be x."""
+    dev, cols = x.device, x.shape[-1]
+    rows = x.numel() // max(cols, 1)
+    dt = _dtype(x)
+    gamma = _input(gamma, cols, torch.float32, dev, "gamma")
+    beta = _input(beta, cols, torch.float32, dev, "beta")
+    y = _buffer(y, x.shape, x.dtype, dev, "y")
+    mean = _buffer(mean, x.shape[:-1], torch.float32, dev, "mean")
+    rstd = _buffer(rstd, x.shape[:-1], torch.float32, dev, "rstd")
+    x = x.contiguous()
+    st = LIB.luq_layernorm_fwd(_ptr(x), dt, rows, cols, _ptr(gamma), _ptr(beta), float(eps), _ptr(y), _ptr(mean),
+                               _ptr(rstd), _stream(dev))
+    _check(st, "luq_layernorm_fwd")
+    return y, mean, rstd
+
+
+def luq_layernorm_bwd(dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, ws=None):
+    """Gradients of luq_layernorm_fwd: (dx, dgamma, dbeta), dx in dy's dtype (it may differ from x's, and dx may be
+    dy), the others float32 [cols]."""
+    dev, cols = x.device, x.shape[-1]
+    rows = x.numel() // max(cols, 1)
+    if dy.shape != x.shape or dy.device != dev:
+        raise ValueError("dy must have x's shape and device")
+    gt, dt = _dtype(dy), _dtype(x)
+    mean = _input(mean, rows, torch.float32, dev, "mean")
+    rstd = _input(rstd, rows, torch.float32, dev, "rstd")
+    gamma = _input(gamma, cols, torch.float32, dev, "gamma")
+    dx = _buffer(dx, dy.shape, dy.dtype, dev, "dx")
+    dgamma = _buffer(dgamma, (cols,), torch.float32, dev, "dgamma")
+    dbeta = _buffer(dbeta, (cols,), torch.float32, dev, "dbeta")
+    if ws is None:
+        ws = _bytes(workspace_size(OP_LAYERNORM_BWD, rows, cols), dev)
+    dy, x = dy.contiguous(), x.contiguous()
+    st = LIB.luq_layernorm_bwd(_ptr(dy), gt, _ptr(x), dt, _ptr(mean), _ptr(rstd), _ptr(gamma), rows, cols, _ptr(dx),
+                               _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws.numel(), _stream(dev))
+    _check(st, "luq_layernorm_bwd")
+    return dx, dgamma, dbeta
+
+
+def _grouped_weights(codes, scale, offsets, N, K, w_row, w_expert, dev, name):
+    """(experts, w_row, w_expert) of a grouped product's weights, their operands checked; K and N*K codes apart
+    unless given."""
+    experts = offsets.numel() - 1
+    w_row = K if w_row is None else w_row
+    w_expert = N * w_row if w_expert is None else w_expert
+    _codes(codes, ((experts - 1) * w_expert + (N - 1) * w_row + K) // 2, dev, name)
+    if offsets.dtype != torch.int32 or not offsets.is_contiguous() or offsets.device != dev:
+        raise ValueError(f"offsets must be contiguous int32 on {dev}")
+    if scale.dtype != torch.float32 or scale.numel() not in (1, experts) or not scale.is_contiguous():
+        raise ValueError("w_scale must be float32, one value or one per expert")
+    return experts, w_row, w_expert
+
+
+def int4_gemm_fwd_grouped(x_codes, x_scale, x_signed, w_codes, w_scale, w_signed, offsets, T, N, K, w_row=None,
+                          w_expert=None, y=None):
+    """y [T, N]: int4_gemm_fwd with each row's expert, rows grouped by offsets [experts + 1] (int32, of
+    luq_group_ids).  w_codes holds [N, K] codes per expert, w_row and w_expert codes apart; w_scale one scale per
+    expert or one for all.  Rows of no expert get 0."""
+    dev = x_codes.device
+    experts, w_row, w_expert = _grouped_weights(w_codes, w_scale, offsets, N, K, w_row, w_expert, dev, "w_codes")
+    y = _buffer(y, (T, N), torch.float32, dev, "y")
+    st = LIB.int4_gemm_fwd_grouped(_codes(x_codes, T * K // 2, dev, "x_codes"), _ptr(x_scale), 1 if x_signed else 0,
+                                   _ptr(w_codes), w_row, w_expert, _ptr(w_scale), w_scale.numel(),
+                                   1 if w_signed else 0, _ptr(offsets), experts, T, N, K, _ptr(y), _stream(dev))
+    _check(st, "int4_gemm_fwd_grouped")
+    return y
+
+
+def luq_gemm_dgrad_grouped(g_codes, alpha, w_codes_t, w_scale, w_signed, offsets, M, N, K, n_samples=1, w_row=None,
+                           w_expert=None, dx=None):
+    """dX [M, N]: luq_gemm_dgrad with each row's expert, rows grouped by offsets.  w_codes_t holds [N, K] transposed
+    codes per expert, w_row and w_expert codes apart; n_samples 1 or 2 | SMP_SUM."""
+    dev = g_codes.device
+    experts, w_row, w_expert = _grouped_weights(w_codes_t, w_scale, offsets, N, K, w_row, w_expert, dev, "w_codes_t")
+    dx = _buffer(dx, (M, N), torch.float32, dev, "dx")
+    g = _codes(g_codes, M * K // (1 if n_samples & SMP_SUM else 2), dev, "g_codes")
+    st = LIB.luq_gemm_dgrad_grouped(g, _ptr(alpha), n_samples, _ptr(w_codes_t), w_row, w_expert, _ptr(w_scale),
+                                    w_scale.numel(), 1 if w_signed else 0, _ptr(offsets), experts, M, N, K, _ptr(dx),
+                                    _stream(dev))
+    _check(st, "luq_gemm_dgrad_grouped")
+    return dx
+
+
+def grouped_wgrad_workspace(T, Nout, Kin, experts):
+    return int(LIB.luq_grouped_wgrad_workspace(T, Nout, Kin, experts))
+
+
+def luq_gemm_wgrad_grouped(g_codes_t, alpha, a_codes_t, a_scale, a_signed, offsets, T, Nout, Kin, n_samples=1, dw=None,
+                           ws=None):
+    """dW [experts, Nout, Kin]: luq_gemm_wgrad over each expert's rows, from transposed codes g^T [Nout, T] and
+    a^T [Kin, T]; experts without rows get 0."""
+    dev = g_codes_t.device
+    experts = offsets.numel() - 1
+    if offsets.dtype != torch.int32 or not offsets.is_contiguous() or offsets.device != dev:
+        raise ValueError(f"offsets must be contiguous int32 on {dev}")
+    dw = _buffer(dw, (experts, Nout, Kin), torch.float32, dev, "dw")
+    g = _codes(g_codes_t, Nout * T // (1 if n_samples & SMP_SUM else 2), dev, "g_codes_t")
+    a = _codes(a_codes_t, Kin * T // 2, dev, "a_codes_t")
+    if ws is None:
+        ws = _bytes(grouped_wgrad_workspace(T, Nout, Kin, experts), dev)
+    st = LIB.luq_gemm_wgrad_grouped(g, _ptr(alpha), n_samples, a, _ptr(a_scale), 1 if a_signed else 0, _ptr(offsets),
+                                    experts, T, Nout, Kin, _ptr(dw), _ptr(ws), ws.numel(), _stream(dev))
+    _check(st, "luq_gemm_wgrad_grouped")
     return dw

@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include "../../include/luq.h"
+#include "../../include/luq_lm.h"
 #include "luq_launch.hpp"
 
 static_assert(LUQ_CARRIER_FP6 == luq::kCarrierFp6, "carrier flag");
@@ -26,6 +27,12 @@ luq_status hip_status(hipError_t e) {
   if (e == hipSuccess) return LUQ_OK;
   return fail(LUQ_ERR_HIP, "HIP launch failed: %s", hipGetErrorString(e));
 }
+
+constexpr int64_t kMaxRows = (int64_t)1 << 30;        // rows, ids, groups and columns
+constexpr int64_t kMaxElements = (int64_t)1 << 48;    // of one tensor: no byte offset overflows
+
+// p holds elements of `size` bytes.
+bool aligned_to(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) == 0; }
 
 bool mul_overflows(int64_t a, int64_t b) { return a > 0 && b > INT64_MAX / a; }
 
@@ -103,6 +110,14 @@ static size_t gemm_workspace(int64_t M, int64_t N, int64_t K) {
   return one > two ? one : two;
 }
 
+// Sizes that luq_group_ids and the row operators take.
+static bool group_sizes(int64_t n, int64_t groups) {
+  return n >= 0 && n <= kMaxRows && groups >= 1 && groups <= kMaxRows;
+}
+static bool row_sizes(int64_t rows, int64_t cols) {
+  return rows >= 0 && rows <= kMaxRows && cols >= 1 && cols <= kMaxRows && rows * cols <= kMaxElements;
+}
+
 size_t luq_workspace_size(int op, int64_t d0, int64_t d1, int64_t d2) {
   switch (op) {
     case LUQ_OP_QUANTIZE_GRAD:
@@ -123,6 +138,12 @@ size_t luq_workspace_size(int op, int64_t d0, int64_t d1, int64_t d2) {
               d2 < ((int64_t)1 << 28))
                  ? luq::conv3x3_wgrad_workspace_bytes(d0, d1, d2)
                  : 0;
+    case LUQ_OP_GROUP_IDS:
+      return group_sizes(d0, d1) ? luq::group_ids_workspace_bytes(d0, d1) : 0;
+    case LUQ_OP_EMBEDDING_GRAD:
+      return row_sizes(d0, d1) ? luq::embedding_grad_workspace_bytes(d0, d1) : 0;
+    case LUQ_OP_LAYERNORM_BWD:
+      return row_sizes(d0, d1) ? luq::layernorm_bwd_workspace_bytes(d0, d1) : 0;
     default:
       return 0;
   }
@@ -412,6 +433,208 @@ luq_status luq_conv3x3_wgrad(const uint8_t* g_codes_t, const float* alpha, int n
   return hip_status(luq::launch_conv3x3_wgrad(g_codes_t, (int64_t)luq::plane_bytes(T * Cout), n_samples, alpha,
                                               a_codes_t, a_scale, a_signed ? 1 : 0, B, H, W, C, Cout, dw, ws,
                                               static_cast<hipStream_t>(stream)));
+}
+
+// ---- operators of luq_lm.h -----------------------------------------------------------
+
+static size_t elem_size(luq_dtype dt) { return dt == LUQ_F32 ? 4 : 2; }
+
+static luq_status check_types(const char* fn, luq_dtype a, luq_dtype b) {
+  if ((a != LUQ_F32 && a != LUQ_BF16) || (b != LUQ_F32 && b != LUQ_BF16)) return fail(LUQ_ERR_DTYPE, "%s: dtype", fn);
+  return LUQ_OK;
+}
+
+static luq_status check_index(const char* fn, luq_index it) {
+  if (it != LUQ_I32 && it != LUQ_I64) return fail(LUQ_ERR_DTYPE, "%s: index type", fn);
+  return LUQ_OK;
+}
+
+static luq_status check_workspace(const char* fn, size_t need, const void* ws, size_t ws_bytes) {
+  if (need && (!ws || ws_bytes < need)) return fail(LUQ_ERR_WORKSPACE, "%s: workspace too small", fn);
+  if (need && !aligned16(ws)) return fail(LUQ_ERR_ALIGN, "%s: ws must be 16-byte aligned", fn);
+  return LUQ_OK;
+}
+
+luq_status luq_group_ids(const void* ids, luq_index it, int64_t n, int64_t groups, int32_t* order, int32_t* offsets,
+                         void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "luq_group_ids";
+  g_last_error[0] = 0;
+  luq_status st = check_index(fn, it);
+  if (st != LUQ_OK) return st;
+  if (!group_sizes(n, groups)) return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30] and groups in [1, 2^30]", fn);
+  if (!offsets || (n > 0 && (!ids || !order))) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned4(order) || !aligned4(offsets))
+    return fail(LUQ_ERR_ALIGN, "%s: ids, order or offsets misaligned", fn);
+  st = check_workspace(fn, luq::group_ids_workspace_bytes(n, groups), ws, ws_bytes);
+  if (st != LUQ_OK) return st;
+  return hip_status(luq::launch_group_ids(ids, it == LUQ_I64, n, groups, order, offsets, ws,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+luq_status luq_embedding_fwd(const void* ids, luq_index it, int64_t n, const void* table, luq_dtype tt, int64_t vocab,
+                             int64_t dim, float scale, void* out, luq_dtype ot, void* stream) {
+  const char* fn = "luq_embedding_fwd";
+  g_last_error[0] = 0;
+  luq_status st = check_index(fn, it);
+  if (st == LUQ_OK) st = check_types(fn, tt, ot);
+  if (st != LUQ_OK) return st;
+  if (!row_sizes(n, dim) || vocab < 0 || vocab > kMaxRows || vocab * dim > kMaxElements)
+    return fail(LUQ_ERR_SHAPE, "%s: n and vocab in [0, 2^30], dim in [1, 2^30]", fn);
+  if (n == 0) return LUQ_OK;
+  if (!ids || !out || (vocab > 0 && !table)) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned_to(table, elem_size(tt)) || !aligned_to(out, elem_size(ot)))
+    return fail(LUQ_ERR_ALIGN, "%s: ids, table or out misaligned", fn);
+  return hip_status(luq::launch_embedding_fwd(ids, it == LUQ_I64, n, table, tt == LUQ_BF16, vocab, dim, scale, out,
+                                              ot == LUQ_BF16, static_cast<hipStream_t>(stream)));
+}
+
+luq_status luq_embedding_grad(const void* dout, luq_dtype gt, const void* ids, luq_index it, const int32_t* order,
+                              const int32_t* offsets, int64_t n, int64_t vocab, int64_t dim, float scale,
+                              int accumulate, float* dtable, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "luq_embedding_grad";
+  g_last_error[0] = 0;
+  luq_status st = check_index(fn, it);
+  if (st == LUQ_OK) st = check_types(fn, gt, gt);
+  if (st != LUQ_OK) return st;
+  if (!row_sizes(n, dim) || vocab < 1 || vocab > kMaxRows || vocab * dim > kMaxElements)
+    return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30], vocab and dim in [1, 2^30]", fn);
+  if (accumulate != 0 && accumulate != 1) return fail(LUQ_ERR_PARAM, "%s: accumulate must be 0 or 1", fn);
+  if (!offsets || !dtable || (n > 0 && (!dout || !ids || !order))) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned_to(dout, elem_size(gt)) || !aligned4(order) ||
+      !aligned4(offsets) || !aligned4(dtable))
+    return fail(LUQ_ERR_ALIGN, "%s: a tensor is misaligned", fn);
+  st = check_workspace(fn, luq::embedding_grad_workspace_bytes(n, dim), ws, ws_bytes);
+  if (st != LUQ_OK) return st;
+  return hip_status(luq::launch_embedding_grad(dout, gt == LUQ_BF16, ids, it == LUQ_I64, order, offsets, n, vocab, dim,
+                                               scale, accumulate, dtable, ws, static_cast<hipStream_t>(stream)));
+}
+
+luq_status luq_layernorm_fwd(const void* x, luq_dtype dt, int64_t rows, int64_t cols, const float* gamma,
+                             const float* beta, float eps, void* y, float* mean, float* rstd, void* stream) {
+  const char* fn = "luq_layernorm_fwd";
+  g_last_error[0] = 0;
+  luq_status st = check_types(fn, dt, dt);
+  if (st != LUQ_OK) return st;
+  if (!row_sizes(rows, cols)) return fail(LUQ_ERR_SHAPE, "%s: rows in [0, 2^30] and cols in [1, 2^30]", fn);
+  if (!(eps >= 0.0f && eps < __builtin_inff())) return fail(LUQ_ERR_PARAM, "%s: eps must be finite and >= 0", fn);
+  if (rows > 0 && (!x || !y)) return fail(LUQ_ERR_NULL, "%s: x or y is NULL", fn);
+  if (!aligned_to(x, elem_size(dt)) || !aligned_to(y, elem_size(dt)) || !aligned4(gamma) || !aligned4(beta) ||
+      !aligned4(mean) || !aligned4(rstd))
+    return fail(LUQ_ERR_ALIGN, "%s: a tensor is misaligned", fn);
+  return hip_status(luq::launch_layernorm_fwd(x, dt == LUQ_BF16, rows, cols, gamma, beta, eps, y, mean, rstd,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+luq_status luq_layernorm_bwd(const void* dy, luq_dtype gt, const void* x, luq_dtype dt, const float* mean,
+                             const float* rstd, const float* gamma, int64_t rows, int64_t cols, void* dx,
+                             float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "luq_layernorm_bwd";
+  g_last_error[0] = 0;
+  luq_status st = check_types(fn, gt, dt);
+  if (st != LUQ_OK) return st;
+  if (!row_sizes(rows, cols)) return fail(LUQ_ERR_SHAPE, "%s: rows in [0, 2^30] and cols in [1, 2^30]", fn);
+  if (rows > 0 && (!dy || !x || !mean || !rstd || !dx)) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned_to(dy, elem_size(gt)) || !aligned_to(dx, elem_size(gt)) || !aligned_to(x, elem_size(dt)) ||
+      !aligned4(mean) || !aligned4(rstd) || !aligned4(gamma) || !aligned4(dgamma) || !aligned4(dbeta))
+    return fail(LUQ_ERR_ALIGN, "%s: a tensor is misaligned", fn);
+  st = check_workspace(fn, luq::layernorm_bwd_workspace_bytes(rows, cols), ws, ws_bytes);
+  if (st != LUQ_OK) return st;
+  return hip_status(luq::launch_layernorm_bwd(dy, gt == LUQ_BF16, x, dt == LUQ_BF16, mean, rstd, gamma, rows, cols, dx,
+                                              dgamma, dbeta, ws, static_cast<hipStream_t>(stream)));
+}
+
+constexpr int64_t kMaxExperts = 4096;
+
+// A grid has below 2^32 threads: 2^23 workgroups of 512, whichever tile is chosen (32 rows
+// and columns at least).
+static bool grid_fits(int64_t row_tiles, int64_t cols) {
+  const int64_t col_tiles = (cols + 31) / 32;
+  return row_tiles < ((int64_t)1 << 23) / col_tiles;
+}
+
+static luq_status grouped_rows(const char* fn, luq::GroupedA kind, int64_t max_k, const uint8_t* A, const float* alpha,
+                               const uint8_t* B, int64_t w_row, int64_t w_expert, const float* bscale,
+                               int64_t w_scales, int b_signed, const int32_t* offsets, int64_t experts, int64_t T,
+                               int64_t N, int64_t K, float* C, void* stream) {
+  if (experts < 1 || experts > kMaxExperts) return fail(LUQ_ERR_SHAPE, "%s: experts in [1, 4096]", fn);
+  if (T < 0 || T > kMaxRows || N < 1 || N > kMaxRows) return fail(LUQ_ERR_SHAPE, "%s: T in [0, 2^30], N in [1, 2^30]", fn);
+  if (K < 32 || (K & 31) || K > max_k)
+    return fail(LUQ_ERR_SHAPE, "%s: K must be a positive multiple of 32 of an int32-exact length", fn);
+  if (w_row < K || (w_row & 31) || w_row > ((int64_t)1 << 22))
+    return fail(LUQ_ERR_SHAPE, "%s: w_row must be a multiple of 32 in [K, 2^22]", fn);
+  if (w_expert < 0 || (w_expert & 31) || w_expert > ((int64_t)1 << 48))
+    return fail(LUQ_ERR_SHAPE, "%s: w_expert must be a non-negative multiple of 32", fn);
+  if (w_scales != 1 && w_scales != experts) return fail(LUQ_ERR_SHAPE, "%s: one weight scale, or one per expert", fn);
+  if (!grid_fits(T / 32 + (experts < T ? experts : T) + 1, N)) return fail(LUQ_ERR_SHAPE, "%s: too many tiles", fn);
+  if (T == 0) return LUQ_OK;
+  if (!A || !alpha || !B || !bscale || !offsets || !C) return fail(LUQ_ERR_NULL, "%s: NULL operand", fn);
+  if (!aligned16(A) || !aligned16(B) || !aligned4(alpha) || !aligned4(bscale) || !aligned4(offsets) || !aligned4(C))
+    return fail(LUQ_ERR_ALIGN, "%s: code operands must be 16-byte aligned, the others 4-byte", fn);
+  return hip_status(luq::launch_grouped_rows(kind, A, alpha, B, w_row, w_expert, bscale, w_scales, b_signed ? 1 : 0,
+                                             offsets, experts, T, N, K, C, static_cast<hipStream_t>(stream)));
+}
+
+static luq_status grouped_samples(const char* fn, int n_samples, luq::GroupedA* kind) {
+  if (n_samples != 1 && n_samples != (LUQ_SMP_SUM | 2))
+    return fail(LUQ_ERR_PARAM, "%s: n_samples must be 1 or LUQ_SMP_SUM | 2", fn);
+  *kind = n_samples == 1 ? luq::GroupedA::kLuq : luq::GroupedA::kSums;
+  return LUQ_OK;
+}
+
+luq_status int4_gemm_fwd_grouped(const uint8_t* x_codes, const float* x_scale, int x_signed, const uint8_t* w_codes,
+                                 int64_t w_row, int64_t w_expert, const float* w_scale, int64_t w_scales, int w_signed,
+                                 const int32_t* offsets, int64_t experts, int64_t T, int64_t N, int64_t K, float* y,
+                                 void* stream) {
+  g_last_error[0] = 0;
+  return grouped_rows("int4_gemm_fwd_grouped", x_signed ? luq::GroupedA::kInt4S : luq::GroupedA::kInt4U, 1 << 17,
+                      x_codes, x_scale, w_codes, w_row, w_expert, w_scale, w_scales, w_signed, offsets, experts, T, N,
+                      K, y, stream);
+}
+
+luq_status luq_gemm_dgrad_grouped(const uint8_t* g_codes, const float* alpha, int n_samples, const uint8_t* w_codes_t,
+                                  int64_t w_row, int64_t w_expert, const float* w_scale, int64_t w_scales,
+                                  int w_signed, const int32_t* offsets, int64_t experts, int64_t T, int64_t N,
+                                  int64_t K, float* dx, void* stream) {
+  const char* fn = "luq_gemm_dgrad_grouped";
+  g_last_error[0] = 0;
+  luq::GroupedA kind;
+  const luq_status st = grouped_samples(fn, n_samples, &kind);
+  if (st != LUQ_OK) return st;
+  return grouped_rows(fn, kind, 1 << 18, g_codes, alpha, w_codes_t, w_row, w_expert, w_scale, w_scales, w_signed,
+                      offsets, experts, T, N, K, dx, stream);
+}
+
+// Sizes of luq_gemm_wgrad_grouped.  T is at most the int32-exact length of a reduction.
+static bool grouped_wgrad_sizes(int64_t T, int64_t Nout, int64_t Kin, int64_t experts) {
+  return T >= 32 && (T & 31) == 0 && T <= (1 << 18) && Nout >= 1 && Nout <= kMaxRows && Kin >= 1 && Kin <= kMaxRows &&
+         experts >= 1 && experts <= kMaxExperts && Nout * Kin <= kMaxElements / experts &&
+         grid_fits((Nout + 31) / 32 * experts, Kin);
+}
+
+size_t luq_grouped_wgrad_workspace(int64_t T, int64_t Nout, int64_t Kin, int64_t experts) {
+  return grouped_wgrad_sizes(T, Nout, Kin, experts) ? luq::grouped_depth_workspace_bytes(T, Nout, Kin, experts) : 0;
+}
+
+luq_status luq_gemm_wgrad_grouped(const uint8_t* g_codes_t, const float* alpha, int n_samples,
+                                  const uint8_t* a_codes_t, const float* a_scale, int a_signed, const int32_t* offsets,
+                                  int64_t experts, int64_t T, int64_t Nout, int64_t Kin, float* dw, void* ws,
+                                  size_t ws_bytes, void* stream) {
+  const char* fn = "luq_gemm_wgrad_grouped";
+  g_last_error[0] = 0;
+  luq::GroupedA kind;
+  luq_status st = grouped_samples(fn, n_samples, &kind);
+  if (st != LUQ_OK) return st;
+  if (experts < 1 || experts > kMaxExperts) return fail(LUQ_ERR_SHAPE, "%s: experts in [1, 4096]", fn);
+  if (!grouped_wgrad_sizes(T, Nout, Kin, experts))
+    return fail(LUQ_ERR_SHAPE, "%s: T must be a multiple of 32 in [32, 2^18], Nout and Kin positive", fn);
+  if (!g_codes_t || !alpha || !a_codes_t || !a_scale || !offsets || !dw) return fail(LUQ_ERR_NULL, "%s: NULL operand", fn);
+  if (!aligned16(g_codes_t) || !aligned16(a_codes_t) || !aligned4(alpha) || !aligned4(a_scale) || !aligned4(offsets) ||
+      !aligned4(dw))
+    return fail(LUQ_ERR_ALIGN, "%s: code operands must be 16-byte aligned, the others 4-byte", fn);
+  st = check_workspace(fn, luq::grouped_depth_workspace_bytes(T, Nout, Kin, experts), ws, ws_bytes);
+  if (st != LUQ_OK) return st;
+  return hip_status(luq::launch_grouped_depth(kind, g_codes_t, alpha, a_codes_t, a_scale, a_signed ? 1 : 0, offsets,
+                                              experts, T, Nout, Kin, dw, ws, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

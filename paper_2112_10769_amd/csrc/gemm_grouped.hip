@@ -1,0 +1,326 @@
+// 4-bit products grouped by expert: the tile kernel of gemm_kernel.hpp on ragged groups
+// whose sizes only the device knows.
+//
+//   rows  (forward, activation gradient)  C[m][n] = s * s_w[e] * sum_k A[m][k] B_e[n][k],
+//         m in group e: every group is a product of its own, of M_e = offsets[e + 1] -
+//         offsets[e] rows.
+//   depth (weight gradient)  C_e[m][n] = s * sum_k A[m][k] B[n][k], k in group e.
+//
+// The grid covers the most tiles that T rows in so many groups can make; a workgroup finds
+// its group from the offsets and leaves if there is none for it.
+#include "gemm_kernel.hpp"
+
+namespace luq {
+
+namespace {
+
+// ---- groups of rows --------------------------------------------------------------------
+
+struct RowsArgs {
+  const uint8_t* A;
+  const uint8_t* B;
+  const int32_t* offsets;
+  int experts, tiles_n, vec, scales;
+  int64_t T, N, K;
+  int64_t w_row, w_expert;   // bytes
+  const float* alpha;
+  const float* bscale;
+  float* C;
+};
+
+// One tile as the tile kernel sees it, moved to the origin: M rows of A from A, N rows of
+// B from B.
+struct RowsTile {
+  static constexpr bool kMaskK = false;
+  const uint8_t* A;
+  const uint8_t* B;
+  int64_t a_plane, M, N, K, ldb, ldc;
+  int rows_a, rows_b;        // rows inside the tile
+  const float* alpha;
+  const float* bscale;
+  float* C;
+  int vec;
+  __device__ __forceinline__ void place(int, int, int64_t& m0, int64_t& n0, int64_t& kbeg, int64_t& kend) const {
+    m0 = n0 = kbeg = 0;
+    kend = K;
+  }
+  __device__ __forceinline__ int64_t row_a(bool i8) const { return i8 ? K : K >> 1; }
+  __device__ __forceinline__ int64_t row_b() const { return ldb; }
+  __device__ __forceinline__ int range_a(int64_t row) const { return (int)(rows_a * row); }
+  // the last row ends where its codes do
+  __device__ __forceinline__ int range_b(int64_t row) const { return (int)((rows_b - 1) * row + (K >> 1)); }
+  __device__ __forceinline__ bool sums() const { return false; }
+  __device__ __forceinline__ uint32_t* out() const { return reinterpret_cast<uint32_t*>(C); }
+  __device__ __forceinline__ int64_t row_c() const { return ldc; }
+};
+
+// Rows of group e (e = experts: the rows after the last group), kept inside the batch
+// whatever the offsets hold.
+__device__ __forceinline__ void group_bounds(const int32_t* offsets, int experts, int T, int e, int& lo, int& hi) {
+  lo = min(max(offsets[e], 0), T);
+  hi = e < experts ? min(max(offsets[e + 1], lo), T) : T;
+}
+
+struct GroupTile {
+  int group, lo, rows, tm, tn;   // the group, its first row and number of rows, the tile in it
+};
+
+// Tile of workgroup bid: tiles are numbered group by group, and within a group in columns
+// of 8 tile-rows; each of the 8 XCDs takes a run of them, as in tile_coords.  Every wave
+// scans the offsets for itself, 64 groups at a time.  False: no tile is left for bid.
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, int T, int bm, int tiles_n, int bid,
+                                          GroupTile& g) {
+  const int lane = threadIdx.x & 63;
+  auto tiles_of = [&](int e, int& lo, int& rows) {
+    int hi = 0;
+    lo = rows = 0;
+    if (e <= experts) {
+      group_bounds(offsets, experts, T, e, lo, hi);
+      rows = hi - lo;
+    }
+    return (rows + bm - 1) / bm;
+  };
+  int total = 0;
+  for (int base = 0; base <= experts; base += 64) {
+    int lo, rows, n = tiles_of(base + lane, lo, rows);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) n += __shfl_xor(n, d, 64);
+    total += __builtin_amdgcn_readfirstlane(n);
+  }
+  total *= tiles_n;
+  if (bid >= total) return false;
+  const int xcd = bid & 7, q = total >> 3, r = total & 7;
+  int L = xcd * q + min(xcd, r) + (bid >> 3);
+  int before = 0;   // tile-rows of the groups before
+  const int row = L / tiles_n;
+  for (int base = 0; base <= experts; base += 64) {
+    int lo, rows;
+    const int n = tiles_of(base + lane, lo, rows);
+    int sum = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(sum, d, 64);
+      if (lane >= d) sum += up;
+    }
+    const uint64_t past = __ballot(before + sum > row);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      g.group = base + at;
+      g.lo = __builtin_amdgcn_readlane(lo, at);
+      g.rows = __builtin_amdgcn_readlane(rows, at);
+      const int ntm = __builtin_amdgcn_readlane(n, at);
+      L -= (before + __builtin_amdgcn_readlane(sum, at) - ntm) * tiles_n;
+      constexpr int G = 8;
+      const int first = (L / (G * tiles_n)) * G, size = min(ntm - first, G);
+      const int in = L - first * tiles_n;
+      g.tm = first + in % size;
+      g.tn = in / size;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  return false;
+}
+
+template <int AC, bool BSIGNED, bool FULLK, int PF, typename S>
+__global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_rows_kernel(RowsArgs a) {
+  GroupTile g;
+  if (!find_tile(a.offsets, a.experts, (int)a.T, S::BM, a.tiles_n, blockIdx.x, g)) return;
+  const int64_t m0 = (int64_t)g.lo + (int64_t)g.tm * S::BM, n0 = (int64_t)g.tn * S::BN;
+  const int64_t m = g.rows - (int64_t)g.tm * S::BM, n = a.N - n0;
+  float* const C = a.C + m0 * a.N + n0;
+  if (g.group == a.experts) {   // rows of no group
+    const int rows = (int)min(m, (int64_t)S::BM), cols = (int)min(n, (int64_t)S::BN);
+    for (int r = threadIdx.x / 64; r < rows; r += S::NW)
+      for (int c = threadIdx.x & 63; c < cols; c += 64) C[r * a.N + c] = 0.0f;
+    return;
+  }
+  RowsTile t;
+  t.A = a.A + m0 * (AC == kAcSum2 ? a.K : a.K >> 1);
+  t.B = a.B + g.group * a.w_expert + n0 * a.w_row;
+  t.a_plane = 0;
+  t.M = m;
+  t.N = n;
+  t.K = a.K;
+  t.ldb = a.w_row;
+  t.ldc = a.N;
+  t.rows_a = (int)min(m, (int64_t)S::BM);
+  t.rows_b = (int)min(n, (int64_t)S::BN);
+  t.alpha = a.alpha;
+  t.bscale = a.bscale + (a.scales == 1 ? 0 : g.group);
+  t.C = C;
+  t.vec = a.vec;
+  gemm_tile<AC, 1, BSIGNED, FULLK, PF, S>(t);
+}
+
+// ---- groups of the reduction -------------------------------------------------------------
+
+struct DepthArgs {
+  const uint8_t* A;
+  const uint8_t* B;
+  const int32_t* offsets;
+  int experts, tiles_m, tiles_n, splits, vec;
+  int64_t T, M, N;
+  const float* alpha;
+  const float* bscale;
+  float* C;
+  int32_t* partial;   // [splits][experts][M][N], or null
+};
+
+struct DepthTile {
+  static constexpr bool kMaskK = true;
+  const uint8_t* A;
+  const uint8_t* B;
+  int64_t a_plane, M, N, T, klo, kend;
+  int64_t ldc;
+  int rows_a, rows_b;
+  const float* alpha;
+  const float* bscale;
+  uint32_t* C;
+  int vec;
+  bool part;
+  __device__ __forceinline__ void place(int, int, int64_t& m0, int64_t& n0, int64_t& kb, int64_t& ke) const {
+    m0 = n0 = 0;
+    kb = klo & ~(int64_t)31;
+    ke = kend;
+  }
+  __device__ __forceinline__ int64_t row_a(bool i8) const { return i8 ? T : T >> 1; }
+  __device__ __forceinline__ int64_t row_b() const { return T >> 1; }
+  __device__ __forceinline__ int range_a(int64_t row) const { return (int)(rows_a * row); }
+  __device__ __forceinline__ int range_b(int64_t row) const { return (int)(rows_b * row); }
+  __device__ __forceinline__ bool sums() const { return part; }
+  __device__ __forceinline__ uint32_t* out() const { return C; }
+  __device__ __forceinline__ int64_t row_c() const { return ldc; }
+};
+
+template <int AC, bool BSIGNED, int PF, typename S>
+__global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_depth_kernel(DepthArgs a) {
+  const int per = a.tiles_m * a.tiles_n, total = per * a.experts;
+  const int xcd = blockIdx.x & 7, q = total >> 3, r = total & 7;
+  int L = xcd * q + min(xcd, r) + (int)(blockIdx.x >> 3);
+  const int e = L / per;
+  L -= e * per;
+  constexpr int G = 8;
+  const int first = (L / (G * a.tiles_n)) * G, size = min(a.tiles_m - first, G);
+  const int in = L - first * a.tiles_n;
+  const int64_t m0 = (int64_t)(first + in % size) * S::BM, n0 = (int64_t)(in / size) * S::BN;
+  int lo, hi;
+  group_bounds(a.offsets, a.experts, (int)a.T, e, lo, hi);
+  if (a.splits > 1) {   // whole stages a split, counted from the group's first 16-byte piece
+    const int kb = lo & ~31, stages = (hi - kb + S::BK - 1) / S::BK;
+    const int chunk = (stages + a.splits - 1) / a.splits * S::BK;
+    const int from = kb + (int)blockIdx.y * chunk;
+    hi = min(hi, from + chunk);
+    lo = min(max(lo, from), hi);
+  }
+  DepthTile t;
+  t.A = a.A + m0 * (AC == kAcSum2 ? a.T : a.T >> 1);
+  t.B = a.B + n0 * (a.T >> 1);
+  t.a_plane = 0;
+  t.M = a.M - m0;
+  t.N = a.N - n0;
+  t.T = a.T;
+  t.klo = lo;
+  t.kend = hi;
+  t.ldc = a.N;
+  t.rows_a = (int)min(t.M, (int64_t)S::BM);
+  t.rows_b = (int)min(t.N, (int64_t)S::BN);
+  t.alpha = a.alpha;
+  t.bscale = a.bscale;
+  t.vec = a.vec;
+  t.part = a.partial != nullptr;
+  const int64_t slab = ((int64_t)blockIdx.y * a.experts + e) * a.M * a.N + m0 * a.N + n0;
+  t.C = t.part ? reinterpret_cast<uint32_t*>(a.partial + slab) : reinterpret_cast<uint32_t*>(a.C + slab);
+  gemm_tile<AC, 1, BSIGNED, true, PF, S>(t);
+}
+
+// ---- launch ------------------------------------------------------------------------------
+
+template <typename S, int AC, bool BSIGNED>
+void launch_rows_tile(RowsArgs a, hipStream_t st) {
+  a.tiles_n = (int)((a.N + S::BN - 1) / S::BN);
+  // whole tiles of T rows, and one partly filled tile for each group that can have rows
+  // and for the rows of no group
+  const int64_t groups = a.experts < a.T ? a.experts : a.T;
+  const dim3 grid((unsigned)((a.T / S::BM + groups + 1) * a.tiles_n));
+  if (a.K % S::BK == 0)
+    hipLaunchKernelGGL((grouped_rows_kernel<AC, BSIGNED, true, 2, S>), grid, dim3(S::THREADS), 0, st, a);
+  else
+    hipLaunchKernelGGL((grouped_rows_kernel<AC, BSIGNED, false, 2, S>), grid, dim3(S::THREADS), 0, st, a);
+}
+
+template <int AC, bool BSIGNED>
+hipError_t launch_rows(const RowsArgs& a, hipStream_t st) {
+  launch_rows_tile<Tile128x128, AC, BSIGNED>(a, st);
+  return hipGetLastError();
+}
+
+template <int AC, bool BSIGNED>
+hipError_t launch_depth(DepthArgs a, hipStream_t st) {
+  using S = Tile128x128;
+  a.tiles_m = (int)((a.M + S::BM - 1) / S::BM);
+  a.tiles_n = (int)((a.N + S::BN - 1) / S::BN);
+  a.vec = (a.N % 4) == 0 && (((uintptr_t)(a.partial ? (void*)a.partial : (void*)a.C)) & 15) == 0;
+  const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n * a.experts), (unsigned)a.splits);
+  hipLaunchKernelGGL((grouped_depth_kernel<AC, BSIGNED, 2, S>), grid, dim3(S::THREADS), 0, st, a);
+  if (a.splits > 1)
+    launch_split_reduce(a.partial, a.splits, a.experts * a.M * a.N,
+                        EpilogueScale<AC, 1, BSIGNED>{a.alpha, a.bscale}, a.C, st);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B, int64_t w_row,
+                               int64_t w_expert, const float* bscale, int64_t scales, int b_signed,
+                               const int32_t* offsets, int64_t experts, int64_t T, int64_t N, int64_t K, float* C,
+                               hipStream_t st) {
+  RowsArgs a;
+  a.A = A;
+  a.B = B;
+  a.offsets = offsets;
+  a.experts = (int)experts;
+  a.tiles_n = 0;
+  a.vec = (N % 4) == 0 && ((uintptr_t)C & 15) == 0;
+  a.scales = (int)scales;
+  a.T = T;
+  a.N = N;
+  a.K = K;
+  a.w_row = w_row / 2;
+  a.w_expert = w_expert / 2;
+  a.alpha = alpha;
+  a.bscale = bscale;
+  a.C = C;
+  switch (kind) {
+    case GroupedA::kLuq: return b_signed ? launch_rows<kAcLuq, true>(a, st) : launch_rows<kAcLuq, false>(a, st);
+    case GroupedA::kSums: return b_signed ? launch_rows<kAcSum2, true>(a, st) : launch_rows<kAcSum2, false>(a, st);
+    case GroupedA::kInt4S: return b_signed ? launch_rows<kAcInt4S, true>(a, st) : launch_rows<kAcInt4S, false>(a, st);
+    default: return b_signed ? launch_rows<kAcInt4U, true>(a, st) : launch_rows<kAcInt4U, false>(a, st);
+  }
+}
+
+size_t grouped_depth_workspace_bytes(int64_t, int64_t, int64_t, int64_t) { return 0; }
+
+hipError_t launch_grouped_depth(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B,
+                                const float* bscale, int b_signed, const int32_t* offsets, int64_t experts, int64_t T,
+                                int64_t M, int64_t N, float* C, void* ws, hipStream_t st) {
+  DepthArgs a;
+  a.A = A;
+  a.B = B;
+  a.offsets = offsets;
+  a.experts = (int)experts;
+  a.tiles_m = a.tiles_n = a.vec = 0;
+  a.splits = 1;
+  a.T = T;
+  a.M = M;
+  a.N = N;
+  a.alpha = alpha;
+  a.bscale = bscale;
+  a.C = C;
+  a.partial = a.splits > 1 ? static_cast<int32_t*>(ws) : nullptr;
+  if (kind == GroupedA::kSums)
+    return b_signed ? launch_depth<kAcSum2, true>(a, st) : launch_depth<kAcSum2, false>(a, st);
+  return b_signed ? launch_depth<kAcLuq, true>(a, st) : launch_depth<kAcLuq, false>(a, st);
+}
+
+}  // namespace luq

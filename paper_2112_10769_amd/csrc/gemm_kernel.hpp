@@ -117,6 +117,21 @@ struct GemmArgs {
   int64_t k_chunk;    // k per split (a multiple of the tile's stage depth)
   int tiles_m, tiles_n;
   int vec;            // N % 4 == 0 and rows of C (or partial) are 16-byte aligned: vector stores
+
+  // What the tile kernel asks of its arguments; the grouped products answer differently.
+  static constexpr bool kMaskK = false;   // k ranges are whole 16-byte pieces
+  // This workgroup's tile (of bm x bn) and k range.
+  __device__ __forceinline__ void place(int bm, int bn, int64_t& m0, int64_t& n0, int64_t& kbeg, int64_t& kend) const;
+  // Bytes per row of A (int8 sums or codes) and of B, and the operands' ranges.
+  __device__ __forceinline__ int64_t row_a(bool i8) const { return i8 ? K : K >> 1; }
+  __device__ __forceinline__ int64_t row_b() const { return K >> 1; }
+  __device__ __forceinline__ int range_a(int64_t row) const { return (int)(M * row); }
+  __device__ __forceinline__ int range_b(int64_t row) const { return (int)(N * row); }
+  __device__ __forceinline__ bool sums() const { return partial != nullptr; }   // chunk sums instead of C
+  __device__ __forceinline__ uint32_t* out() const {
+    return partial ? reinterpret_cast<uint32_t*>(partial + (int64_t)blockIdx.y * M * N) : reinterpret_cast<uint32_t*>(C);
+  }
+  __device__ __forceinline__ int64_t row_c() const { return N; }
 };
 
 // Block -> output tile.  Blocks are dispatched round-robin over the 8 XCDs
@@ -135,6 +150,16 @@ __device__ __forceinline__ void tile_coords(int bid, int ntm, int ntn, int& tm, 
   const int in_group = L - (L / per_group) * per_group;
   tm = first_m + in_group % gsize;
   tn = in_group / gsize;
+}
+
+__device__ __forceinline__ void GemmArgs::place(int bm, int bn, int64_t& m0, int64_t& n0, int64_t& kbeg,
+                                                int64_t& kend) const {
+  int tm, tn;
+  tile_coords(blockIdx.x, tiles_m, tiles_n, tm, tn);
+  m0 = (int64_t)tm * bm;
+  n0 = (int64_t)tn * bn;
+  kbeg = (int64_t)blockIdx.y * k_chunk;
+  kend = min(kbeg + k_chunk, K);
 }
 
 // fl32(fl32(alpha / NS) * s_B) times the exact powers of two of the
@@ -218,8 +243,13 @@ using Tile32x64 = GemmShape<1, 2, 4, 1, 1, 4>;
 using Tile32x32 = GemmShape<1, 1, 8, 1, 1, 4>;
 using Tile64x64k1 = GemmShape<2, 2, 1, 1, 1, 4>;
 
-template <int AC, int NS, bool BSIGNED, bool FULLK, int PF, typename S>
-__global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs a) {
+//
+// Args::kMaskK: the k range begins and ends at any code.  kbeg is then a.klo rounded down
+// to a 16-byte piece, kend the end itself, and codes of A outside [klo, kend) are cleared
+// before they are expanded (what B holds there does not matter: the products are those of
+// integers).  Only the first and the last stage pay for it.
+template <int AC, int NS, bool BSIGNED, bool FULLK, int PF, typename S, typename Args>
+__device__ __forceinline__ void gemm_tile(const Args& a) {
   constexpr int BM = S::BM, kBK = S::BK, kThr = S::THREADS, KG = S::KG;
   constexpr int kPitch = kBK + 16;        // A row: 8 KG slots of 16 bytes, 16 bytes of pad
   constexpr int STAGE = BM * kPitch;
@@ -230,28 +260,26 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
   constexpr int NA = kI8 ? 2 : NS;
   static_assert(ACH == 1 || ACH == 2, "at most one A half-chunk per k-step");
   static_assert(BM * KC % kThr == 0, "every thread loads the same chunks");
+  static_assert(!Args::kMaskK || (FULLK && NS == 1), "masked k ranges: one A operand, stages past kend are cleared");
   constexpr int EP = 32 * TN + 4;         // epilogue slab row pitch in 32-bit words
   constexpr int kSlabs = S::NW * 32 * EP * 4;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE > kSlabs ? 2 * STAGE : kSlabs];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int kg = wave / (S::WM * S::WN), wm = (wave / S::WN) % S::WM, wn = wave % S::WN, h = lane >> 5;
-  int tm, tn;
-  tile_coords(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
-  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * S::BN;
-  const int64_t kbeg = (int64_t)blockIdx.y * a.k_chunk;
-  const int64_t kend = min(kbeg + a.k_chunk, a.K);
+  int64_t m0, n0, kbeg, kend;
+  a.place(BM, S::BN, m0, n0, kbeg, kend);
   const int nkt = (int)((kend - kbeg + kBK - 1) / kBK);
-  const int64_t ld = a.K >> 1;              // bytes per B row (and per nibble A row)
-  const int64_t lda = kI8 ? a.K : ld;       // bytes per A row
+  const int64_t ld = a.row_b();             // bytes per B row
+  const int64_t lda = a.row_a(kI8);         // bytes per A row
 
   __amdgpu_buffer_rsrc_t rsa[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s)
     rsa[s] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.A + s * a.a_plane), (short)0,
-                                               (int)(a.M * lda), kBufferFlags);
+                                               a.range_a(lda), kBufferFlags);
   const __amdgpu_buffer_rsrc_t rsb =
-      __builtin_amdgcn_make_buffer_rsrc((void*)a.B, (short)0, (int)(a.N * ld), kBufferFlags);
+      __builtin_amdgcn_make_buffer_rsrc((void*)a.B, (short)0, a.range_b(ld), kBufferFlags);
   // A loader: chunk i of a thread is row c/KC, 16 nibble bytes (32 k) at 16*(c%KC)
   int offa[ACH], kca[ACH], slota[ACH], rowa[ACH];
 #pragma unroll
@@ -261,7 +289,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
     rowa[i] = row;
     // slot of the chunk's first half; the second is 2 further
     slota[i] = 8 * (kc >> 2) + 4 * (kc & 1) + ((kc >> 1) & 1);
-    offa[i] = kI8 ? (int)((m0 + row) * lda + kbeg + kc * 32) : (int)((m0 + row) * ld + (kbeg >> 1) + kc * 16);
+    offa[i] = kI8 ? (int)((m0 + row) * lda + kbeg + kc * 32) : (int)((m0 + row) * lda + (kbeg >> 1) + kc * 16);
   }
   // B loader: load q takes the rows 2i + q of a 32-row block, lane l the
   // 16-byte chunk kcb of row (l & 30) + q, so that neighbouring lanes read 32
@@ -315,6 +343,25 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
         r.b[j][0][d] = odd ? u : x;
         r.b[j][1][d] = odd ? y : u;
       }
+  };
+  // clears the codes of stage t outside [klo, kend); a dword holds 8 codes, or 4 int8 sums
+  auto mask_a = [&](ARegs& r, int t) {
+    if constexpr (Args::kMaskK) {
+      const int64_t k0 = kbeg + (int64_t)t * kBK;
+      if (k0 >= a.klo && k0 + kBK <= kend) return;
+      constexpr int PER = kI8 ? 4 : 8, BITS = 32 / PER;
+#pragma unroll
+      for (int i = 0; i < ACH; ++i)
+#pragma unroll
+        for (int s = 0; s < NA; ++s)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const int64_t k = k0 + kca[i] + (4 * s + d) * PER;   // s = 1: the second half of the sums
+            const int lo = (int)min(max(a.klo - k, (int64_t)0), (int64_t)PER);
+            const int hi = (int)min(max(kend - k, (int64_t)0), (int64_t)PER);
+            r.a[s][i][d] &= (uint32_t)((1ull << (hi * BITS)) - 1) & ~(uint32_t)((1ull << (lo * BITS)) - 1);
+          }
+    }
   };
   // half hf of A chunk i (its k 16hf .. 16hf+15) -> 16 bytes of LDS
   auto expand_a = [&](const ARegs& r, int buf, int i, int hf) {
@@ -381,6 +428,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
   // multiply stage t from buffer cb and B set rb while expanding the A codes
   // of stage t+1 (ra) into the other buffer; rbn is the next stage's B set
   auto step = [&](int cb, ARegs& ra, int ta, BRegs& rb, int tb, BRegs& rbn) {
+    if constexpr (Args::kMaskK) mask_a(ra, ta - 2);
     if constexpr (PF >= 1) read_a(cb, 0, fa2[0]);
     if constexpr (PF != 3) pair_b(rb, 0);
     if constexpr (PF == 2) frag_b(rb, 0, fb2[0]);
@@ -442,6 +490,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
   load_b(b1, 1, 0);
   load_b(b1, 1, 1);
   __builtin_amdgcn_sched_barrier(0);
+  if constexpr (Args::kMaskK) mask_a(r0, 0);
 #pragma unroll
   for (int kk = 0; kk < 2 * ACH; ++kk) expand_a(r0, 0, kk >> 1, kk & 1);
   if constexpr (PF == 3) {
@@ -473,10 +522,9 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
   static_assert(TN <= 2 && SR % (2 / TN) == 0, "4-byte stores: whole rows per instruction");
   uint32_t* E = reinterpret_cast<uint32_t*>(lds) + wave * 32 * EP;
   const uint32_t* E0 = reinterpret_cast<const uint32_t*>(lds) + (wave % (S::WM * S::WN)) * 32 * EP;
-  const bool part = a.partial != nullptr;
+  const bool part = a.sums();
   const float sc = part ? 0.0f : epilogue_scale<AC, NS, BSIGNED>(*a.alpha, *a.bscale);
-  uint32_t* out = part ? reinterpret_cast<uint32_t*>(a.partial + (int64_t)blockIdx.y * a.M * a.N)
-                       : reinterpret_cast<uint32_t*>(a.C);
+  uint32_t* out = a.out();
   const int64_t rbase = m0 + wm * TM * 32, cbase = n0 + wn * TN * 32;
   const int srow = lane / LPR, scol = (lane % LPR) * 4;
   __syncthreads();  // every wave is done with the stage buffers
@@ -512,7 +560,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
               for (int r = 0; r < 4; ++r) v[r] = __float_as_uint(__fmul_rn((float)(int32_t)v[r], sc));
             }
           }
-          *reinterpret_cast<v4u*>(out + row * a.N + col) = v;
+          *reinterpret_cast<v4u*>(out + row * a.row_c() + col) = v;
         }
       }
     } else if (cbase < a.N && rbase + i * 32 + kg * SR < a.M) {
@@ -524,7 +572,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
       const int wrow = el / WC, wcol = el % WC;
       const int64_t row0 = rbase + i * 32 + kg * SR, col = cbase + wcol;
       const int inside = (int)min(a.M - row0, (int64_t)SR), rows = inside - wrow;   // the lane's rows
-      uint32_t* const dst = out + (row0 + wrow) * a.N + col;
+      uint32_t* const dst = out + (row0 + wrow) * a.row_c() + col;
       const uint32_t* src = E0 + (kg * SR + wrow) * EP + wcol;
       auto batch = [&](int rr, auto u_, auto whole) __attribute__((always_inline)) {
         constexpr int U = decltype(u_)::value;
@@ -540,11 +588,11 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
           for (int u = 0; u < U; ++u)
             if (!part) v[u] = __float_as_uint(__fmul_rn((float)(int32_t)v[u], sc));
         }
-        uint32_t* const o = dst + rr * a.N;
+        uint32_t* const o = dst + rr * a.row_c();
         if (col < a.N) {
 #pragma unroll
           for (int u = 0; u < U; ++u)
-            if (decltype(whole)::value || rr + u * RS < rows) o[u * RS * a.N] = v[u];
+            if (decltype(whole)::value || rr + u * RS < rows) o[u * RS * a.row_c()] = v[u];
         }
       };
       if (inside == SR) {
@@ -555,6 +603,11 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs 
     }
     __syncthreads();  // the slab is rewritten by the next i
   }
+}
+
+template <int AC, int NS, bool BSIGNED, bool FULLK, int PF, typename S>
+__global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(GemmArgs a) {
+  gemm_tile<AC, NS, BSIGNED, FULLK, PF, S>(a);
 }
 
 // Sums the split-K chunk sums in int64 in a fixed order and applies the scales.  A

@@ -1,0 +1,219 @@
+// Positions grouped by id: a stable least-significant-digit radix sort of (id, position)
+// and the offsets of every id in the result.
+//
+// Each pass sorts by one digit of at most 9 bits: a histogram of every block's range, then
+// a scatter in which every block derives its bases from all blocks' histograms (so no
+// launch is spent on a scan) and ranks its keys by ballots, wave by wave in order of
+// position.  Nothing depends on the order in which blocks or atomics run: the histogram's
+// LDS atomics only count.
+//
+// Ids outside [0, groups) get the key `groups`, which sorts last.
+#include "luq_device.hpp"
+#include "luq_launch.hpp"
+
+namespace luq {
+
+namespace {
+
+constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
+constexpr int kSortThreads = 512, kSortWaves = kSortThreads / kWave;
+constexpr int kItems = 8, kPiece = kSortThreads * kItems;   // keys a block ranks at a time
+constexpr int kMaxSortBlocks = 256;
+
+// Where a pass reads its keys from.
+enum Source { kIds32, kIds64, kKeys };
+
+struct SortPass {
+  const void* keys;      // ids or keys
+  const int32_t* pos;    // positions of the keys, or null: the keys are in order of position
+  int64_t n, per;        // per: keys a block covers, a multiple of kPiece
+  uint32_t groups;
+  int shift, bits, blocks;
+};
+
+template <int SRC>
+__device__ __forceinline__ uint32_t load_key(const SortPass& a, int64_t i) {
+  if constexpr (SRC == kKeys) return static_cast<const uint32_t*>(a.keys)[i];
+  const int64_t id = SRC == kIds32 ? (int64_t)static_cast<const int32_t*>(a.keys)[i]
+                                   : static_cast<const int64_t*>(a.keys)[i];
+  return id >= 0 && id < (int64_t)a.groups ? (uint32_t)id : a.groups;
+}
+
+template <int SRC>
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPass a, uint32_t* counts) {
+  __shared__ uint32_t hist[kBins];
+  const int bins = 1 << a.bits;
+  for (int d = threadIdx.x; d < bins; d += kSortThreads) hist[d] = 0;
+  __syncthreads();
+  const int64_t lo = (int64_t)blockIdx.x * a.per, hi = min(lo + a.per, a.n);
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads)
+    atomicAdd(&hist[(load_key<SRC>(a, i) >> a.shift) & (bins - 1)], 1u);
+  __syncthreads();
+  for (int d = threadIdx.x; d < bins; d += kSortThreads) counts[(int64_t)blockIdx.x * bins + d] = hist[d];
+}
+
+// Exclusive prefix sums of one value per thread over the block; scratch holds a word per wave.
+__device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* scratch) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  uint32_t sum = v;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const uint32_t up = (uint32_t)__shfl_up((int)sum, d, kWave);
+    if (lane >= d) sum += up;
+  }
+  if (lane == kWave - 1) scratch[wave] = sum;
+  __syncthreads();
+  uint32_t before = 0;
+  for (int w = 0; w < wave; ++w) before += scratch[w];
+  __syncthreads();
+  return before + sum - v;
+}
+
+template <int SRC>
+__global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortPass a, const uint32_t* counts,
+                                                                   uint32_t* out_keys, int32_t* out_pos) {
+  __shared__ uint32_t base[kBins];
+  __shared__ uint32_t count[kSortWaves][kBins];
+  __shared__ uint32_t scratch[kSortWaves];
+  const int bins = 1 << a.bits, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  // where this block's keys of digit d begin: all smaller digits, then the blocks before
+  uint32_t total = 0, before = 0;
+  const int d0 = threadIdx.x;
+  if (d0 < bins)
+    for (int b = 0; b < a.blocks; ++b) {
+      const uint32_t c = counts[(int64_t)b * bins + d0];
+      if (b < (int)blockIdx.x) before += c;
+      total += c;
+    }
+  const uint32_t smaller = block_prefix(total, scratch);
+  if (d0 < bins) base[d0] = smaller + before;
+  const int64_t lo = (int64_t)blockIdx.x * a.per, hi = min(lo + a.per, a.n);
+  for (int64_t piece = lo; piece < hi; piece += kPiece) {
+    for (int w = 0; w < kSortWaves; ++w)
+      if (d0 < bins) count[w][d0] = 0;
+    __syncthreads();
+    // wave w ranks the keys [w * 64 * kItems, ...) of the piece, 64 at a time
+    uint32_t key[kItems], rank[kItems];
+    volatile uint32_t* mine = count[wave];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int64_t i = piece + (wave * kItems + k) * kWave + lane;
+      const bool in = i < hi;
+      key[k] = in ? load_key<SRC>(a, i) : 0;
+      const uint32_t d = (key[k] >> a.shift) & (bins - 1);
+      uint64_t same = __ballot(in);
+      for (int bit = 0; bit < a.bits; ++bit) {
+        const uint64_t set = __ballot((d >> bit) & 1);
+        same &= (d >> bit) & 1 ? set : ~set;
+      }
+      const uint64_t below = same & ((1ull << lane) - 1);
+      const uint32_t first = in ? mine[d] : 0;
+      rank[k] = first + __popcll(below);
+      // all lanes have read the count before the lowest lane of the digit raises it
+      if (in && below == 0) mine[d] = first + __popcll(same);
+    }
+    __syncthreads();
+    if (d0 < bins) {
+      uint32_t run = base[d0];
+      for (int w = 0; w < kSortWaves; ++w) {
+        const uint32_t c = count[w][d0];
+        count[w][d0] = run;
+        run += c;
+      }
+      base[d0] = run;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int64_t i = piece + (wave * kItems + k) * kWave + lane;
+      if (i < hi) {
+        const uint32_t at = count[wave][(key[k] >> a.shift) & (bins - 1)] + rank[k];
+        out_keys[at] = key[k];
+        out_pos[at] = a.pos ? a.pos[i] : (int32_t)i;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// offsets[v] = number of keys below v, by bisection of the sorted keys.
+__global__ __launch_bounds__(256) void group_offsets_kernel(const uint32_t* keys, int64_t n, int64_t groups,
+                                                            int32_t* offsets) {
+  const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (v > groups) return;
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (keys[mid] < (uint32_t)v) lo = mid + 1;
+    else hi = mid;
+  }
+  offsets[v] = (int32_t)lo;
+}
+
+struct SortPlan {
+  int passes, bits, blocks;
+  int64_t per;
+};
+
+SortPlan plan_sort(int64_t n, int64_t groups) {
+  int bits = 1;
+  while ((groups >> bits) != 0) ++bits;   // keys 0 .. groups
+  SortPlan p;
+  p.passes = (bits + kDigitBits - 1) / kDigitBits;
+  p.bits = (bits + p.passes - 1) / p.passes;
+  const int64_t pieces = (n + kPiece - 1) / kPiece;
+  const int64_t per = (pieces + kMaxSortBlocks - 1) / kMaxSortBlocks;
+  p.per = per * kPiece;
+  p.blocks = (int)((pieces + per - 1) / (per > 0 ? per : 1));
+  return p;
+}
+
+size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+}  // namespace
+
+// Two sets of keys and positions, and the blocks' histograms.
+size_t group_ids_workspace_bytes(int64_t n, int64_t groups) {
+  if (n == 0) return 0;
+  const SortPlan p = plan_sort(n, groups);
+  return 4 * round256((size_t)n * 4) + (size_t)p.blocks * kBins * 4;
+}
+
+hipError_t launch_group_ids(const void* ids, int i64, int64_t n, int64_t groups, int32_t* order, int32_t* offsets,
+                            void* ws, hipStream_t st) {
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  const size_t part = round256((size_t)n * 4);
+  const uint32_t* sorted = nullptr;
+  if (n > 0) {
+    const SortPlan p = plan_sort(n, groups);
+    uint32_t* const counts = reinterpret_cast<uint32_t*>(w + 4 * part);
+    SortPass a;
+    a.keys = ids;
+    a.pos = nullptr;
+    a.n = n;
+    a.per = p.per;
+    a.groups = (uint32_t)groups;
+    a.bits = p.bits;
+    a.blocks = p.blocks;
+    for (int pass = 0; pass < p.passes; ++pass) {
+      a.shift = pass * p.bits;
+      uint32_t* const keys = reinterpret_cast<uint32_t*>(w + 2 * (pass & 1) * part);
+      int32_t* const pos = pass + 1 == p.passes ? order : reinterpret_cast<int32_t*>(w + (2 * (pass & 1) + 1) * part);
+      auto launch = [&](auto count, auto scatter) {
+        hipLaunchKernelGGL(count, dim3(p.blocks), dim3(kSortThreads), 0, st, a, counts);
+        hipLaunchKernelGGL(scatter, dim3(p.blocks), dim3(kSortThreads), 0, st, a, counts, keys, pos);
+      };
+      if (pass > 0) launch(sort_count_kernel<kKeys>, sort_scatter_kernel<kKeys>);
+      else if (i64) launch(sort_count_kernel<kIds64>, sort_scatter_kernel<kIds64>);
+      else launch(sort_count_kernel<kIds32>, sort_scatter_kernel<kIds32>);
+      a.keys = keys;
+      a.pos = pos;
+      sorted = keys;
+    }
+  }
+  hipLaunchKernelGGL(group_offsets_kernel, dim3((unsigned)(groups / 256 + 1)), dim3(256), 0, st, sorted, n, groups,
+                     offsets);
+  return hipGetLastError();
+}
+
+}  // namespace luq

@@ -86,6 +86,38 @@ hipError_t launch_conv3x3_wgrad(const uint8_t* g, int64_t g_plane, int ns, const
                                 const float* ascale, int a_signed, int64_t B, int64_t H, int64_t W, int64_t C,
                                 int64_t Cout, float* dw, void* ws, hipStream_t st);
 
+// Operators of luq_lm.h.
+size_t group_ids_workspace_bytes(int64_t n, int64_t groups);
+hipError_t launch_group_ids(const void* ids, int i64, int64_t n, int64_t groups, int32_t* order, int32_t* offsets,
+                            void* ws, hipStream_t st);
+
+hipError_t launch_embedding_fwd(const void* ids, int i64, int64_t n, const void* table, int t_bf16, int64_t vocab,
+                                int64_t dim, float scale, void* out, int o_bf16, hipStream_t st);
+size_t embedding_grad_workspace_bytes(int64_t n, int64_t dim);
+hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, int i64, const int32_t* order,
+                                 const int32_t* offsets, int64_t n, int64_t vocab, int64_t dim, float scale,
+                                 int accumulate, float* dtable, void* ws, hipStream_t st);
+
+hipError_t launch_layernorm_fwd(const void* x, int bf16, int64_t rows, int64_t cols, const float* gamma,
+                                const float* beta, float eps, void* y, float* mean, float* rstd, hipStream_t st);
+size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+hipError_t launch_layernorm_bwd(const void* dy, int g_bf16, const void* x, int bf16, const float* mean,
+                                const float* rstd, const float* gamma, int64_t rows, int64_t cols, void* dx,
+                                float* dgamma, float* dbeta, void* ws, hipStream_t st);
+
+// Products grouped by expert; the A operand's codes.
+enum class GroupedA { kLuq, kSums, kInt4S, kInt4U };
+// C [T][N], the rows grouped; w_row and w_expert in codes.
+hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B, int64_t w_row,
+                               int64_t w_expert, const float* bscale, int64_t scales, int b_signed,
+                               const int32_t* offsets, int64_t experts, int64_t T, int64_t N, int64_t K, float* C,
+                               hipStream_t st);
+// C [experts][M][N], the reduction over T grouped.
+size_t grouped_depth_workspace_bytes(int64_t T, int64_t M, int64_t N, int64_t experts);
+hipError_t launch_grouped_depth(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B,
+                                const float* bscale, int b_signed, const int32_t* offsets, int64_t experts, int64_t T,
+                                int64_t M, int64_t N, float* C, void* ws, hipStream_t st);
+
 hipError_t launch_im2col3x3_t(const uint8_t* act, int64_t B, int64_t H, int64_t W, int64_t C,
                               uint8_t* col_t, hipStream_t st);
 

@@ -1,0 +1,229 @@
+"""luq_layernorm_fwd and luq_layernorm_bwd against plain forms in 64 bits, through the C ABI."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from gpu_util import announce, host  # noqa: E402
+import lm_util as U  # noqa: E402
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+COLS = [1, 2, 3, 7, 8, 63, 64, 65, 130, 511, 512, 513, 1001, 1024, 2047, 2048, 2056, 4096, 5003, 8192, 8200, 16384,
+        16391, 32768, 32776, 40001]
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2112_10769_amd as lib
+    return lib
+
+
+def _inputs(rows, cols, dt, gt=None, seed=0, mean=0.5):
+    gen = torch.Generator(device="cuda").manual_seed(seed + rows * 131 + cols)
+    x = (torch.randn(rows, cols, device="cuda", generator=gen) * 1.5 + mean).to(DT[dt])
+    gamma = 1.0 + 0.2 * torch.randn(cols, device="cuda", generator=gen)
+    beta = 0.3 * torch.randn(cols, device="cuda", generator=gen)
+    dy = (torch.randn(rows, cols, device="cuda", generator=gen) * 0.01).to(DT[gt or dt])
+    return x, gamma, beta, dy
+
+
+def _forward(L, x, gamma, beta, eps, what, **kw):
+    announce("layernorm_fwd", what)
+    got = L.luq_layernorm_fwd(x, gamma, beta, eps, **kw)
+    return [host(v.float()) for v in got]
+
+
+def _check_forward(got, x, gamma, beta, eps, what):
+    ref, bound = U.layernorm(host(x.float()), None if gamma is None else host(gamma),
+                             None if beta is None else host(beta), eps, x.dtype == torch.bfloat16)
+    for g, r, b, name in zip(got, ref, bound, ("y", "mean", "rstd")):
+        U.within(g, r, b, (what, name))
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_forward(L, cols, dt):
+    for rows in (1, 5, 67):
+        x, gamma, beta, _ = _inputs(rows, cols, dt)
+        _check_forward(_forward(L, x, gamma, beta, 1e-5, (rows, cols, dt)), x, gamma, beta, 1e-5, (rows, cols, dt))
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("dt,gt", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+def test_backward(L, cols, dt, gt):
+    for rows in (1, 6, 133):
+        x, gamma, beta, dy = _inputs(rows, cols, dt, gt)
+        _, mean, rstd = L.luq_layernorm_fwd(x, gamma, beta)
+        announce("layernorm_bwd", rows, cols, dt, gt)
+        got = L.luq_layernorm_bwd(dy, x, mean, rstd, gamma)
+        ref, bound = U.layernorm_grad(host(dy.float()), host(x.float()), host(mean), host(rstd), host(gamma),
+                                      gt == "bf16")
+        for g, r, b, name in zip(got, ref, bound, ("dx", "dgamma", "dbeta")):
+            U.within(host(g.float()), r, b, (rows, cols, dt, gt, name))
+        again = L.luq_layernorm_bwd(dy, x, mean, rstd, gamma)
+        assert all(torch.equal(a, b) for a, b in zip(got, again)), "the order of the sums is fixed"
+
+
+@pytest.mark.parametrize("rows,cols", [(3000, 40), (2050, 513), (5000, 1024), (1027, 4100), (700, 9000)])
+def test_many_rows(L, rows, cols):
+    x, gamma, beta, dy = _inputs(rows, cols, "bf16", "f32")
+    got = _forward(L, x, gamma, beta, 1e-5, (rows, cols))
+    _check_forward(got, x, gamma, beta, 1e-5, (rows, cols))
+    _, mean, rstd = L.luq_layernorm_fwd(x, gamma, beta)
+    announce("layernorm_bwd", rows, cols)
+    got = L.luq_layernorm_bwd(dy, x, mean, rstd, gamma)
+    ref, bound = U.layernorm_grad(host(dy), host(x.float()), host(mean), host(rstd), host(gamma), False)
+    for g, r, b, name in zip(got, ref, bound, ("dx", "dgamma", "dbeta")):
+        U.within(host(g), r, b, (rows, cols, name))
+
+
+def test_without_weight_and_bias(L):
+    x, gamma, beta, dy = _inputs(9, 300, "f32")
+    for g, b in ((None, None), (gamma, None), (None, beta)):
+        _check_forward(_forward(L, x, g, b, 1e-5, "parts"), x, g, b, 1e-5, "parts")
+    _, mean, rstd = L.luq_layernorm_fwd(x)
+    got = L.luq_layernorm_bwd(dy, x, mean, rstd)
+    ref, bound = U.layernorm_grad(host(dy), host(x), host(mean), host(rstd), None, False)
+    for g, r, b in zip(got, ref, bound):
+        U.within(host(g), r, b, "no weight")
+
+
+@pytest.mark.parametrize("mean", [1e3, -3e4])
+def test_rows_far_from_zero(L, mean):
+    """The variance from the differences keeps its digits where E[x^2] - mean^2 has none left."""
+    x, gamma, beta, _ = _inputs(33, 3001, "f32", mean=mean)
+    _check_forward(_forward(L, x, gamma, beta, 1e-5, mean), x, gamma, beta, 1e-5, mean)
+
+
+def test_constant_and_extreme_rows(L):
+    """A constant row gives beta; NaN and infinity stay in their rows; huge and tiny rows."""
+    cols = 777
+    x = torch.full((6, cols), 2.5, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x[1:] = torch.randn(5, cols, device="cuda", generator=gen)
+    x[2, 5], x[3, 9] = float("nan"), float("inf")
+    x[4] *= 1e17
+    x[5] *= 1e-18
+    gamma, beta = torch.ones(cols, device="cuda"), torch.full((cols,), 0.25, device="cuda")
+    y, mean, rstd = _forward(L, x, gamma, beta, 1e-5, "extreme")
+    assert (y[0] == 0.25).all() and abs(rstd[0] - 1e-5 ** -0.5) < 1e-3
+    assert np.isnan(y[2]).all() and np.isnan(y[3]).all()
+    keep = [1, 4, 5]
+    (ry, rm, rr), (by, bm, br) = U.layernorm(host(x)[keep], host(gamma), host(beta), 1e-5, False)
+    U.within(y[keep], ry, by, "extreme")
+    U.within(rstd[keep], rr, br, "extreme rstd")
+    dy = torch.ones(6, cols, device="cuda")
+    dx, dgamma, dbeta = L.luq_layernorm_bwd(dy, x, torch.from_numpy(mean).cuda(), torch.from_numpy(rstd).cuda(), gamma)
+    assert np.isfinite(host(dx)[[0, 1, 4, 5]]).all() and np.isnan(host(dx)[2]).all()
+    assert (host(dbeta) == 6).all()
+
+
+def test_no_rows(L):
+    announce("layernorm no rows")
+    for cols in (5, 1024):
+        x = torch.empty(0, cols, device="cuda")
+        y, mean, rstd = L.luq_layernorm_fwd(x)
+        nan = torch.full((cols,), float("nan"), device="cuda")
+        _, dgamma, dbeta = L.luq_layernorm_bwd(x, x, mean, rstd, dgamma=nan.clone(), dbeta=nan.clone())
+        assert (dgamma == 0).all() and (dbeta == 0).all()
+
+
+@pytest.mark.parametrize("cols", [100, 1001, 4096, 40001])
+def test_in_place(L, cols):
+    """y over x, and dx over dy."""
+    x, gamma, beta, dy = _inputs(70, cols, "bf16")
+    y, mean, rstd = L.luq_layernorm_fwd(x, gamma, beta)
+    dx, dgamma, dbeta = L.luq_layernorm_bwd(dy, x, mean, rstd, gamma)
+    x2, dy2 = x.clone(), dy.clone()
+    announce("layernorm in place", cols)
+    L.luq_layernorm_fwd(x2, gamma, beta, y=x2)
+    assert torch.equal(x2, y)
+    _, dgamma2, dbeta2 = L.luq_layernorm_bwd(dy2, x, mean, rstd, gamma, dx=dy2)
+    assert torch.equal(dy2, dx) and torch.equal(dgamma2, dgamma) and torch.equal(dbeta2, dbeta)
+
+
+@pytest.mark.parametrize("offset", [1, 2, 3])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_unaligned(L, offset, dt):
+    """Tensors that begin anywhere inside a 16-byte piece; nothing outside them is written."""
+    rows, cols = 21, 1024
+    x0, gamma, beta, dy0 = _inputs(rows, cols, dt)
+    n = rows * cols
+
+    def moved(t):
+        f = torch.zeros(n + 8, dtype=t.dtype, device="cuda")
+        f[offset:offset + n] = t.reshape(-1)
+        return f, f[offset:offset + n].view(rows, cols)
+    _, x = moved(x0)
+    _, dy = moved(dy0)
+    fy, y = moved(torch.zeros_like(x0))
+    fdx, dx = moved(torch.zeros_like(x0))
+    g1 = torch.zeros(cols + 8, device="cuda")
+    g1[offset:offset + cols] = gamma
+    gm = g1[offset:offset + cols]
+    announce("layernorm unaligned", offset, dt)
+    _, mean, rstd = L.luq_layernorm_fwd(x, gm, beta, y=y)
+    got = (y, mean, rstd)
+    _check_forward([host(v.float()) for v in got], x0, gamma, beta, 1e-5, offset)
+    got = L.luq_layernorm_bwd(dy, x, mean, rstd, gm, dx=dx)
+    ref, bound = U.layernorm_grad(host(dy0.float()), host(x0.float()), host(mean), host(rstd), host(gamma), dt == "bf16")
+    for g, r, b in zip(got, ref, bound):
+        U.within(host(g.float()), r, b, offset)
+    for f in (fy, fdx):
+        assert not f[:offset].any() and not f[offset + n:].any()
+
+
+def test_strided_input(L):
+    x, gamma, beta, dy = _inputs(40, 256, "f32")
+    wide = torch.zeros(40, 300, device="cuda")
+    wide[:, :256] = x
+    got = _forward(L, wide[:, :256], gamma, beta, 1e-5, "strided")
+    _check_forward(got, x, gamma, beta, 1e-5, "strided")
+
+
+def test_gradient_is_the_derivative(L):
+    """Against differences of the 64-bit forward pass, along random directions."""
+    rows, cols, eps = 12, 96, 1e-3
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((rows, cols)).astype(np.float32)
+    gamma = (1 + 0.3 * rng.standard_normal(cols)).astype(np.float32)
+    beta = rng.standard_normal(cols).astype(np.float32)
+    dy = rng.standard_normal((rows, cols)).astype(np.float32)
+    dev = [torch.from_numpy(v).cuda() for v in (x, gamma, beta, dy)]
+    _, mean, rstd = L.luq_layernorm_fwd(dev[0], dev[1], dev[2], eps)
+    announce("layernorm_bwd differences")
+    dx, dgamma, dbeta = (host(v).astype(np.float64) for v in L.luq_layernorm_bwd(dev[3], dev[0], mean, rstd, dev[1]))
+
+    def loss(x, gamma, beta):
+        return float((U.layernorm(x, gamma, beta, eps, False)[0][0] * dy).sum())
+    h = 1e-4
+    for k in range(4):
+        vx, vg, vb = (rng.standard_normal(s) for s in ((rows, cols), cols, cols))
+        for name, d, v, at in (("x", dx, vx, 0), ("gamma", dgamma, vg, 1), ("beta", dbeta, vb, 2)):
+            args = [x.astype(np.float64), gamma.astype(np.float64), beta.astype(np.float64)]
+            up, down = list(args), list(args)
+            up[at], down[at] = args[at] + h * v, args[at] - h * v
+            slope = (loss(*up) - loss(*down)) / (2 * h)
+            # truncation h^2 times a third derivative of order |dy| |v|^3, fp32 statistics and sums
+            tol = 1e-5 * np.abs(d * v).sum() + 10 * h * h * np.abs(dy).sum()
+            assert abs((d * v).sum() - slope) <= tol, (name, k)
+
+
+def test_beyond_32_bits(L):
+    """Rows past 2^31 elements."""
+    rows, cols = 70001, 32768
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    last, gamma, beta, _ = _inputs(1, cols, "bf16")
+    x[-1] = last[0]
+    announce("layernorm 64-bit offsets")
+    y, mean, rstd = L.luq_layernorm_fwd(x, gamma, beta)
+    _check_forward([host(v[-1:].float()) for v in (y, mean, rstd)], last, gamma, beta, 1e-5, "last row")
+    dy = host(y[-1:].float())
+    dx, dgamma, dbeta = L.luq_layernorm_bwd(y, x, mean, rstd, gamma, dx=y)
+    ref, bound = U.layernorm_grad(dy, host(last.float()), host(mean[-1:]), host(rstd[-1:]), host(gamma), True)
+    U.within(host(dx[-1:].float()), ref[0], bound[0], "last row")
+    del x, y, dx
+    torch.cuda.empty_cache()

@@ -1,0 +1,210 @@
+"""The entry points of include/luq_lm.h: exported, declared in the binding, and refusing
+invalid arguments on the host.  Every call here fails its checks: nothing is enqueued."""
+import ctypes
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "luq_lm.h")
+
+torch = pytest.importorskip("torch")
+luq = pytest.importorskip("paper_2112_10769_amd")
+LIB = luq.LIB
+
+P, P2, P3 = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x20000), ctypes.c_void_p(0x30000)
+P4, P8 = ctypes.c_void_p(0x10004), ctypes.c_void_p(0x10008)
+ODD, HALF = ctypes.c_void_p(0x10001), ctypes.c_void_p(0x10002)
+NUL = None
+WS = 1 << 40
+SHAPE, DTYPE, PARAM, NULL, WSP, ALIGN = 2, 3, 4, 1, 5, 6
+
+
+def test_declared_functions_are_exported():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"^[a-z_][\w \*]*?\b((?:luq|int4)_\w+)\s*\(", text, flags=re.M))
+    assert names == set(luq.EXPORTS_LM)
+    for n in names:
+        assert hasattr(LIB, n) and (hasattr(luq, n) or n == "luq_grouped_wgrad_workspace")
+
+
+def _call(fn, defaults, kw):
+    a = dict(defaults, **kw)
+    assert set(a) == set(defaults)
+    return getattr(LIB, fn)(*a.values())
+
+
+GROUP = dict(ids=P, it=0, n=100, groups=10, order=P2, offsets=P3, ws=P, ws_bytes=WS, stream=NUL)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(it=2), DTYPE), (dict(n=-1), SHAPE), (dict(n=(1 << 30) + 1), SHAPE), (dict(groups=0), SHAPE),
+    (dict(groups=(1 << 30) + 1), SHAPE), (dict(ids=NUL), NULL), (dict(order=NUL), NULL), (dict(offsets=NUL), NULL),
+    (dict(ids=ODD), ALIGN), (dict(ids=P4, it=1), ALIGN), (dict(order=HALF), ALIGN), (dict(offsets=HALF), ALIGN),
+    (dict(ws=NUL), WSP), (dict(ws_bytes=0), WSP), (dict(ws=P8), ALIGN),
+])
+def test_group_ids(kw, status):
+    assert _call("luq_group_ids", GROUP, kw) == status
+    assert LIB.luq_last_error()
+
+
+LOOKUP = dict(ids=P, it=0, n=10, table=P2, tt=0, vocab=100, dim=8, scale=1.0, out=P3, ot=0, stream=NUL)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(it=-1), DTYPE), (dict(tt=2), DTYPE), (dict(ot=5), DTYPE), (dict(n=-1), SHAPE), (dict(vocab=-1), SHAPE),
+    (dict(dim=0), SHAPE), (dict(n=1 << 30, dim=1 << 30), SHAPE), (dict(vocab=1 << 30, dim=1 << 30, n=0), SHAPE),
+    (dict(ids=NUL), NULL), (dict(table=NUL), NULL), (dict(out=NUL), NULL), (dict(ids=P4, it=1), ALIGN),
+    (dict(table=HALF), ALIGN), (dict(out=HALF), ALIGN), (dict(table=ODD, tt=1), ALIGN), (dict(out=ODD, ot=1), ALIGN),
+])
+def test_embedding_fwd(kw, status):
+    assert _call("luq_embedding_fwd", LOOKUP, kw) == status
+    assert LIB.luq_last_error()
+
+
+GRAD = dict(dout=P, gt=0, ids=P, it=0, order=P2, offsets=P2, n=10, vocab=100, dim=8, scale=1.0, accumulate=0, dtable=P3,
+            ws=P, ws_bytes=WS, stream=NUL)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(gt=2), DTYPE), (dict(it=2), DTYPE), (dict(n=-1), SHAPE), (dict(vocab=0), SHAPE), (dict(dim=0), SHAPE),
+    (dict(vocab=1 << 30, dim=1 << 30), SHAPE), (dict(accumulate=2), PARAM), (dict(dout=NUL), NULL), (dict(ids=NUL), NULL),
+    (dict(order=NUL), NULL), (dict(offsets=NUL), NULL), (dict(dtable=NUL), NULL), (dict(dout=HALF), ALIGN),
+    (dict(dtable=HALF), ALIGN), (dict(order=ODD), ALIGN), (dict(ids=P4, it=1), ALIGN),
+])
+def test_embedding_grad(kw, status):
+    assert _call("luq_embedding_grad", GRAD, kw) == status
+    assert LIB.luq_last_error()
+
+
+NORM = dict(x=P, dt=0, rows=4, cols=8, gamma=P2, beta=P2, eps=1e-5, y=P3, mean=P2, rstd=P2, stream=NUL)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=2), DTYPE), (dict(rows=-1), SHAPE), (dict(cols=0), SHAPE), (dict(rows=1 << 30, cols=1 << 30), SHAPE),
+    (dict(eps=-1e-9), PARAM), (dict(eps=float("nan")), PARAM), (dict(eps=float("inf")), PARAM), (dict(x=NUL), NULL),
+    (dict(y=NUL), NULL), (dict(x=HALF), ALIGN), (dict(x=ODD, dt=1), ALIGN), (dict(gamma=HALF), ALIGN),
+    (dict(beta=ODD), ALIGN), (dict(mean=HALF), ALIGN), (dict(rstd=HALF), ALIGN),
+])
+def test_layernorm_fwd(kw, status):
+    assert _call("luq_layernorm_fwd", NORM, kw) == status
+    assert LIB.luq_last_error()
+
+
+NORM_BWD = dict(dy=P, gt=0, x=P, dt=0, mean=P2, rstd=P2, gamma=P2, rows=4, cols=8, dx=P3, dgamma=P3, dbeta=P3, ws=P,
+                ws_bytes=WS, stream=NUL)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(gt=2), DTYPE), (dict(dt=2), DTYPE), (dict(rows=-1), SHAPE), (dict(cols=0), SHAPE), (dict(dy=NUL), NULL),
+    (dict(x=NUL), NULL), (dict(mean=NUL), NULL), (dict(rstd=NUL), NULL), (dict(dx=NUL), NULL), (dict(dy=HALF), ALIGN),
+    (dict(dx=ODD, gt=1), ALIGN), (dict(x=HALF), ALIGN), (dict(dgamma=HALF), ALIGN), (dict(dbeta=HALF), ALIGN),
+])
+def test_layernorm_bwd(kw, status):
+    assert _call("luq_layernorm_bwd", NORM_BWD, kw) == status
+    assert LIB.luq_last_error()
+
+
+FWD = dict(x=P, xs=P2, x_signed=1, w=P, w_row=64, w_expert=640, ws=P2, w_scales=4, w_signed=1, offsets=P3, experts=4, T=100,
+           N=10, K=64, y=P3, stream=NUL)
+ROWS_BAD = [
+    (dict(experts=0), SHAPE), (dict(experts=4097, w_scales=1), SHAPE), (dict(T=-1), SHAPE), (dict(T=(1 << 30) + 1), SHAPE),
+    (dict(N=0), SHAPE), (dict(K=48), SHAPE), (dict(K=0), SHAPE), (dict(K=(1 << 18) + 32, w_row=(1 << 18) + 32), SHAPE),
+    (dict(w_row=32), SHAPE), (dict(w_row=72), SHAPE), (dict(w_row=(1 << 22) + 32), SHAPE), (dict(w_expert=-32), SHAPE),
+    (dict(w_expert=648), SHAPE), (dict(w_scales=3), SHAPE), (dict(T=1 << 25, N=1 << 12), SHAPE), (dict(x=NUL), NULL),
+    (dict(xs=NUL), NULL), (dict(w=NUL), NULL), (dict(ws=NUL), NULL), (dict(offsets=NUL), NULL), (dict(y=NUL), NULL),
+    (dict(x=P8), ALIGN), (dict(w=P8), ALIGN), (dict(y=HALF), ALIGN), (dict(xs=HALF), ALIGN), (dict(offsets=HALF), ALIGN),
+]
+
+
+@pytest.mark.parametrize("kw,status", ROWS_BAD + [(dict(K=(1 << 17) + 32, w_row=(1 << 17) + 32), SHAPE)])
+def test_forward_grouped(kw, status):
+    assert _call("int4_gemm_fwd_grouped", FWD, kw) == status
+    assert LIB.luq_last_error()
+
+
+DGRAD = dict(x=P, xs=P2, n_samples=1, w=P, w_row=64, w_expert=640, ws=P2, w_scales=4, w_signed=1, offsets=P3, experts=4,
+             T=100, N=10, K=64, y=P3, stream=NUL)
+
+
+@pytest.mark.parametrize("kw,status", ROWS_BAD + [(dict(n_samples=2), PARAM), (dict(n_samples=0), PARAM),
+                                                  (dict(n_samples=0x41), PARAM), (dict(n_samples=0x11), PARAM)])
+def test_dgrad_grouped(kw, status):
+    assert _call("luq_gemm_dgrad_grouped", DGRAD, kw) == status
+    assert LIB.luq_last_error()
+
+
+WGRAD = dict(g=P, alpha=P2, n_samples=1, a=P, a_scale=P2, a_signed=1, offsets=P3, experts=4, T=128, Nout=10, Kin=20, dw=P3,
+             ws=P, ws_bytes=WS, stream=NUL)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_samples=2), PARAM), (dict(n_samples=0x41), PARAM), (dict(experts=0), SHAPE), (dict(experts=4097), SHAPE),
+    (dict(T=0), SHAPE), (dict(T=40), SHAPE), (dict(T=(1 << 18) + 32), SHAPE), (dict(Nout=0), SHAPE), (dict(Kin=0), SHAPE),
+    (dict(Nout=1 << 30, Kin=1 << 30), SHAPE), (dict(g=NUL), NULL), (dict(alpha=NUL), NULL), (dict(a=NUL), NULL),
+    (dict(a_scale=NUL), NULL), (dict(offsets=NUL), NULL), (dict(dw=NUL), NULL), (dict(g=P8), ALIGN), (dict(a=P4), ALIGN),
+    (dict(dw=HALF), ALIGN), (dict(alpha=ODD), ALIGN),
+])
+def test_wgrad_grouped(kw, status):
+    assert _call("luq_gemm_wgrad_grouped", WGRAD, kw) == status
+    assert LIB.luq_last_error()
+
+
+def test_workspace_queries_take_any_sizes():
+    big = 1 << 62
+    for op in (luq.OP_GROUP_IDS, luq.OP_EMBEDDING_GRAD, luq.OP_LAYERNORM_BWD):
+        for d in ((-1, 5), (5, -1), (5, 0), (big, big), (big, 1), (1, big), (1 << 30, 1 << 30)):
+            if op == luq.OP_GROUP_IDS and d == (1 << 30, 1 << 30):
+                continue
+            assert luq.workspace_size(op, *d) == 0, (op, d)
+    for d in ((0, 1, 1, 1), (31, 1, 1, 1), (32, 0, 1, 1), (32, big, big, 1), (32, 1, 1, 0), (32, 1, 1, big), (big, 1, 1, 1)):
+        assert luq.grouped_wgrad_workspace(*d) == 0, d
+
+
+def test_binding_checks_buffers():
+    """Wrong dtypes, sizes and devices are refused before any pointer is taken."""
+    ids = torch.zeros(5, dtype=torch.int64)
+    with pytest.raises(TypeError):
+        luq.luq_group_ids(ids.float(), 3)
+    with pytest.raises(ValueError):
+        luq.luq_group_ids(ids, 3, order=torch.zeros(5, dtype=torch.int64))
+    with pytest.raises(ValueError):
+        luq.luq_group_ids(ids, 3, offsets=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        luq.luq_embedding_fwd(ids, torch.zeros(4))
+    with pytest.raises(TypeError):
+        luq.luq_embedding_fwd(ids, torch.zeros(4, 2, dtype=torch.float64))
+    with pytest.raises(ValueError):
+        luq.luq_embedding_fwd(ids, torch.zeros(4, 2), out=torch.zeros(5, 3))
+    order, offsets = torch.zeros(5, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        luq.luq_embedding_grad(torch.zeros(4, 2), ids, order, offsets)
+    with pytest.raises(ValueError):
+        luq.luq_embedding_grad(torch.zeros(5, 2), ids, order[:4], offsets)
+    with pytest.raises(ValueError):
+        luq.luq_embedding_grad(torch.zeros(5, 2), ids, order, offsets.long())
+    with pytest.raises(ValueError):
+        luq.luq_embedding_grad(torch.zeros(5, 2), ids, order, offsets, accumulate=True)
+    x = torch.zeros(4, 6)
+    with pytest.raises(ValueError):
+        luq.luq_layernorm_fwd(x, gamma=torch.zeros(5))
+    with pytest.raises(ValueError):
+        luq.luq_layernorm_fwd(x, beta=torch.zeros(6, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        luq.luq_layernorm_fwd(x, y=torch.zeros(6, 4).t())
+    with pytest.raises(ValueError):
+        luq.luq_layernorm_bwd(torch.zeros(4, 5), x, torch.zeros(4), torch.zeros(4))
+    with pytest.raises(ValueError):
+        luq.luq_layernorm_bwd(x, x, torch.zeros(3), torch.zeros(4))
+    codes, one = torch.zeros(64, dtype=torch.uint8), torch.ones(1)
+    with pytest.raises(ValueError):
+        luq.int4_gemm_fwd_grouped(codes, one, True, codes[:31], one, True, offsets, 4, 1, 32)
+    with pytest.raises(ValueError):
+        luq.int4_gemm_fwd_grouped(codes, one, True, codes, torch.ones(2), True, offsets, 4, 1, 32)
+    with pytest.raises(ValueError):
+        luq.luq_gemm_dgrad_grouped(codes, one, codes, one, True, offsets, 40, 1, 32)
+    with pytest.raises(ValueError):
+        luq.luq_gemm_wgrad_grouped(codes, one, codes, one, True, offsets.long(), 32, 1, 1)
+    with pytest.raises(ValueError):
+        luq.luq_gemm_wgrad_grouped(codes, one, codes, one, True, offsets, 32, 5, 1)
