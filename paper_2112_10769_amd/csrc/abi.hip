@@ -28,8 +28,10 @@ luq_status hip_status(hipError_t e) {
   return fail(LUQ_ERR_HIP, "HIP launch failed: %s", hipGetErrorString(e));
 }
 
-constexpr int64_t kMaxRows = (int64_t)1 << 30;        // rows, ids, groups and columns
-constexpr int64_t kMaxElements = (int64_t)1 << 48;    // of one tensor: no byte offset overflows
+// Sizes of the operators of luq_lm.h: no tensor in memory is larger, and grids of these
+// stay below 2^32 threads.
+constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxGroups = (int64_t)1 << 28, kMaxCols = (int64_t)1 << 23;
+constexpr int64_t kMaxElements = (int64_t)1 << 38;
 
 // p holds elements of `size` bytes.
 bool aligned_to(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) == 0; }
@@ -112,10 +114,10 @@ static size_t gemm_workspace(int64_t M, int64_t N, int64_t K) {
 
 // Sizes that luq_group_ids and the row operators take.
 static bool group_sizes(int64_t n, int64_t groups) {
-  return n >= 0 && n <= kMaxRows && groups >= 1 && groups <= kMaxRows;
+  return n >= 0 && n <= kMaxRows && groups >= 1 && groups <= kMaxGroups;
 }
 static bool row_sizes(int64_t rows, int64_t cols) {
-  return rows >= 0 && rows <= kMaxRows && cols >= 1 && cols <= kMaxRows && rows * cols <= kMaxElements;
+  return rows >= 0 && rows <= kMaxRows && cols >= 1 && cols <= kMaxCols && rows * cols <= kMaxElements;
 }
 
 size_t luq_workspace_size(int op, int64_t d0, int64_t d1, int64_t d2) {
@@ -461,7 +463,7 @@ luq_status luq_group_ids(const void* ids, luq_index it, int64_t n, int64_t group
   g_last_error[0] = 0;
   luq_status st = check_index(fn, it);
   if (st != LUQ_OK) return st;
-  if (!group_sizes(n, groups)) return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30] and groups in [1, 2^30]", fn);
+  if (!group_sizes(n, groups)) return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30] and groups in [1, 2^28]", fn);
   if (!offsets || (n > 0 && (!ids || !order))) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
   if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned4(order) || !aligned4(offsets))
     return fail(LUQ_ERR_ALIGN, "%s: ids, order or offsets misaligned", fn);
@@ -478,8 +480,8 @@ luq_status luq_embedding_fwd(const void* ids, luq_index it, int64_t n, const voi
   luq_status st = check_index(fn, it);
   if (st == LUQ_OK) st = check_types(fn, tt, ot);
   if (st != LUQ_OK) return st;
-  if (!row_sizes(n, dim) || vocab < 0 || vocab > kMaxRows || vocab * dim > kMaxElements)
-    return fail(LUQ_ERR_SHAPE, "%s: n and vocab in [0, 2^30], dim in [1, 2^30]", fn);
+  if (!row_sizes(n, dim) || vocab < 0 || vocab > kMaxGroups || vocab * dim > kMaxElements)
+    return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30], vocab in [0, 2^28], dim in [1, 2^23]", fn);
   if (n == 0) return LUQ_OK;
   if (!ids || !out || (vocab > 0 && !table)) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
   if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned_to(table, elem_size(tt)) || !aligned_to(out, elem_size(ot)))
@@ -496,8 +498,8 @@ luq_status luq_embedding_grad(const void* dout, luq_dtype gt, const void* ids, l
   luq_status st = check_index(fn, it);
   if (st == LUQ_OK) st = check_types(fn, gt, gt);
   if (st != LUQ_OK) return st;
-  if (!row_sizes(n, dim) || vocab < 1 || vocab > kMaxRows || vocab * dim > kMaxElements)
-    return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30], vocab and dim in [1, 2^30]", fn);
+  if (!row_sizes(n, dim) || vocab < 1 || vocab > kMaxGroups || vocab * dim > kMaxElements)
+    return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30], vocab in [1, 2^28], dim in [1, 2^23]", fn);
   if (accumulate != 0 && accumulate != 1) return fail(LUQ_ERR_PARAM, "%s: accumulate must be 0 or 1", fn);
   if (!offsets || !dtable || (n > 0 && (!dout || !ids || !order))) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
   if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned_to(dout, elem_size(gt)) || !aligned4(order) ||
@@ -515,7 +517,7 @@ luq_status luq_layernorm_fwd(const void* x, luq_dtype dt, int64_t rows, int64_t 
   g_last_error[0] = 0;
   luq_status st = check_types(fn, dt, dt);
   if (st != LUQ_OK) return st;
-  if (!row_sizes(rows, cols)) return fail(LUQ_ERR_SHAPE, "%s: rows in [0, 2^30] and cols in [1, 2^30]", fn);
+  if (!row_sizes(rows, cols)) return fail(LUQ_ERR_SHAPE, "%s: rows in [0, 2^30] and cols in [1, 2^23]", fn);
   if (!(eps >= 0.0f && eps < __builtin_inff())) return fail(LUQ_ERR_PARAM, "%s: eps must be finite and >= 0", fn);
   if (rows > 0 && (!x || !y)) return fail(LUQ_ERR_NULL, "%s: x or y is NULL", fn);
   if (!aligned_to(x, elem_size(dt)) || !aligned_to(y, elem_size(dt)) || !aligned4(gamma) || !aligned4(beta) ||
@@ -532,7 +534,7 @@ luq_status luq_layernorm_bwd(const void* dy, luq_dtype gt, const void* x, luq_dt
   g_last_error[0] = 0;
   luq_status st = check_types(fn, gt, dt);
   if (st != LUQ_OK) return st;
-  if (!row_sizes(rows, cols)) return fail(LUQ_ERR_SHAPE, "%s: rows in [0, 2^30] and cols in [1, 2^30]", fn);
+  if (!row_sizes(rows, cols)) return fail(LUQ_ERR_SHAPE, "%s: rows in [0, 2^30] and cols in [1, 2^23]", fn);
   if (rows > 0 && (!dy || !x || !mean || !rstd || !dx)) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
   if (!aligned_to(dy, elem_size(gt)) || !aligned_to(dx, elem_size(gt)) || !aligned_to(x, elem_size(dt)) ||
       !aligned4(mean) || !aligned4(rstd) || !aligned4(gamma) || !aligned4(dgamma) || !aligned4(dbeta))

@@ -12,37 +12,215 @@ namespace luq {
 
 namespace {
 
-template <typename ID, typename TT, typename OT>
-__global__ __launch_bounds__(256) void embedding_fwd_kernel(const ID* ids, const TT* table, int64_t vocab, int64_t dim,
-                                                            float scale, OT* out) {
-  const int64_t i = blockIdx.x, id = ids[i];
-  OT* const dst = out + i * dim;
-  const TT* const src = table + id * dim;
-  for (int64_t c = threadIdx.x; c < dim; c += 256) {
-    float v = 0.0f;
-    if (id >= vocab) v = __builtin_nanf("");
-    else if (id >= 0) v = __fmul_rn(to_f32(src[c]), scale);
-    dst[c] = from_f32<OT>(v);
+// ---- lookup ------------------------------------------------------------------------------
+
+// A row is taken by 2^log_lanes lanes of each block along y, kRows rows of a lane group in
+// flight together.
+template <typename ID, typename TT, typename OT, int kRows>
+__global__ __launch_bounds__(256) void embedding_fwd_kernel(const ID* __restrict__ ids, int64_t n,
+                                                            const TT* __restrict__ table, int64_t vocab, int64_t dim,
+                                                            float scale, OT* __restrict__ out, int log_lanes) {
+  constexpr int V = kPack<TT, OT>;
+  const int lanes = 1 << log_lanes, groups = 256 >> log_lanes;
+  const int64_t first = ((int64_t)blockIdx.x * groups + (threadIdx.x >> log_lanes)) * kRows;
+  int64_t id[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) id[r] = first + r < n ? (int64_t)ids[first + r] : -1;
+  const int64_t step = (int64_t)gridDim.y * lanes * V;
+  for (int64_t c = ((int64_t)blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * V; c < dim; c += step) {
+    float v[kRows][V];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      if (id[r] >= 0 && id[r] < vocab) load_row<V>(table + id[r] * dim + c, dim - c, v[r]);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const bool row = id[r] >= 0 && id[r] < vocab;
+      const float none = id[r] >= 0 ? __builtin_nanf("") : 0.0f;   // off the table, or padding
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[r][k] = row ? __fmul_rn(v[r][k], scale) : none;
+      if (first + r < n) store_row<V>(out + (first + r) * dim + c, dim - c, v[r]);
+    }
   }
 }
 
-template <typename GT>
-__global__ __launch_bounds__(256) void embedding_grad_kernel(const GT* dout, const int32_t* order, const int32_t* offsets,
-                                                             int64_t n, int64_t dim, float scale, int accumulate,
-                                                             float* dtable) {
-  const int64_t v = blockIdx.x;
-  const int64_t lo = min(max((int64_t)offsets[v], (int64_t)0), n), hi = min((int64_t)offsets[v + 1], n);
-  float* const dst = dtable + v * dim;
-  if (accumulate && lo >= hi) return;
-  for (int64_t c = threadIdx.x; c < dim; c += 256) {
-    float s = 0.0f;
-    for (int64_t p = lo; p < hi; ++p) {
-      const int64_t i = order[p];
-      if (i >= 0 && i < n) s += to_f32(dout[i * dim + c]);
-    }
-    s *= scale;
-    dst[c] = accumulate ? dst[c] + s : s;
+// ---- gradient ----------------------------------------------------------------------------
+//
+// The sorted positions are cut into pieces of equal length whatever the ids are, so that a
+// frequent id costs no more than rare ones.  A lane group sums one piece over its slab of
+// columns, several rows in flight.  Ids that begin and end inside the piece are written at
+// once; the sum of an id that continues from the piece before (the head) or into the next
+// (the tail) goes to the workspace, and a second launch adds tail and heads in order.
+
+struct GradArgs {
+  const int32_t* order;
+  const int32_t* offsets;
+  int64_t n, vocab, dim;
+  float scale;
+  int accumulate;
+  float* dtable;
+  float* partial;      // [pieces][2][dim]: heads and tails
+  int piece;           // positions per piece
+  int64_t pieces;
+  int log_lanes;       // lanes per row
+  int slabs;           // slabs of 2^log_lanes * V columns
+  int64_t sum_blocks;  // blocks that sum; those after them clear the rows of ids that do not occur
+};
+
+__device__ __forceinline__ int64_t grouped_count(const GradArgs& a) {
+  return min(max((int64_t)a.offsets[a.vocab], (int64_t)0), a.n);
+}
+
+// (position, id) at sorted place q; id -1 if there is none.
+template <typename ID>
+__device__ __forceinline__ void sorted_at(const GradArgs& a, const ID* ids, int64_t q, int64_t end, int64_t& pos,
+                                          int64_t& id) {
+  pos = q < end ? (int64_t)a.order[q] : -1;
+  id = -1;
+  if (pos >= 0 && pos < a.n) id = (int64_t)ids[pos];
+  if (id >= a.vocab) id = -1;
+}
+
+template <int V>
+__device__ __forceinline__ void write_row(const GradArgs& a, int64_t id, int64_t c, float (&sum)[V]) {
+  float* const dst = a.dtable + id * a.dim + c;
+#pragma unroll
+  for (int k = 0; k < V; ++k) sum[k] *= a.scale;
+  if (a.accumulate) {
+    float old[V];
+    load_row<V>(dst, a.dim - c, old);
+#pragma unroll
+    for (int k = 0; k < V; ++k) sum[k] += old[k];
   }
+  store_row<V>(dst, a.dim - c, sum);
+}
+
+constexpr int kClearRows = 16;   // rows of the table a clearing wave looks at
+
+template <typename ID, typename GT>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict__ dout, const ID* __restrict__ ids,
+                                                            GradArgs a) {
+  constexpr int V = kPack<GT, GT>, U = 8;   // rows in flight
+  if ((int64_t)blockIdx.x >= a.sum_blocks) {
+    const int lane = threadIdx.x & 63;
+    const int64_t v0 = (((int64_t)blockIdx.x - a.sum_blocks) * 4 + (threadIdx.x >> 6)) * kClearRows;
+    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t v = v0; v < min(v0 + kClearRows, a.vocab); ++v)
+      if (a.offsets[v] >= a.offsets[v + 1])
+        for (int64_t c = lane * 4; c < a.dim; c += 256) store_row<4>(a.dtable + v * a.dim + c, a.dim - c, zero);
+    return;
+  }
+  const int lanes = 1 << a.log_lanes;
+  const int64_t job = (int64_t)blockIdx.x * (256 >> a.log_lanes) + (threadIdx.x >> a.log_lanes);
+  const int64_t p = job / a.slabs;
+  const int64_t c = ((job - p * a.slabs) * lanes + (threadIdx.x & (lanes - 1))) * V;
+  const int64_t count = grouped_count(a);
+  const int64_t q0 = p * a.piece, q1 = min(q0 + a.piece, count);
+  if (p >= a.pieces || q0 >= q1 || c >= a.dim) return;
+  const int64_t left = a.dim - c;
+  int64_t pos[U], id[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) sorted_at(a, ids, q0 + u, q1, pos[u], id[u]);
+  // the head continues the piece before it
+  bool head = id[0] >= 0 && a.offsets[id[0]] < q0;
+  int64_t cur = id[0];
+  float sum[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) sum[k] = 0.0f;
+  auto flush = [&](bool last) {
+    if (cur >= 0) {
+      if (head) store_row<V>(a.partial + 2 * p * a.dim + c, left, sum);
+      else if (last && a.offsets[cur + 1] > q1) store_row<V>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
+      else write_row<V>(a, cur, c, sum);
+    }
+    head = false;
+  };
+  for (int64_t q = q0; q < q1; q += U) {
+    float row[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (id[u] >= 0) load_row<V>(dout + pos[u] * a.dim + c, left, row[u]);
+    int64_t next[U], next_id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) sorted_at(a, ids, q + U + u, q1, next[u], next_id[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (q + u < q1) {
+        if (id[u] != cur) {
+          flush(false);
+          cur = id[u];
+#pragma unroll
+          for (int k = 0; k < V; ++k) sum[k] = 0.0f;
+        }
+        if (id[u] >= 0) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) sum[k] += row[u][k];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      pos[u] = next[u];
+      id[u] = next_id[u];
+    }
+  }
+  flush(true);
+}
+
+// A workgroup for each piece and 256 columns: where an id begins in the piece and goes on
+// into later ones, its four waves add a quarter of the heads each, and their sums meet in
+// LDS.
+template <typename ID>
+__global__ __launch_bounds__(256) void embedding_join_kernel(const ID* __restrict__ ids, GradArgs a) {
+  __shared__ float part[4][64][4];
+  constexpr int U = 8;
+  const int64_t p = blockIdx.x, count = grouped_count(a);
+  const int64_t q0 = p * a.piece, q1 = q0 + a.piece;
+  if (q1 >= count) return;                         // the last piece continues nowhere
+  int64_t pos, id;
+  sorted_at(a, ids, q1 - 1, count, pos, id);
+  if (id < 0 || a.offsets[id] < q0 || a.offsets[id + 1] <= q1) return;
+  const int64_t last = min(((int64_t)a.offsets[id + 1] - 1) / a.piece, a.pieces - 1);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4, left = a.dim - c;
+  const int64_t heads = last - p, from = p + 1 + heads * wave / 4, to = p + 1 + heads * (wave + 1) / 4;
+  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (left > 0) {
+    if (wave == 0) load_row<4>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
+    for (int64_t h = from; h < to; h += U) {
+      float v[U][4];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (h + u < to) load_row<4>(a.partial + 2 * (h + u) * a.dim + c, left, v[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (h + u < to)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum[k] += v[u][k];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) part[wave][lane][k] = sum[k];
+  __syncthreads();
+  if (wave == 0 && left > 0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[k] = (part[0][lane][k] + part[1][lane][k]) + (part[2][lane][k] + part[3][lane][k]);
+    write_row<4>(a, id, c, sum);
+  }
+}
+
+// log2 of the lanes a row of dim elements gets, pack elements each.
+int row_lanes(int64_t dim, int pack, int most) {
+  int l = 0;
+  while (l < most && ((int64_t)pack << l) < dim) ++l;
+  return l;
+}
+
+// Positions per piece: enough pieces to fill the machine, and no fewer than 8 positions.
+int grad_piece(int64_t n, int64_t dim) {
+  const int64_t waves_per_piece = (dim + 255) / 256;
+  int piece = 64;
+  while (piece > 8 && n / piece * waves_per_piece < 4096) piece /= 2;
+  return piece;
 }
 
 }  // namespace
@@ -53,9 +231,22 @@ hipError_t launch_embedding_fwd(const void* ids, int i64, int64_t n, const void*
     using ID = decltype(id);
     using TT = decltype(tt);
     using OT = decltype(ot);
-    hipLaunchKernelGGL((embedding_fwd_kernel<ID, TT, OT>), dim3((unsigned)n), dim3(256), 0, st,
-                       static_cast<const ID*>(ids), static_cast<const TT*>(table), vocab, dim, scale,
-                       static_cast<OT*>(out));
+    const int log_lanes = row_lanes(dim, kPack<TT, OT>, 8);
+    const int64_t groups = 256 >> log_lanes, pass = (int64_t)kPack<TT, OT> << log_lanes;
+    auto go = [&](auto kernel, int64_t rows, int64_t along) {
+      // a grid holds below 2^32 threads
+      const int64_t most = ((int64_t)1 << 23) * groups * rows;
+      for (int64_t at = 0; at < n; at += most) {
+        const int64_t m = n - at < most ? n - at : most;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((m + groups * rows - 1) / (groups * rows)), (unsigned)along),
+                           dim3(256), 0, st, static_cast<const ID*>(ids) + at, m, static_cast<const TT*>(table), vocab,
+                           dim, scale, static_cast<OT*>(out) + at * dim, log_lanes);
+      }
+    };
+    // few rows: a block for every 256 packs of each, so that no load waits for another
+    const int64_t along = (dim + pass - 1) / pass;
+    if (n >= 4096 * groups) go(embedding_fwd_kernel<ID, TT, OT, 4>, 4, 1);
+    else go(embedding_fwd_kernel<ID, TT, OT, 1>, 1, n < 1024 && along < 65536 ? along : 1);
   };
   auto types = [&](auto id) {
     if (t_bf16) o_bf16 ? launch(id, uint16_t{}, uint16_t{}) : launch(id, uint16_t{}, float{});
@@ -65,18 +256,44 @@ hipError_t launch_embedding_fwd(const void* ids, int i64, int64_t n, const void*
   return hipGetLastError();
 }
 
-size_t embedding_grad_workspace_bytes(int64_t, int64_t) { return 0; }
+size_t embedding_grad_workspace_bytes(int64_t n, int64_t dim) {
+  const int64_t piece = grad_piece(n, dim);
+  return (size_t)((n + piece - 1) / piece) * 2 * (size_t)dim * sizeof(float);
+}
 
-hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void*, int, const int32_t* order,
+hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, int i64, const int32_t* order,
                                  const int32_t* offsets, int64_t n, int64_t vocab, int64_t dim, float scale,
-                                 int accumulate, float* dtable, void*, hipStream_t st) {
-  const dim3 grid((unsigned)vocab);
-  if (g_bf16)
-    hipLaunchKernelGGL((embedding_grad_kernel<uint16_t>), grid, dim3(256), 0, st, static_cast<const uint16_t*>(dout),
-                       order, offsets, n, dim, scale, accumulate, dtable);
-  else
-    hipLaunchKernelGGL((embedding_grad_kernel<float>), grid, dim3(256), 0, st, static_cast<const float*>(dout), order,
-                       offsets, n, dim, scale, accumulate, dtable);
+                                 int accumulate, float* dtable, void* ws, hipStream_t st) {
+  GradArgs a;
+  a.order = order;
+  a.offsets = offsets;
+  a.n = n;
+  a.vocab = vocab;
+  a.dim = dim;
+  a.scale = scale;
+  a.accumulate = accumulate;
+  a.dtable = dtable;
+  a.partial = static_cast<float*>(ws);
+  a.piece = grad_piece(n, dim);
+  a.pieces = (n + a.piece - 1) / a.piece;
+  auto launch = [&](auto id, auto gt) {
+    using ID = decltype(id);
+    using GT = decltype(gt);
+    constexpr int V = kPack<GT, GT>;
+    a.log_lanes = row_lanes(dim, V, 6);
+    a.slabs = (int)((dim + ((int64_t)V << a.log_lanes) - 1) / ((int64_t)V << a.log_lanes));
+    const int64_t groups = 256 >> a.log_lanes;
+    a.sum_blocks = (a.pieces * a.slabs + groups - 1) / groups;
+    const int64_t clear = accumulate ? 0 : (vocab + 4 * kClearRows - 1) / (4 * kClearRows);
+    if (a.sum_blocks + clear > 0)
+      hipLaunchKernelGGL((embedding_sum_kernel<ID, GT>), dim3((unsigned)(a.sum_blocks + clear)), dim3(256), 0, st,
+                         static_cast<const GT*>(dout), static_cast<const ID*>(ids), a);
+    if (a.pieces > 1)
+      hipLaunchKernelGGL((embedding_join_kernel<ID>), dim3((unsigned)(a.pieces - 1), (unsigned)((dim + 255) / 256)),
+                         dim3(256), 0, st, static_cast<const ID*>(ids), a);
+  };
+  if (i64) g_bf16 ? launch(int64_t{}, uint16_t{}) : launch(int64_t{}, float{});
+  else g_bf16 ? launch(int32_t{}, uint16_t{}) : launch(int32_t{}, float{});
   return hipGetLastError();
 }
 

@@ -22,6 +22,73 @@ __device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) {
   return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
+// V consecutive elements (16 or 32 bytes) at p, which is aligned to its elements only: rows
+// of any width begin anywhere, and the memory unit takes 16-byte accesses at any address.
+typedef uint32_t u4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+template <int V>
+__device__ __forceinline__ void load_pack(const float* p, float (&v)[V]) {
+  static_assert(V % 4 == 0, "whole 16-byte pieces");
+  typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+  for (int i = 0; i < V; i += 4) {
+    const f4 q = *reinterpret_cast<const f4*>(p + i);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[i + k] = q[k];
+  }
+}
+template <int V>
+__device__ __forceinline__ void load_pack(const uint16_t* p, float (&v)[V]) {
+  static_assert(V == 8, "one 16-byte piece");
+  const u4_any q = *reinterpret_cast<const u4_any*>(p);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = __uint_as_float(q[k] << 16);
+    v[2 * k + 1] = __uint_as_float(q[k] & 0xFFFF0000u);
+  }
+}
+template <int V>
+__device__ __forceinline__ void store_pack(float* p, const float (&v)[V]) {
+  typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+  for (int i = 0; i < V; i += 4) *reinterpret_cast<f4*>(p + i) = f4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+}
+template <int V>
+__device__ __forceinline__ void store_pack(uint16_t* p, const float (&v)[V]) {
+  static_assert(V == 8, "one 16-byte piece");
+  u4_any q;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    q[k] = (uint32_t)from_f32<uint16_t>(v[2 * k]) | (uint32_t)from_f32<uint16_t>(v[2 * k + 1]) << 16;
+  *reinterpret_cast<u4_any*>(p) = q;
+}
+
+// The same for the `left` elements that a row has from p on: a whole pack, or its first
+// elements (the others read as 0 and are not written).
+template <int V, typename T>
+__device__ __forceinline__ void load_row(const T* p, int64_t left, float (&v)[V]) {
+  if (left >= V) {
+    load_pack(p, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = k < left ? to_f32(p[k]) : 0.0f;
+  }
+}
+template <int V, typename T>
+__device__ __forceinline__ void store_row(T* p, int64_t left, const float (&v)[V]) {
+  if (left >= V) {
+    store_pack(p, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k < left) p[k] = from_f32<T>(v[k]);
+  }
+}
+
+// Elements a lane takes at a time: 16 bytes of the narrower type.
+template <typename A, typename B>
+constexpr int kPack = sizeof(A) == 2 || sizeof(B) == 2 ? 8 : 4;
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, kWave);
