@@ -610,7 +610,7 @@ luq_status luq_gemm_dgrad_grouped(const uint8_t* g_codes, const float* alpha, in
 static bool grouped_wgrad_sizes(int64_t T, int64_t Nout, int64_t Kin, int64_t experts) {
   return T >= 32 && (T & 31) == 0 && T <= (1 << 18) && Nout >= 1 && Nout <= kMaxRows && Kin >= 1 && Kin <= kMaxRows &&
          experts >= 1 && experts <= kMaxExperts && Nout * Kin <= kMaxElements / experts &&
-         grid_fits((Nout + 31) / 32 * experts, Kin);
+         grid_fits(((Nout + 31) / 32 + 7) * experts, Kin);
 }
 
 size_t luq_grouped_wgrad_workspace(int64_t T, int64_t Nout, int64_t Kin, int64_t experts) {

@@ -8,7 +8,7 @@
 //
 // The grid covers the most tiles that T rows in so many groups can make; a workgroup finds
 // its group from the offsets and leaves if there is none for it.
-#include "gemm_kernel.hpp"
+#include "grouped_plan.hpp"
 
 namespace luq {
 
@@ -20,7 +20,7 @@ struct RowsArgs {
   const uint8_t* A;
   const uint8_t* B;
   const int32_t* offsets;
-  int experts, tiles_n, vec, scales;
+  int experts, tiles_n, vec, streamed, scales;
   int64_t T, N, K;
   int64_t w_row, w_expert;   // bytes
   const float* alpha;
@@ -39,7 +39,7 @@ struct RowsTile {
   const float* alpha;
   const float* bscale;
   float* C;
-  int vec;
+  int vec, streamed;
   __device__ __forceinline__ void place(int, int, int64_t& m0, int64_t& n0, int64_t& kbeg, int64_t& kend) const {
     m0 = n0 = kbeg = 0;
     kend = K;
@@ -52,6 +52,10 @@ struct RowsTile {
   __device__ __forceinline__ bool sums() const { return false; }
   __device__ __forceinline__ uint32_t* out() const { return reinterpret_cast<uint32_t*>(C); }
   __device__ __forceinline__ int64_t row_c() const { return ldc; }
+  // Outputs that the last-level cache does not hold go around it (8192 x 16384: 588 -> 583
+  // us); smaller ones stay there for the quantizer that reads them next (alone, 2048 x 4096
+  // take 23.4 -> 21.5 us streamed, and with that quantizer 40.2 -> 40.6).
+  __device__ __forceinline__ bool stream() const { return streamed; }
 };
 
 // Rows of group e (e = experts: the rows after the last group), kept inside the batch
@@ -150,6 +154,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_rows_kernel(RowsAr
   t.bscale = a.bscale + (a.scales == 1 ? 0 : g.group);
   t.C = C;
   t.vec = a.vec;
+  t.streamed = a.streamed;
   gemm_tile<AC, 1, BSIGNED, FULLK, PF, S>(t);
 }
 
@@ -167,6 +172,10 @@ struct DepthArgs {
   int32_t* partial;   // [splits][experts][M][N], or null
 };
 
+// A group's k range is read from a multiple of 128 codes on (64 bytes; 128 of the int8 sums),
+// as the stages of an ungrouped product are: the codes before the group are cleared.
+constexpr int kDepthAlign = 128;
+
 struct DepthTile {
   static constexpr bool kMaskK = true;
   const uint8_t* A;
@@ -181,7 +190,7 @@ struct DepthTile {
   bool part;
   __device__ __forceinline__ void place(int, int, int64_t& m0, int64_t& n0, int64_t& kb, int64_t& ke) const {
     m0 = n0 = 0;
-    kb = klo & ~(int64_t)31;
+    kb = klo & ~(int64_t)(kDepthAlign - 1);
     ke = kend;
   }
   __device__ __forceinline__ int64_t row_a(bool i8) const { return i8 ? T : T >> 1; }
@@ -191,23 +200,28 @@ struct DepthTile {
   __device__ __forceinline__ bool sums() const { return part; }
   __device__ __forceinline__ uint32_t* out() const { return C; }
   __device__ __forceinline__ int64_t row_c() const { return ldc; }
+  // The weight gradient is next read by the optimizer, after the rest of the backward pass:
+  // it goes around the caches (16 experts, 1024 -> 4096, 16384 rows: 128 -> 117 us, 512 ->
+  // 1024 over 8192 rows 19.0 -> 16.9).
+  __device__ __forceinline__ bool stream() const { return !part; }
 };
 
 template <int AC, bool BSIGNED, int PF, typename S>
 __global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_depth_kernel(DepthArgs a) {
-  const int per = a.tiles_m * a.tiles_n, total = per * a.experts;
-  const int xcd = blockIdx.x & 7, q = total >> 3, r = total & 7;
-  int L = xcd * q + min(xcd, r) + (int)(blockIdx.x >> 3);
-  const int e = L / per;
-  L -= e * per;
+  // Groups differ in length, so each of the 8 XCDs takes an eighth of every group's tiles (a
+  // run of whole groups for each left XCDs waiting for the one with the longest)
+  const int per = a.tiles_m * a.tiles_n, share = (per + 7) / 8;
+  const int xcd = blockIdx.x & 7, at = (int)(blockIdx.x >> 3), e = at / share;
+  const int L = xcd * share + at - e * share;
+  if (L >= per) return;
   constexpr int G = 8;
   const int first = (L / (G * a.tiles_n)) * G, size = min(a.tiles_m - first, G);
   const int in = L - first * a.tiles_n;
   const int64_t m0 = (int64_t)(first + in % size) * S::BM, n0 = (int64_t)(in / size) * S::BN;
   int lo, hi;
   group_bounds(a.offsets, a.experts, (int)a.T, e, lo, hi);
-  if (a.splits > 1) {   // whole stages a split, counted from the group's first 16-byte piece
-    const int kb = lo & ~31, stages = (hi - kb + S::BK - 1) / S::BK;
+  if (a.splits > 1) {   // whole stages a split
+    const int kb = lo & ~(kDepthAlign - 1), stages = (hi - kb + S::BK - 1) / S::BK;
     const int chunk = (stages + a.splits - 1) / a.splits * S::BK;
     const int from = kb + (int)blockIdx.y * chunk;
     hi = min(hi, from + chunk);
@@ -244,25 +258,44 @@ void launch_rows_tile(RowsArgs a, hipStream_t st) {
   const int64_t groups = a.experts < a.T ? a.experts : a.T;
   const dim3 grid((unsigned)((a.T / S::BM + groups + 1) * a.tiles_n));
   if (a.K % S::BK == 0)
-    hipLaunchKernelGGL((grouped_rows_kernel<AC, BSIGNED, true, 2, S>), grid, dim3(S::THREADS), 0, st, a);
+    hipLaunchKernelGGL((grouped_rows_kernel<AC, BSIGNED, true, prefetch_depth<S, AC, 1, BSIGNED, true>(), S>), grid, dim3(S::THREADS), 0, st, a);
   else
-    hipLaunchKernelGGL((grouped_rows_kernel<AC, BSIGNED, false, 2, S>), grid, dim3(S::THREADS), 0, st, a);
+    hipLaunchKernelGGL((grouped_rows_kernel<AC, BSIGNED, false, prefetch_depth<S, AC, 1, BSIGNED, false>(), S>), grid, dim3(S::THREADS), 0, st, a);
 }
 
 template <int AC, bool BSIGNED>
 hipError_t launch_rows(const RowsArgs& a, hipStream_t st) {
-  launch_rows_tile<Tile128x128, AC, BSIGNED>(a, st);
+  switch (plan_rows(a.T, a.N, a.K, a.experts)) {
+    case kTile256x256: launch_rows_tile<Tile256x256, AC, BSIGNED>(a, st); break;
+    case kTile128x128: launch_rows_tile<Tile128x128, AC, BSIGNED>(a, st); break;
+    case kTile64x128: launch_rows_tile<Tile64x128, AC, BSIGNED>(a, st); break;
+    case kTile32x64: launch_rows_tile<Tile32x64, AC, BSIGNED>(a, st); break;
+    case kTile32x32: launch_rows_tile<Tile32x32, AC, BSIGNED>(a, st); break;
+    default: launch_rows_tile<Tile64x64k1, AC, BSIGNED>(a, st); break;
+  }
   return hipGetLastError();
 }
 
-template <int AC, bool BSIGNED>
-hipError_t launch_depth(DepthArgs a, hipStream_t st) {
-  using S = Tile128x128;
+template <typename S, int AC, bool BSIGNED>
+void launch_depth_tile(DepthArgs a, hipStream_t st) {
   a.tiles_m = (int)((a.M + S::BM - 1) / S::BM);
   a.tiles_n = (int)((a.N + S::BN - 1) / S::BN);
+  const dim3 grid((unsigned)(((int64_t)a.tiles_m * a.tiles_n + 7) / 8 * 8 * a.experts), (unsigned)a.splits);
+  hipLaunchKernelGGL((grouped_depth_kernel<AC, BSIGNED, prefetch_depth<S, AC, 1, BSIGNED, true>(), S>), grid,
+                     dim3(S::THREADS), 0, st, a);
+}
+
+template <int AC, bool BSIGNED>
+hipError_t launch_depth(DepthArgs a, GemmTile tile, hipStream_t st) {
   a.vec = (a.N % 4) == 0 && (((uintptr_t)(a.partial ? (void*)a.partial : (void*)a.C)) & 15) == 0;
-  const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n * a.experts), (unsigned)a.splits);
-  hipLaunchKernelGGL((grouped_depth_kernel<AC, BSIGNED, 2, S>), grid, dim3(S::THREADS), 0, st, a);
+  switch (tile) {
+    case kTile256x256: launch_depth_tile<Tile256x256, AC, BSIGNED>(a, st); break;
+    case kTile128x256: launch_depth_tile<Tile128x256, AC, BSIGNED>(a, st); break;
+    case kTile128x128: launch_depth_tile<Tile128x128, AC, BSIGNED>(a, st); break;
+    case kTile64x128: launch_depth_tile<Tile64x128, AC, BSIGNED>(a, st); break;
+    case kTile32x64: launch_depth_tile<Tile32x64, AC, BSIGNED>(a, st); break;
+    default: launch_depth_tile<Tile64x64k1, AC, BSIGNED>(a, st); break;
+  }
   if (a.splits > 1)
     launch_split_reduce(a.partial, a.splits, a.experts * a.M * a.N,
                         EpilogueScale<AC, 1, BSIGNED>{a.alpha, a.bscale}, a.C, st);
@@ -282,6 +315,7 @@ hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alp
   a.experts = (int)experts;
   a.tiles_n = 0;
   a.vec = (N % 4) == 0 && ((uintptr_t)C & 15) == 0;
+  a.streamed = T * N > kCachedOutputs;
   a.scales = (int)scales;
   a.T = T;
   a.N = N;
@@ -299,7 +333,10 @@ hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alp
   }
 }
 
-size_t grouped_depth_workspace_bytes(int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t grouped_depth_workspace_bytes(int64_t T, int64_t M, int64_t N, int64_t experts) {
+  const int splits = plan_depth(T, M, N, experts).splits;
+  return splits > 1 ? (size_t)splits * experts * M * N * sizeof(int32_t) : 0;
+}
 
 hipError_t launch_grouped_depth(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B,
                                 const float* bscale, int b_signed, const int32_t* offsets, int64_t experts, int64_t T,
@@ -310,7 +347,8 @@ hipError_t launch_grouped_depth(GroupedA kind, const uint8_t* A, const float* al
   a.offsets = offsets;
   a.experts = (int)experts;
   a.tiles_m = a.tiles_n = a.vec = 0;
-  a.splits = 1;
+  const DepthPlan p = plan_depth(T, M, N, experts);
+  a.splits = p.splits;
   a.T = T;
   a.M = M;
   a.N = N;
@@ -319,8 +357,8 @@ hipError_t launch_grouped_depth(GroupedA kind, const uint8_t* A, const float* al
   a.C = C;
   a.partial = a.splits > 1 ? static_cast<int32_t*>(ws) : nullptr;
   if (kind == GroupedA::kSums)
-    return b_signed ? launch_depth<kAcSum2, true>(a, st) : launch_depth<kAcSum2, false>(a, st);
-  return b_signed ? launch_depth<kAcLuq, true>(a, st) : launch_depth<kAcLuq, false>(a, st);
+    return b_signed ? launch_depth<kAcSum2, true>(a, p.tile, st) : launch_depth<kAcSum2, false>(a, p.tile, st);
+  return b_signed ? launch_depth<kAcLuq, true>(a, p.tile, st) : launch_depth<kAcLuq, false>(a, p.tile, st);
 }
 
 }  // namespace luq

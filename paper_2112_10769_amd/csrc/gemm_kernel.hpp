@@ -132,6 +132,7 @@ struct GemmArgs {
     return partial ? reinterpret_cast<uint32_t*>(partial + (int64_t)blockIdx.y * M * N) : reinterpret_cast<uint32_t*>(C);
   }
   __device__ __forceinline__ int64_t row_c() const { return N; }
+  __device__ __forceinline__ bool stream() const { return false; }   // non-temporal stores
 };
 
 // Block -> output tile.  Blocks are dispatched round-robin over the 8 XCDs
@@ -347,8 +348,8 @@ __device__ __forceinline__ void gemm_tile(const Args& a) {
   // clears the codes of stage t outside [klo, kend); a dword holds 8 codes, or 4 int8 sums
   auto mask_a = [&](ARegs& r, int t) {
     if constexpr (Args::kMaskK) {
-      const int64_t k0 = kbeg + (int64_t)t * kBK;
-      if (k0 >= a.klo && k0 + kBK <= kend) return;
+      const int lo = (int)(a.klo - kbeg) - t * kBK, hi = (int)(kend - kbeg) - t * kBK;   // of this stage
+      if (lo <= 0 && hi >= kBK) return;
       constexpr int PER = kI8 ? 4 : 8, BITS = 32 / PER;
 #pragma unroll
       for (int i = 0; i < ACH; ++i)
@@ -356,10 +357,9 @@ __device__ __forceinline__ void gemm_tile(const Args& a) {
         for (int s = 0; s < NA; ++s)
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
-            const int64_t k = k0 + kca[i] + (4 * s + d) * PER;   // s = 1: the second half of the sums
-            const int lo = (int)min(max(a.klo - k, (int64_t)0), (int64_t)PER);
-            const int hi = (int)min(max(kend - k, (int64_t)0), (int64_t)PER);
-            r.a[s][i][d] &= (uint32_t)((1ull << (hi * BITS)) - 1) & ~(uint32_t)((1ull << (lo * BITS)) - 1);
+            const int k = kca[i] + (4 * s + d) * PER;   // s = 1: the second half of the sums
+            const int from = min(max(lo - k, 0), PER), to = min(max(hi - k, 0), PER);
+            r.a[s][i][d] &= (uint32_t)(0xFFFFFFFFull << (from * BITS)) & ~(uint32_t)(0xFFFFFFFFull << (to * BITS));
           }
     }
   };
@@ -560,7 +560,9 @@ __device__ __forceinline__ void gemm_tile(const Args& a) {
               for (int r = 0; r < 4; ++r) v[r] = __float_as_uint(__fmul_rn((float)(int32_t)v[r], sc));
             }
           }
-          *reinterpret_cast<v4u*>(out + row * a.row_c() + col) = v;
+          v4u* const dst = reinterpret_cast<v4u*>(out + row * a.row_c() + col);
+          if (a.stream()) __builtin_nontemporal_store(v, dst);
+          else *dst = v;
         }
       }
     } else if (cbase < a.N && rbase + i * 32 + kg * SR < a.M) {
@@ -776,6 +778,14 @@ constexpr bool tile_built(PlanKind kind, int t) {
   return kind == kPlanOne || (t != kTile64x64 && t != kTile32x32);
 }
 
+// Predicted time of nb workgroups of s stages of 128 k each.
+static float tile_time(const TileCost& c, PlanKind kind, int64_t nb, float s) {
+  const float mean = nb < kCus ? 1.0f : (float)nb * (1.0f / kCus);
+  const float per_cu = mean + kBusiest[kind] * ((float)((nb + kCus - 1) / kCus) - mean);
+  const float alone = s * c.stage1 + c.fixed1, shared = per_cu * (s * c.stage + c.fixed);
+  return alone > shared ? alone : shared;
+}
+
 struct GemmPlan {
   GemmTile tile;
   int64_t tiles_m, tiles_n;
@@ -805,11 +815,7 @@ static GemmPlan search_plan(int64_t M, int64_t N, int64_t K, int64_t max_exact_k
       const int64_t chunk = want == 1 ? stages : (stages - 1) / want + 1;
       const int64_t splits = want == 1 ? 1 : (stages - 1) / chunk + 1;
       const float s = (float)(chunk << c.lk) * (1.0f / 128);
-      const int64_t nb = nt * splits;
-      const float mean = nb < kCus ? 1.0f : (float)nb * (1.0f / kCus);
-      const float per_cu = mean + kBusiest[kind] * ((float)((nb + kCus - 1) / kCus) - mean);
-      const float alone = s * c.stage1 + c.fixed1, shared = per_cu * (s * c.stage + c.fixed);
-      float cost = alone > shared ? alone : shared;
+      float cost = tile_time(c, kind, nt * splits, s);
       if (M * N > kCachedOutputs && c.ln < 7) cost *= kNarrowBeyondCache;
       if (splits > 1) cost += sc.launch + split_out * (float)splits;
       if (best.splits == 0 || cost < best_cost) {
@@ -852,22 +858,28 @@ static size_t split_bytes(const GemmPlan& p, int64_t M, int64_t N) {
   return b;
 }
 
-template <typename S, int AC, int NS, bool BSIGNED>
-static void launch_tile(const GemmArgs& a, dim3 grid, hipStream_t st) {
-  // Prefetch depth, by what measured best; registers are 256 a wave for the two largest
-  // tiles and 128 for the others, and a deeper mode costs more of them.  256x256: the
-  // next stage's fragments too (PF 3), but for the int8 sums with unsigned B and two
-  // planes (PF 2: two planes spill 2 to 5 registers in either mode, and PF 1 took 8192 x
-  // 4096 over K = 16384 from 555 to 582 us).  With a partly filled last stage the k tests
-  // take registers: the int8 sums spilled 4 in PF 1 and none in PF 0 (4096 x 4096 over
-  // 1056: 32.1 -> 31.0 us).  64x64 with four k-groups, partial: PF 1 (up to 5 spilled in
-  // PF 2; 1024 x 512 over 4128, LUQ 11.6 -> 11.0 us, sums 10.1 -> 9.6).  Elsewhere one
-  // k-step ahead.
+// Prefetch depth, by what measured best; registers are 256 a wave for the two largest
+// tiles and 128 for the others, and a deeper mode costs more of them.  256x256: the
+// next stage's fragments too (PF 3), but for the int8 sums with unsigned B and two
+// planes (PF 2: two planes spill 2 to 5 registers in either mode, and PF 1 took 8192 x
+// 4096 over K = 16384 from 555 to 582 us).  With a partly filled last stage the k tests
+// take registers: the int8 sums spilled 4 in PF 1 and none in PF 0 (4096 x 4096 over
+// 1056: 32.1 -> 31.0 us).  64x64 with four k-groups, partial: PF 1 (up to 5 spilled in
+// PF 2; 1024 x 512 over 4128, LUQ 11.6 -> 11.0 us, sums 10.1 -> 9.6).  Elsewhere one
+// k-step ahead.
+template <typename S, int AC, int NS, bool BSIGNED, bool FULLK>
+constexpr int prefetch_depth() {
   constexpr bool kBig = S::BM == 256, kLuq1 = AC == kAcLuq && NS == 1, kLuq2 = AC == kAcLuq && NS == 2;
   constexpr int kSmall = S::BM == 64 && S::BN == 128 ? 1 : 2;
   constexpr bool k64 = S::BM == 64 && S::BN == 64 && S::KG == 4;   // one code per k only
-  constexpr int kPfFull = !kBig ? kSmall : kLuq2 ? 2 : AC == kAcSum2 && !BSIGNED ? 2 : 3;
-  constexpr int kPfPart = !kBig ? (k64 ? 1 : kSmall) : kLuq1 ? 2 : kLuq2 || AC == kAcSum2 ? 0 : 1;
+  if (FULLK) return !kBig ? kSmall : kLuq2 ? 2 : AC == kAcSum2 && !BSIGNED ? 2 : 3;
+  return !kBig ? (k64 ? 1 : kSmall) : kLuq1 ? 2 : kLuq2 || AC == kAcSum2 ? 0 : 1;
+}
+
+template <typename S, int AC, int NS, bool BSIGNED>
+static void launch_tile(const GemmArgs& a, dim3 grid, hipStream_t st) {
+  constexpr int kPfFull = prefetch_depth<S, AC, NS, BSIGNED, true>();
+  constexpr int kPfPart = prefetch_depth<S, AC, NS, BSIGNED, false>();
   if (a.K % S::BK == 0)
     hipLaunchKernelGGL((gemm_tile_kernel<AC, NS, BSIGNED, true, kPfFull, S>), grid, dim3(S::THREADS), 0, st, a);
   else

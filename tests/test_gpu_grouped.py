@@ -94,9 +94,25 @@ def test_rows(L, sizes, tail, kind, b_signed):
         _check_rows(L, sizes, tail, N, K, kind, b_signed, scales=N != 67)
 
 
+# Every tile, on whole stages and on a partly filled last one (test_lm_plan_cpu.py).
+LARGE_ROWS = [([256, 300, 0, 512], 512, 256), ([700, 1, 256], 333, 1184), ([2000, 100], 640, 128), ([64] * 9, 2048, 512),
+              ([2] * 70, 96, 2080), ([3, 1, 0, 2], 100, 2048), ([3, 1, 0, 2], 100, 2080), ([1, 0, 2] * 20, 1024, 512),
+              ([1, 0, 2] * 20, 1024, 544), ([520, 500], 1024, 512), ([520, 500], 1024, 544), ([300, 500, 200], 1500, 128),
+              ([300, 500, 200], 1500, 160), ([2000, 1900, 2100], 2300, 256), ([2000, 1900, 2100], 2300, 160),
+              ([1] * 64, 2048, 128), ([1] * 64, 2048, 96), ([70] * 8, 4096, 256), ([70] * 8, 4096, 288),
+              ([1900, 2100], 4096, 544), ([2300, 1700], 4096, 1024), ([300, 700], 4100, 96), ([500, 500], 4096, 128),
+              ([250, 0, 300, 450], 512, 1056), ([140, 160], 2048, 1024), ([130, 170], 512, 160), ([130, 170], 512, 512)]
+
+
+def rows_shapes():
+    """(experts, T, N, K) of the tests above and below."""
+    small = [(len(sizes), sum(sizes) + tail, N, K) for sizes, tail in GROUPS
+             for N, K in ((1, 32), (67, 96), (256, 1024), (130, 544))]
+    return small + [(len(sizes), sum(sizes) + 3, N, K) for sizes, N, K in LARGE_ROWS]
+
+
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("sizes,N,K", [([256, 300, 0, 512], 512, 256), ([700, 1, 256], 333, 1184),
-                                       ([2000, 100], 640, 128), ([64] * 9, 2048, 512), ([2] * 70, 96, 2080)])
+@pytest.mark.parametrize("sizes,N,K", LARGE_ROWS)
 def test_rows_of_larger_tiles(L, kind, sizes, N, K):
     _check_rows(L, sizes, 3, N, K, kind, True)
 
@@ -219,9 +235,22 @@ def test_depth(L, sizes, kind, b_signed):
         _check_depth(L, sizes, Nout, Kin, kind, b_signed)
 
 
+LARGE_DEPTHS = [([600, 1, 1500], 512, 520), ([4000, 100], 64, 64), ([2048] * 3, 256, 512), ([9000], 40, 96),
+                ([100] * 30, 256, 256), ([30, 2, 500, 1, 200], 2300, 2100), ([777, 900], 2048, 1024), ([1500, 333], 1000, 1030),
+                ([5] * 64, 200, 200), ([130, 0, 77, 260] * 8, 300, 140), ([6000, 5000], 512, 1024),
+                ([900, 1148], 2048, 2048), ([500, 400, 1, 1147], 2048, 2048), ([4096], 100, 90)]
+
+
+def depth_shapes():
+    """(experts, T, Nout, Kin) of the tests above and below."""
+    def rows(sizes):
+        return max(32, -(-sum(sizes) // 32) * 32)
+    small = [(len(s), rows(s), M, N) for s in DEPTHS for M, N in ((1, 1), (67, 33), (128, 256), (300, 130))]
+    return small + [(len(s), rows(s), M, N) for s, M, N in LARGE_DEPTHS]
+
+
 @pytest.mark.parametrize("kind", ["luq", "sums"])
-@pytest.mark.parametrize("sizes,Nout,Kin", [([600, 1, 1500], 512, 520), ([4000, 100], 64, 64), ([2048] * 3, 256, 512),
-                                            ([9000], 40, 96), ([100] * 30, 256, 256)])
+@pytest.mark.parametrize("sizes,Nout,Kin", LARGE_DEPTHS)
 def test_depth_of_larger_tiles(L, kind, sizes, Nout, Kin):
     _check_depth(L, sizes, Nout, Kin, kind, True)
 
