@@ -51,6 +51,10 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const ID* __restrict
 // once; the sum of an id that continues from the piece before (the head) or into the next
 // (the tail) goes to the workspace, and a second launch adds tail and heads in order.
 
+struct Span {
+  int32_t id, last;   // the id that a piece hands on (-1: none), and the piece it ends in
+};
+
 struct GradArgs {
   const int32_t* order;
   const int32_t* offsets;
@@ -58,27 +62,14 @@ struct GradArgs {
   float scale;
   int accumulate;
   float* dtable;
+  Span* spans;         // [pieces]
   float* partial;      // [pieces][2][dim]: heads and tails
-  int piece;           // positions per piece
+  int piece;           // positions per piece, at most kMaxPiece
   int64_t pieces;
   int log_lanes;       // lanes per row
   int slabs;           // slabs of 2^log_lanes * V columns
   int64_t sum_blocks;  // blocks that sum; those after them clear the rows of ids that do not occur
 };
-
-__device__ __forceinline__ int64_t grouped_count(const GradArgs& a) {
-  return min(max((int64_t)a.offsets[a.vocab], (int64_t)0), a.n);
-}
-
-// (position, id) at sorted place q; id -1 if there is none.
-template <typename ID>
-__device__ __forceinline__ void sorted_at(const GradArgs& a, const ID* ids, int64_t q, int64_t end, int64_t& pos,
-                                          int64_t& id) {
-  pos = q < end ? (int64_t)a.order[q] : -1;
-  id = -1;
-  if (pos >= 0 && pos < a.n) id = (int64_t)ids[pos];
-  if (id >= a.vocab) id = -1;
-}
 
 template <int V>
 __device__ __forceinline__ void write_row(const GradArgs& a, int64_t id, int64_t c, float (&sum)[V]) {
@@ -94,12 +85,13 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int64_t id, int64_t
   store_row<V>(dst, a.dim - c, sum);
 }
 
-constexpr int kClearRows = 16;   // rows of the table a clearing wave looks at
+constexpr int kClearRows = 16;                  // rows of the table a clearing wave looks at
+constexpr int kMaxPiece = 64, kMinLanes = 8;    // a block's positions and ids fit LDS
 
 template <typename ID, typename GT>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict__ dout, const ID* __restrict__ ids,
                                                             GradArgs a) {
-  constexpr int V = kPack<GT, GT>, U = 8;   // rows in flight
+  constexpr int V = kPack<GT, GT>, U = 8;   // rows in flight, twice
   if ((int64_t)blockIdx.x >= a.sum_blocks) {
     const int lane = threadIdx.x & 63;
     const int64_t v0 = (((int64_t)blockIdx.x - a.sum_blocks) * 4 + (threadIdx.x >> 6)) * kClearRows;
@@ -109,80 +101,99 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict
         for (int64_t c = lane * 4; c < a.dim; c += 256) store_row<4>(a.dtable + v * a.dim + c, a.dim - c, zero);
     return;
   }
-  const int lanes = 1 << a.log_lanes;
+  // the piece's positions and ids, read ahead of the rows: (position, id), id -1 if there is none
+  __shared__ int2 entry_s[256 / kMinLanes][kMaxPiece];
+  const int lanes = 1 << a.log_lanes, lane = threadIdx.x & (lanes - 1);
+  int2* const entry = entry_s[threadIdx.x >> a.log_lanes];
   const int64_t job = (int64_t)blockIdx.x * (256 >> a.log_lanes) + (threadIdx.x >> a.log_lanes);
   const int64_t p = job / a.slabs;
-  const int64_t c = ((job - p * a.slabs) * lanes + (threadIdx.x & (lanes - 1))) * V;
-  const int64_t count = grouped_count(a);
-  const int64_t q0 = p * a.piece, q1 = min(q0 + a.piece, count);
-  if (p >= a.pieces || q0 >= q1 || c >= a.dim) return;
+  const int64_t c = ((job - p * a.slabs) * lanes + lane) * V;
+  const int64_t count = min(max((int64_t)a.offsets[a.vocab], (int64_t)0), a.n);   // positions that have a group
+  const int64_t q0 = p * a.piece;
+  const int len = (int)max((int64_t)0, min((int64_t)a.piece, count - q0));
+  for (int k = lane; k < a.piece; k += lanes) {
+    int2 e = make_int2(0, -1);
+    if (k < len) {
+      const int64_t pos = a.order[q0 + k];
+      if (pos >= 0 && pos < a.n) {
+        const int64_t id = (int64_t)ids[pos];
+        e = make_int2((int)pos, id < a.vocab ? (int)id : -1);
+      }
+    }
+    entry[k] = e;
+  }
+  __syncthreads();
+  if (p >= a.pieces) return;
+  // the last id goes on behind the piece; the first one came from before it
+  const int last_id = len > 0 ? entry[len - 1].y : -1, first_id = entry[0].y;
+  const int64_t end = last_id >= 0 ? (int64_t)a.offsets[last_id + 1] : 0;
+  const bool onward = end > q0 + len;
+  bool head = first_id >= 0 && a.offsets[first_id] < q0;
+  if (c == 0)   // a piece inside an id's run hands nothing on: it is a head as a whole
+    a.spans[p] = onward && !(head && first_id == last_id)
+                     ? Span{last_id, (int)min((end - 1) / a.piece, a.pieces - 1)}
+                     : Span{-1, 0};
+  if (len == 0 || c >= a.dim) return;
   const int64_t left = a.dim - c;
-  int64_t pos[U], id[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) sorted_at(a, ids, q0 + u, q1, pos[u], id[u]);
-  // the head continues the piece before it
-  bool head = id[0] >= 0 && a.offsets[id[0]] < q0;
-  int64_t cur = id[0];
+  int cur = first_id;
   float sum[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) sum[k] = 0.0f;
   auto flush = [&](bool last) {
     if (cur >= 0) {
       if (head) store_row<V>(a.partial + 2 * p * a.dim + c, left, sum);
-      else if (last && a.offsets[cur + 1] > q1) store_row<V>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
+      else if (last && onward) store_row<V>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
       else write_row<V>(a, cur, c, sum);
     }
     head = false;
   };
-  for (int64_t q = q0; q < q1; q += U) {
-    float row[U][V];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (id[u] >= 0) load_row<V>(dout + pos[u] * a.dim + c, left, row[u]);
-    int64_t next[U], next_id[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) sorted_at(a, ids, q + U + u, q1, next[u], next_id[u]);
+  typedef RowPack<GT, V> Pack;
+  Pack row[2][U];
+  int id[2][U];
+  auto fetch = [&](int buf, int at) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (q + u < q1) {
-        if (id[u] != cur) {
-          flush(false);
-          cur = id[u];
+      const int2 e = entry[min(at + u, len - 1)];
+      id[buf][u] = at + u < len ? e.y : -1;
+      if (id[buf][u] >= 0) row[buf][u].load(dout + (int64_t)e.x * a.dim + c, left);
+    }
+  };
+  auto add = [&](int buf, int at) {
 #pragma unroll
-          for (int k = 0; k < V; ++k) sum[k] = 0.0f;
-        }
-        if (id[u] >= 0) {
+    for (int u = 0; u < U; ++u) {
+      if (at + u < len && id[buf][u] != cur) {
+        flush(false);
+        cur = id[buf][u];
 #pragma unroll
-          for (int k = 0; k < V; ++k) sum[k] += row[u][k];
-        }
+        for (int k = 0; k < V; ++k) sum[k] = 0.0f;
+      }
+      if (id[buf][u] >= 0) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) sum[k] += row[buf][u].get(k);
       }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      pos[u] = next[u];
-      id[u] = next_id[u];
-    }
+  };
+  fetch(0, 0);
+  for (int at = 0; at < len; at += 2 * U) {
+    fetch(1, at + U);
+    add(0, at);
+    fetch(0, at + 2 * U);
+    add(1, at + U);
   }
   flush(true);
 }
 
-// A workgroup for each piece and 256 columns: where an id begins in the piece and goes on
-// into later ones, its four waves add a quarter of the heads each, and their sums meet in
-// LDS.
-template <typename ID>
-__global__ __launch_bounds__(256) void embedding_join_kernel(const ID* __restrict__ ids, GradArgs a) {
+// A workgroup for each piece and 256 columns: where the piece hands an id on, its four
+// waves add a quarter of the later pieces' heads each, and their sums meet in LDS.
+__global__ __launch_bounds__(256) void embedding_join_kernel(GradArgs a) {
   __shared__ float part[4][64][4];
   constexpr int U = 8;
-  const int64_t p = blockIdx.x, count = grouped_count(a);
-  const int64_t q0 = p * a.piece, q1 = q0 + a.piece;
-  if (q1 >= count) return;                         // the last piece continues nowhere
-  int64_t pos, id;
-  sorted_at(a, ids, q1 - 1, count, pos, id);
-  if (id < 0 || a.offsets[id] < q0 || a.offsets[id + 1] <= q1) return;
-  const int64_t last = min(((int64_t)a.offsets[id + 1] - 1) / a.piece, a.pieces - 1);
+  const int64_t p = blockIdx.x;
+  const Span span = a.spans[p];
+  if (span.id < 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4, left = a.dim - c;
-  const int64_t heads = last - p, from = p + 1 + heads * wave / 4, to = p + 1 + heads * (wave + 1) / 4;
+  const int64_t heads = span.last - p, from = p + 1 + heads * wave / 4, to = p + 1 + heads * (wave + 1) / 4;
   float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   if (left > 0) {
     if (wave == 0) load_row<4>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
@@ -204,13 +215,13 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const ID* __restric
   if (wave == 0 && left > 0) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum[k] = (part[0][lane][k] + part[1][lane][k]) + (part[2][lane][k] + part[3][lane][k]);
-    write_row<4>(a, id, c, sum);
+    write_row<4>(a, span.id, c, sum);
   }
 }
 
 // log2 of the lanes a row of dim elements gets, pack elements each.
-int row_lanes(int64_t dim, int pack, int most) {
-  int l = 0;
+int row_lanes(int64_t dim, int pack, int least, int most) {
+  int l = least;
   while (l < most && ((int64_t)pack << l) < dim) ++l;
   return l;
 }
@@ -218,7 +229,7 @@ int row_lanes(int64_t dim, int pack, int most) {
 // Positions per piece: enough pieces to fill the machine, and no fewer than 8 positions.
 int grad_piece(int64_t n, int64_t dim) {
   const int64_t waves_per_piece = (dim + 255) / 256;
-  int piece = 64;
+  int piece = kMaxPiece;
   while (piece > 8 && n / piece * waves_per_piece < 4096) piece /= 2;
   return piece;
 }
@@ -231,7 +242,7 @@ hipError_t launch_embedding_fwd(const void* ids, int i64, int64_t n, const void*
     using ID = decltype(id);
     using TT = decltype(tt);
     using OT = decltype(ot);
-    const int log_lanes = row_lanes(dim, kPack<TT, OT>, 8);
+    const int log_lanes = row_lanes(dim, kPack<TT, OT>, 0, 8);
     const int64_t groups = 256 >> log_lanes, pass = (int64_t)kPack<TT, OT> << log_lanes;
     auto go = [&](auto kernel, int64_t rows, int64_t along) {
       // a grid holds below 2^32 threads
@@ -257,8 +268,8 @@ hipError_t launch_embedding_fwd(const void* ids, int i64, int64_t n, const void*
 }
 
 size_t embedding_grad_workspace_bytes(int64_t n, int64_t dim) {
-  const int64_t piece = grad_piece(n, dim);
-  return (size_t)((n + piece - 1) / piece) * 2 * (size_t)dim * sizeof(float);
+  const int64_t piece = grad_piece(n, dim), pieces = (n + piece - 1) / piece;
+  return (size_t)pieces * (sizeof(Span) + 2 * (size_t)dim * sizeof(float));
 }
 
 hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, int i64, const int32_t* order,
@@ -273,14 +284,15 @@ hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, 
   a.scale = scale;
   a.accumulate = accumulate;
   a.dtable = dtable;
-  a.partial = static_cast<float*>(ws);
   a.piece = grad_piece(n, dim);
   a.pieces = (n + a.piece - 1) / a.piece;
+  a.spans = static_cast<Span*>(ws);
+  a.partial = reinterpret_cast<float*>(a.spans + a.pieces);
   auto launch = [&](auto id, auto gt) {
     using ID = decltype(id);
     using GT = decltype(gt);
     constexpr int V = kPack<GT, GT>;
-    a.log_lanes = row_lanes(dim, V, 6);
+    a.log_lanes = row_lanes(dim, V, 3, 6);
     a.slabs = (int)((dim + ((int64_t)V << a.log_lanes) - 1) / ((int64_t)V << a.log_lanes));
     const int64_t groups = 256 >> a.log_lanes;
     a.sum_blocks = (a.pieces * a.slabs + groups - 1) / groups;
@@ -289,8 +301,8 @@ hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, 
       hipLaunchKernelGGL((embedding_sum_kernel<ID, GT>), dim3((unsigned)(a.sum_blocks + clear)), dim3(256), 0, st,
                          static_cast<const GT*>(dout), static_cast<const ID*>(ids), a);
     if (a.pieces > 1)
-      hipLaunchKernelGGL((embedding_join_kernel<ID>), dim3((unsigned)(a.pieces - 1), (unsigned)((dim + 255) / 256)),
-                         dim3(256), 0, st, static_cast<const ID*>(ids), a);
+      hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)(a.pieces - 1), (unsigned)((dim + 255) / 256)), dim3(256),
+                         0, st, a);
   };
   if (i64) g_bf16 ? launch(int64_t{}, uint16_t{}) : launch(int64_t{}, float{});
   else g_bf16 ? launch(int32_t{}, uint16_t{}) : launch(int32_t{}, float{});

@@ -49,34 +49,18 @@ constexpr int kRowsAtOnce = TPR > kWave ? 1 : 256 / TPR;
 template <int TPR>
 constexpr int kThreads = TPR > kWave ? TPR : 256;
 
-// A row's packs as they lie in memory, CH per thread: pack i of thread t holds the columns
-// from (i * TPR + t) * V on.
+// A thread's CH packs of a row: pack i of thread t holds the columns from (i * TPR + t) * V on.
 template <typename T, int V, int TPR, int CH>
 struct RowRaw {
-  typedef uint32_t raw __attribute__((ext_vector_type(4)));
-  static constexpr int Q = V * sizeof(T) / 16;
-  raw q[CH][Q];
-
+  RowPack<T, V> pack[CH];
   __device__ __forceinline__ void load(const T* row, int64_t cols, int t) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int64_t c = (int64_t)(i * TPR + t) * V;
-      if (c + V <= cols) {
-#pragma unroll
-        for (int k = 0; k < Q; ++k) q[i][k] = reinterpret_cast<const u4_any*>(row + c)[k];
-      } else {
-        T e[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) e[k] = c + k < cols ? row[c + k] : T(0);
-        __builtin_memcpy(q[i], e, sizeof(e));
-      }
+      pack[i].load(row + c, cols - c);
     }
   }
-  __device__ __forceinline__ float get(int i, int k) const {
-    if constexpr (sizeof(T) == 4) return __uint_as_float(q[i][k / 4][k % 4]);
-    const uint32_t w = q[i][0][k / 2];
-    return __uint_as_float(k & 1 ? w & 0xFFFF0000u : w << 16);
-  }
+  __device__ __forceinline__ float get(int i, int k) const { return pack[i].get(k); }
 };
 
 template <typename T, int TPR, int CH>

@@ -85,6 +85,32 @@ __device__ __forceinline__ void store_row(T* p, int64_t left, const float (&v)[V
   }
 }
 
+// A pack as it lies in memory, converted when it is used: loads of later rows are in flight
+// in as few registers as they have bytes.
+template <typename T, int V>
+struct RowPack {
+  static constexpr int Q = V * sizeof(T) / 16;
+  typedef uint32_t raw __attribute__((ext_vector_type(4)));
+  raw q[Q];
+  // the `left` elements that the row has from p on; none where left <= 0
+  __device__ __forceinline__ void load(const T* p, int64_t left) {
+    if (left >= V) {
+#pragma unroll
+      for (int k = 0; k < Q; ++k) q[k] = reinterpret_cast<const u4_any*>(p)[k];
+    } else {
+      T e[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) e[k] = k < left ? p[k] : T(0);
+      __builtin_memcpy(q, e, sizeof(e));
+    }
+  }
+  __device__ __forceinline__ float get(int k) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(q[k / 4][k % 4]);
+    const uint32_t w = q[0][k / 2];
+    return __uint_as_float(k & 1 ? w & 0xFFFF0000u : w << 16);
+  }
+};
+
 // Elements a lane takes at a time: 16 bytes of the narrower type.
 template <typename A, typename B>
 constexpr int kPack = sizeof(A) == 2 || sizeof(B) == 2 ? 8 : 4;

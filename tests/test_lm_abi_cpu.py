@@ -35,7 +35,7 @@ def _call(fn, defaults, kw):
     return getattr(LIB, fn)(*a.values())
 
 
-GROUP = dict(ids=P, it=0, n=100, groups=10, order=P2, offsets=P3, ws=P, ws_bytes=WS, stream=NUL)
+GROUP = dict(ids=P, it=0, n=100000, groups=10, order=P2, offsets=P3, ws=P, ws_bytes=WS, stream=NUL)
 
 
 @pytest.mark.parametrize("kw,status", [
