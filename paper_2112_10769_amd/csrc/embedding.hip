@@ -5,6 +5,8 @@
 // Both are bound by memory: the lookup reads and writes a row per id, the gradient reads a
 // row per id and writes the table once.  The gradient takes the positions grouped by id
 // (group_ids.hip), so that every row of the table has one writer and its sum one order.
+#include <type_traits>
+
 #include "luq_launch.hpp"
 #include "row_ops.hpp"
 
@@ -46,8 +48,10 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const ID* __restrict
 // ---- gradient ----------------------------------------------------------------------------
 //
 // The sorted positions are cut into pieces of equal length whatever the ids are, so that a
-// frequent id costs no more than rare ones.  A lane group sums one piece over its slab of
-// columns, several rows in flight.  Ids that begin and end inside the piece are written at
+// frequent id costs no more than rare ones.  A wave sums one piece over its slab of columns:
+// the lanes hold the piece's positions and ids, which are wave-uniform in the loop, and two
+// batches of rows are in flight (a narrow row takes fewer elements a lane, not fewer lanes:
+// several pieces a wave, whose ids end at different rows, took 60000 rows of 64 35 us).  Ids that begin and end inside the piece are written at
 // once; the sum of an id that continues from the piece before (the head) or into the next
 // (the tail) goes to the workspace, and a second launch adds tail and heads in order.
 
@@ -64,10 +68,9 @@ struct GradArgs {
   float* dtable;
   Span* spans;         // [pieces]
   float* partial;      // [pieces][2][dim]: heads and tails
-  int piece;           // positions per piece, at most kMaxPiece
+  int piece;           // positions per piece, at most a wave's lanes
   int64_t pieces;
-  int log_lanes;       // lanes per row
-  int slabs;           // slabs of 2^log_lanes * V columns
+  int slabs;           // slabs of 64 V columns
   int64_t sum_blocks;  // blocks that sum; those after them clear the rows of ids that do not occur
 };
 
@@ -85,47 +88,44 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int64_t id, int64_t
   store_row<V>(dst, a.dim - c, sum);
 }
 
-constexpr int kClearRows = 16;                  // rows of the table a clearing wave looks at
-constexpr int kMaxPiece = 64, kMinLanes = 8;    // a block's positions and ids fit LDS
+constexpr int kClearRows = 16;   // rows of the table a clearing wave looks at
 
-template <typename ID, typename GT>
+template <typename ID, typename GT, int V>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict__ dout, const ID* __restrict__ ids,
                                                             GradArgs a) {
-  constexpr int V = kPack<GT, GT>, U = 8;   // rows in flight, twice
+  constexpr int U = V * sizeof(GT) >= 16 ? 8 : 16;   // rows of a batch
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int64_t)blockIdx.x >= a.sum_blocks) {
-    const int lane = threadIdx.x & 63;
-    const int64_t v0 = (((int64_t)blockIdx.x - a.sum_blocks) * 4 + (threadIdx.x >> 6)) * kClearRows;
+    const int64_t v0 = (((int64_t)blockIdx.x - a.sum_blocks) * 4 + wave) * kClearRows;
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t v = v0; v < min(v0 + kClearRows, a.vocab); ++v)
-      if (a.offsets[v] >= a.offsets[v + 1])
-        for (int64_t c = lane * 4; c < a.dim; c += 256) store_row<4>(a.dtable + v * a.dim + c, a.dim - c, zero);
+    // the rows' offsets at once: nothing but stores is left in the loop
+    const int32_t from = v0 + lane <= a.vocab && lane <= kClearRows ? a.offsets[v0 + lane] : 0;
+    const int32_t to = __shfl_down(from, 1, 64);
+    uint64_t empty = __ballot(lane < kClearRows && v0 + lane < a.vocab && from >= to);
+    for (; empty; empty &= empty - 1) {
+      float* const dst = a.dtable + (v0 + __builtin_ctzll(empty)) * a.dim;
+      for (int64_t c = lane * 4; c < a.dim; c += 256) store_row<4>(dst + c, a.dim - c, zero);
+    }
     return;
   }
-  // the piece's positions and ids, read ahead of the rows: (position, id), id -1 if there is none
-  __shared__ int2 entry_s[256 / kMinLanes][kMaxPiece];
-  const int lanes = 1 << a.log_lanes, lane = threadIdx.x & (lanes - 1);
-  int2* const entry = entry_s[threadIdx.x >> a.log_lanes];
-  const int64_t job = (int64_t)blockIdx.x * (256 >> a.log_lanes) + (threadIdx.x >> a.log_lanes);
-  const int64_t p = job / a.slabs;
-  const int64_t c = ((job - p * a.slabs) * lanes + lane) * V;
+  const int64_t job = (int64_t)blockIdx.x * 4 + wave, p = job / a.slabs;
+  if (p >= a.pieces) return;
+  const int64_t c = ((job - p * a.slabs) * 64 + lane) * V, left = a.dim - c;
   const int64_t count = min(max((int64_t)a.offsets[a.vocab], (int64_t)0), a.n);   // positions that have a group
   const int64_t q0 = p * a.piece;
   const int len = (int)max((int64_t)0, min((int64_t)a.piece, count - q0));
-  for (int k = lane; k < a.piece; k += lanes) {
-    int2 e = make_int2(0, -1);
-    if (k < len) {
-      const int64_t pos = a.order[q0 + k];
-      if (pos >= 0 && pos < a.n) {
-        const int64_t id = (int64_t)ids[pos];
-        e = make_int2((int)pos, id < a.vocab ? (int)id : -1);
-      }
+  // lane k: position and id of the piece's k-th row, id -1 if there is none
+  int pos = 0, ident = -1;
+  if (lane < len) {
+    pos = a.order[q0 + lane];
+    if (pos >= 0 && pos < a.n) {
+      const int64_t id = (int64_t)ids[pos];
+      if (id >= 0 && id < a.vocab) ident = (int)id;
     }
-    entry[k] = e;
   }
-  __syncthreads();
-  if (p >= a.pieces) return;
   // the last id goes on behind the piece; the first one came from before it
-  const int last_id = len > 0 ? entry[len - 1].y : -1, first_id = entry[0].y;
+  const int first_id = __builtin_amdgcn_readlane(ident, 0);
+  const int last_id = len > 0 ? __builtin_amdgcn_readlane(ident, len - 1) : -1;
   const int64_t end = last_id >= 0 ? (int64_t)a.offsets[last_id + 1] : 0;
   const bool onward = end > q0 + len;
   bool head = first_id >= 0 && a.offsets[first_id] < q0;
@@ -133,46 +133,45 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict
     a.spans[p] = onward && !(head && first_id == last_id)
                      ? Span{last_id, (int)min((end - 1) / a.piece, a.pieces - 1)}
                      : Span{-1, 0};
-  if (len == 0 || c >= a.dim) return;
-  const int64_t left = a.dim - c;
   int cur = first_id;
   float sum[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) sum[k] = 0.0f;
   auto flush = [&](bool last) {
-    if (cur >= 0) {
+    if (cur >= 0 && left > 0) {
       if (head) store_row<V>(a.partial + 2 * p * a.dim + c, left, sum);
       else if (last && onward) store_row<V>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
       else write_row<V>(a, cur, c, sum);
     }
     head = false;
   };
-  typedef RowPack<GT, V> Pack;
-  Pack row[2][U];
-  int id[2][U];
+  RowPack<GT, V> row[2][U];
   auto fetch = [&](int buf, int at) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int2 e = entry[min(at + u, len - 1)];
-      id[buf][u] = at + u < len ? e.y : -1;
-      if (id[buf][u] >= 0) row[buf][u].load(dout + (int64_t)e.x * a.dim + c, left);
-    }
+    for (int u = 0; u < U; ++u)
+      if (at + u < len) {
+        const int64_t from = __builtin_amdgcn_readlane(pos, at + u);
+        if (__builtin_amdgcn_readlane(ident, at + u) >= 0) row[buf][u].load(dout + from * a.dim + c, left);
+      }
   };
   auto add = [&](int buf, int at) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (at + u < len && id[buf][u] != cur) {
-        flush(false);
-        cur = id[buf][u];
+    for (int u = 0; u < U; ++u)
+      if (at + u < len) {
+        const int id = __builtin_amdgcn_readlane(ident, at + u);
+        if (id != cur) {
+          flush(false);
+          cur = id;
 #pragma unroll
-        for (int k = 0; k < V; ++k) sum[k] = 0.0f;
-      }
-      if (id[buf][u] >= 0) {
+          for (int k = 0; k < V; ++k) sum[k] = 0.0f;
+        }
+        if (id >= 0) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) sum[k] += row[buf][u].get(k);
+          for (int k = 0; k < V; ++k) sum[k] += row[buf][u].get(k);
+        }
       }
-    }
   };
+  if (len == 0) return;
   fetch(0, 0);
   for (int at = 0; at < len; at += 2 * U) {
     fetch(1, at + U);
@@ -183,17 +182,17 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict
   flush(true);
 }
 
-// A workgroup for each piece and 256 columns: where the piece hands an id on, its four
-// waves add a quarter of the later pieces' heads each, and their sums meet in LDS.
-__global__ __launch_bounds__(256) void embedding_join_kernel(GradArgs a) {
-  __shared__ float part[4][64][4];
-  constexpr int U = 8;
+// A workgroup for each piece and 256 columns: where the piece hands an id on, its eight
+// waves add an eighth of the later pieces' heads each, and their sums meet in LDS.
+__global__ __launch_bounds__(512) void embedding_join_kernel(GradArgs a) {
+  constexpr int W = 8, U = 8;
+  __shared__ float part[W][64][4];
   const int64_t p = blockIdx.x;
   const Span span = a.spans[p];
   if (span.id < 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4, left = a.dim - c;
-  const int64_t heads = span.last - p, from = p + 1 + heads * wave / 4, to = p + 1 + heads * (wave + 1) / 4;
+  const int64_t heads = span.last - p, from = p + 1 + heads * wave / W, to = p + 1 + heads * (wave + 1) / W;
   float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   if (left > 0) {
     if (wave == 0) load_row<4>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
@@ -214,23 +213,28 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(GradArgs a) {
   __syncthreads();
   if (wave == 0 && left > 0) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum[k] = (part[0][lane][k] + part[1][lane][k]) + (part[2][lane][k] + part[3][lane][k]);
+    for (int k = 0; k < 4; ++k) {
+      sum[k] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) sum[k] += part[w][lane][k];
+    }
     write_row<4>(a, span.id, c, sum);
   }
 }
 
 // log2 of the lanes a row of dim elements gets, pack elements each.
-int row_lanes(int64_t dim, int pack, int least, int most) {
-  int l = least;
+int row_lanes(int64_t dim, int pack, int most) {
+  int l = 0;
   while (l < most && ((int64_t)pack << l) < dim) ++l;
   return l;
 }
 
-// Positions per piece: enough pieces to fill the machine, and no fewer than 8 positions.
+// Positions per piece: enough pieces to fill the machine, and no fewer than 16 positions (65536
+// rows of 1024 bf16: 64 positions 100 us, 32 89, 16 94; 16384 rows: 16 positions 38, 8 44).
 int grad_piece(int64_t n, int64_t dim) {
   const int64_t waves_per_piece = (dim + 255) / 256;
-  int piece = kMaxPiece;
-  while (piece > 8 && n / piece * waves_per_piece < 4096) piece /= 2;
+  int piece = 64;
+  while (piece > 16 && n / piece * waves_per_piece < 8192) piece /= 2;
   return piece;
 }
 
@@ -242,7 +246,7 @@ hipError_t launch_embedding_fwd(const void* ids, int i64, int64_t n, const void*
     using ID = decltype(id);
     using TT = decltype(tt);
     using OT = decltype(ot);
-    const int log_lanes = row_lanes(dim, kPack<TT, OT>, 0, 8);
+    const int log_lanes = row_lanes(dim, kPack<TT, OT>, 8);
     const int64_t groups = 256 >> log_lanes, pass = (int64_t)kPack<TT, OT> << log_lanes;
     auto go = [&](auto kernel, int64_t rows, int64_t along) {
       // a grid holds below 2^32 threads
@@ -291,17 +295,22 @@ hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, 
   auto launch = [&](auto id, auto gt) {
     using ID = decltype(id);
     using GT = decltype(gt);
-    constexpr int V = kPack<GT, GT>;
-    a.log_lanes = row_lanes(dim, V, 3, 6);
-    a.slabs = (int)((dim + ((int64_t)V << a.log_lanes) - 1) / ((int64_t)V << a.log_lanes));
-    const int64_t groups = 256 >> a.log_lanes;
-    a.sum_blocks = (a.pieces * a.slabs + groups - 1) / groups;
-    const int64_t clear = accumulate ? 0 : (vocab + 4 * kClearRows - 1) / (4 * kClearRows);
-    if (a.sum_blocks + clear > 0)
-      hipLaunchKernelGGL((embedding_sum_kernel<ID, GT>), dim3((unsigned)(a.sum_blocks + clear)), dim3(256), 0, st,
-                         static_cast<const GT*>(dout), static_cast<const ID*>(ids), a);
+    auto sum = [&](auto pack) {
+      constexpr int V = decltype(pack)::value;
+      a.slabs = (int)((dim + 64 * V - 1) / (64 * V));
+      a.sum_blocks = (a.pieces * a.slabs + 3) / 4;
+      const int64_t clear = accumulate ? 0 : (vocab + 4 * kClearRows - 1) / (4 * kClearRows);
+      if (a.sum_blocks + clear > 0)
+        hipLaunchKernelGGL((embedding_sum_kernel<ID, GT, V>), dim3((unsigned)(a.sum_blocks + clear)), dim3(256), 0, st,
+                           static_cast<const GT*>(dout), static_cast<const ID*>(ids), a);
+    };
+    constexpr int kMost = kPack<GT, GT>;
+    if (dim <= 64) sum(std::integral_constant<int, 1>{});
+    else if (dim <= 128) sum(std::integral_constant<int, 2>{});
+    else if (dim <= 256 || kMost == 4) sum(std::integral_constant<int, 4>{});
+    else sum(std::integral_constant<int, kMost>{});
     if (a.pieces > 1)
-      hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)(a.pieces - 1), (unsigned)((dim + 255) / 256)), dim3(256),
+      hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)(a.pieces - 1), (unsigned)((dim + 255) / 256)), dim3(512),
                          0, st, a);
   };
   if (i64) g_bf16 ? launch(int64_t{}, uint16_t{}) : launch(int64_t{}, float{});

@@ -17,8 +17,8 @@ namespace luq {
 namespace {
 
 constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
-constexpr int kSortThreads = 512, kSortWaves = kSortThreads / kWave;
-constexpr int kItems = 2, kPiece = kSortThreads * kItems;   // keys a block ranks at a time
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
+constexpr int kItems = 1, kPiece = kSortThreads * kItems;   // keys a block ranks at a time
 constexpr int kMaxSortBlocks = 128;
 
 // Where a pass reads its keys from.
@@ -76,20 +76,30 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortPass a, 
   __shared__ uint32_t base[kBins];
   __shared__ uint32_t count[kSortWaves][kBins];
   __shared__ uint32_t scratch[kSortWaves];
+  __shared__ uint32_t totals[kSortThreads], befores[kSortThreads];
   const int bins = 1 << a.bits, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   // where this block's keys of digit d begin: all smaller digits, then the blocks before
+  // (the block's threads share the blocks of a digit, 16 histograms in flight each)
+  const int d0 = threadIdx.x, shares = kSortThreads >> a.bits, share = threadIdx.x >> a.bits;
   uint32_t total = 0, before = 0;
-  const int d0 = threadIdx.x;
+  for (int b0 = share * 16; b0 < a.blocks; b0 += shares * 16) {
+    uint32_t c[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) c[k] = b0 + k < a.blocks ? counts[(b0 + k) * bins + (d0 & (bins - 1))] : 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      if (b0 + k < (int)blockIdx.x) before += c[k];
+      total += c[k];
+    }
+  }
+  totals[threadIdx.x] = total;
+  befores[threadIdx.x] = before;
+  __syncthreads();
+  total = before = 0;
   if (d0 < bins)
-    for (int b0 = 0; b0 < a.blocks; b0 += 16) {
-      uint32_t c[16];
-#pragma unroll
-      for (int k = 0; k < 16; ++k) c[k] = b0 + k < a.blocks ? counts[(b0 + k) * bins + d0] : 0;
-#pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        if (b0 + k < (int)blockIdx.x) before += c[k];
-        total += c[k];
-      }
+    for (int k = 0; k < shares; ++k) {
+      total += totals[(k << a.bits) + d0];
+      before += befores[(k << a.bits) + d0];
     }
   const uint32_t smaller = block_prefix(total, scratch);
   if (d0 < bins) base[d0] = smaller + before;

@@ -22,13 +22,19 @@ __device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) {
   return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// V consecutive elements (16 or 32 bytes) at p, which is aligned to its elements only: rows
-// of any width begin anywhere, and the memory unit takes 16-byte accesses at any address.
+// V consecutive elements at p, which is aligned to its elements only: rows of any width
+// begin anywhere, and the memory unit takes 16-byte accesses at any address.
 typedef uint32_t u4_any __attribute__((ext_vector_type(4), aligned(2)));
 
 template <int V>
 __device__ __forceinline__ void load_pack(const float* p, float (&v)[V]) {
-  static_assert(V % 4 == 0, "whole 16-byte pieces");
+  if constexpr (V < 4) {
+    typedef float fv __attribute__((ext_vector_type(V), aligned(4)));
+    const fv q = *reinterpret_cast<const fv*>(p);
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = q[k];
+    return;
+  }
   typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
   for (int i = 0; i < V; i += 4) {
@@ -49,6 +55,14 @@ __device__ __forceinline__ void load_pack(const uint16_t* p, float (&v)[V]) {
 }
 template <int V>
 __device__ __forceinline__ void store_pack(float* p, const float (&v)[V]) {
+  if constexpr (V < 4) {
+    typedef float fv __attribute__((ext_vector_type(V), aligned(4)));
+    fv q;
+#pragma unroll
+    for (int k = 0; k < V; ++k) q[k] = v[k];
+    *reinterpret_cast<fv*>(p) = q;
+    return;
+  }
   typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
   for (int i = 0; i < V; i += 4) *reinterpret_cast<f4*>(p + i) = f4{v[i], v[i + 1], v[i + 2], v[i + 3]};
@@ -89,25 +103,43 @@ __device__ __forceinline__ void store_row(T* p, int64_t left, const float (&v)[V
 // in as few registers as they have bytes.
 template <typename T, int V>
 struct RowPack {
-  static constexpr int Q = V * sizeof(T) / 16;
-  typedef uint32_t raw __attribute__((ext_vector_type(4)));
-  raw q[Q];
+  static constexpr int kBytes = V * sizeof(T), W = kBytes < 4 ? 1 : kBytes / 4;
+  uint32_t w[W];
   // the `left` elements that the row has from p on; none where left <= 0
   __device__ __forceinline__ void load(const T* p, int64_t left) {
     if (left >= V) {
+      if constexpr (kBytes >= 16) {
 #pragma unroll
-      for (int k = 0; k < Q; ++k) q[k] = reinterpret_cast<const u4_any*>(p)[k];
+        for (int k = 0; k < W; k += 4) {
+          const u4_any q = reinterpret_cast<const u4_any*>(p)[k / 4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[k + i] = q[i];
+        }
+      } else if constexpr (kBytes == 8) {
+        typedef uint32_t u2_any __attribute__((ext_vector_type(2), aligned(2)));
+        const u2_any q = *reinterpret_cast<const u2_any*>(p);
+        w[0] = q[0];
+        w[1] = q[1];
+      } else if constexpr (kBytes == 4) {
+        typedef uint32_t u1_any __attribute__((aligned(2)));
+        w[0] = *reinterpret_cast<const u1_any*>(p);
+      } else {
+        w[0] = *p;
+      }
     } else {
-      T e[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k) e[k] = k < left ? p[k] : T(0);
-      __builtin_memcpy(q, e, sizeof(e));
+      for (int k = 0; k < W; ++k) w[k] = 0;
+#pragma unroll
+      for (int k = 0; k < V - 1; ++k)
+        if (k < left) {
+          if constexpr (sizeof(T) == 4) w[k] = __float_as_uint(p[k]);
+          else w[k / 2] |= (uint32_t)p[k] << (16 * (k & 1));
+        }
     }
   }
   __device__ __forceinline__ float get(int k) const {
-    if constexpr (sizeof(T) == 4) return __uint_as_float(q[k / 4][k % 4]);
-    const uint32_t w = q[0][k / 2];
-    return __uint_as_float(k & 1 ? w & 0xFFFF0000u : w << 16);
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
+    return __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
   }
 };
 
