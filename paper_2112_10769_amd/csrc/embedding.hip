@@ -30,17 +30,28 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const ID* __restrict
   for (int r = 0; r < kRows; ++r) id[r] = first + r < n ? (int64_t)ids[first + r] : -1;
   const int64_t step = (int64_t)gridDim.y * lanes * V;
   for (int64_t c = ((int64_t)blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * V; c < dim; c += step) {
-    float v[kRows][V];
+    const PackAt<V> at((int)c, (int)dim);
+    RowPack<TT, V> raw[kRows];
+    if (dim >= V) {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-      if (id[r] >= 0 && id[r] < vocab) load_row<V>(table + id[r] * dim + c, dim - c, v[r]);
+      for (int r = 0; r < kRows; ++r)
+        if (id[r] >= 0 && id[r] < vocab) raw[r].load(table + id[r] * dim + at.begin);
+    }
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
+      if (first + r >= n) continue;
       const bool row = id[r] >= 0 && id[r] < vocab;
       const float none = id[r] >= 0 ? __builtin_nanf("") : 0.0f;   // off the table, or padding
+      OT* const dst = out + (first + r) * dim;
+      if (dim >= V) {
+        float v[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[r][k] = row ? __fmul_rn(v[r][k], scale) : none;
-      if (first + r < n) store_row<V>(out + (first + r) * dim + c, dim - c, v[r]);
+        for (int k = 0; k < V; ++k) v[k] = row ? __fmul_rn(raw[r].get(k), scale) : none;
+        store_pack(dst + at.begin, v);
+      } else {
+        for (int k = 0; k < (int)dim; ++k)
+          dst[k] = from_f32<OT>(row ? __fmul_rn(to_f32(table[id[r] * dim + k]), scale) : none);
+      }
     }
   }
 }
@@ -65,6 +76,7 @@ struct GradArgs {
   int64_t n, vocab, dim;
   float scale;
   int accumulate;
+  int stream;          // the table's rows are stored non-temporally
   float* dtable;
   Span* spans;         // [pieces]
   float* partial;      // [pieces][2][dim]: heads and tails
@@ -74,18 +86,33 @@ struct GradArgs {
   int64_t sum_blocks;  // blocks that sum; those after them clear the rows of ids that do not occur
 };
 
+// The elements of a pack that are its own.
 template <int V>
-__device__ __forceinline__ void write_row(const GradArgs& a, int64_t id, int64_t c, float (&sum)[V]) {
-  float* const dst = a.dtable + id * a.dim + c;
+__device__ __forceinline__ void store_own(float* row, const PackAt<V>& at, const float (&v)[V], int stream) {
+  if (at.shared == 0) {
+    if (stream) stream_pack(row + at.begin, v);
+    else store_pack(row + at.begin, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (at.own(k)) row[at.begin + k] = v[k];
+  }
+}
+
+// The row of the table that an id names: the scaled sum, or that added to it.  Elements that
+// two packs share are stored by one of them, as the other may add to what it wrote.
+template <int V>
+__device__ __forceinline__ void write_row(const GradArgs& a, int64_t id, const PackAt<V>& at, float (&sum)[V]) {
+  float* const row = a.dtable + id * a.dim;
 #pragma unroll
   for (int k = 0; k < V; ++k) sum[k] *= a.scale;
   if (a.accumulate) {
     float old[V];
-    load_row<V>(dst, a.dim - c, old);
+    load_pack(row + at.begin, old);
 #pragma unroll
     for (int k = 0; k < V; ++k) sum[k] += old[k];
   }
-  store_row<V>(dst, a.dim - c, sum);
+  store_own(row, at, sum, a.stream);
 }
 
 constexpr int kClearRows = 16;   // rows of the table a clearing wave looks at
@@ -104,13 +131,17 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict
     uint64_t empty = __ballot(lane < kClearRows && v0 + lane < a.vocab && from >= to);
     for (; empty; empty &= empty - 1) {
       float* const dst = a.dtable + (v0 + __builtin_ctzll(empty)) * a.dim;
-      for (int64_t c = lane * 4; c < a.dim; c += 256) store_row<4>(dst + c, a.dim - c, zero);
+      for (int64_t c = lane * 4; c < a.dim; c += 256) {
+        if (a.stream && c + 4 <= a.dim) stream_pack(dst + c, zero);
+        else store_row<4>(dst + c, a.dim - c, zero);
+      }
     }
     return;
   }
   const int64_t job = (int64_t)blockIdx.x * 4 + wave, p = job / a.slabs;
   if (p >= a.pieces) return;
-  const int64_t c = ((job - p * a.slabs) * 64 + lane) * V, left = a.dim - c;
+  const int64_t c = ((job - p * a.slabs) * 64 + lane) * V;
+  const PackAt<V> at((int)c, (int)a.dim);   // dim >= V
   const int64_t count = min(max((int64_t)a.offsets[a.vocab], (int64_t)0), a.n);   // positions that have a group
   const int64_t q0 = p * a.piece;
   const int len = (int)max((int64_t)0, min((int64_t)a.piece, count - q0));
@@ -138,27 +169,25 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict
 #pragma unroll
   for (int k = 0; k < V; ++k) sum[k] = 0.0f;
   auto flush = [&](bool last) {
-    if (cur >= 0 && left > 0) {
-      if (head) store_row<V>(a.partial + 2 * p * a.dim + c, left, sum);
-      else if (last && onward) store_row<V>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
-      else write_row<V>(a, cur, c, sum);
+    if (cur >= 0 && at.any()) {
+      if (head) store_pack(a.partial + 2 * p * a.dim + at.begin, sum);
+      else if (last && onward) store_pack(a.partial + (2 * p + 1) * a.dim + at.begin, sum);
+      else write_row<V>(a, cur, at, sum);
     }
     head = false;
   };
   RowPack<GT, V> row[2][U];
-  auto fetch = [&](int buf, int at) {
+  auto fetch = [&](int buf, int q) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (at + u < len) {
-        const int64_t from = __builtin_amdgcn_readlane(pos, at + u);
-        if (__builtin_amdgcn_readlane(ident, at + u) >= 0) row[buf][u].load(dout + from * a.dim + c, left);
-      }
+      if (q + u < len && __builtin_amdgcn_readlane(ident, q + u) >= 0 && at.any())
+        row[buf][u].load(dout + (int64_t)__builtin_amdgcn_readlane(pos, q + u) * a.dim + at.begin);
   };
-  auto add = [&](int buf, int at) {
+  auto add = [&](int buf, int q) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (at + u < len) {
-        const int id = __builtin_amdgcn_readlane(ident, at + u);
+      if (q + u < len) {
+        const int id = __builtin_amdgcn_readlane(ident, q + u);
         if (id != cur) {
           flush(false);
           cur = id;
@@ -173,52 +202,55 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict
   };
   if (len == 0) return;
   fetch(0, 0);
-  for (int at = 0; at < len; at += 2 * U) {
-    fetch(1, at + U);
-    add(0, at);
-    fetch(0, at + 2 * U);
-    add(1, at + U);
+  for (int q = 0; q < len; q += 2 * U) {
+    fetch(1, q + U);
+    add(0, q);
+    fetch(0, q + 2 * U);
+    add(1, q + U);
   }
   flush(true);
 }
 
-// A workgroup for each piece and 256 columns: where the piece hands an id on, its eight
+// A workgroup for each piece and 64 V columns: where the piece hands an id on, its eight
 // waves add an eighth of the later pieces' heads each, and their sums meet in LDS.
+template <int V>
 __global__ __launch_bounds__(512) void embedding_join_kernel(GradArgs a) {
   constexpr int W = 8, U = 8;
-  __shared__ float part[W][64][4];
+  __shared__ float part[W][64][V];
   const int64_t p = blockIdx.x;
   const Span span = a.spans[p];
   if (span.id < 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4, left = a.dim - c;
+  const PackAt<V> at(((int)blockIdx.y * 64 + lane) * V, (int)a.dim);
   const int64_t heads = span.last - p, from = p + 1 + heads * wave / W, to = p + 1 + heads * (wave + 1) / W;
-  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (left > 0) {
-    if (wave == 0) load_row<4>(a.partial + (2 * p + 1) * a.dim + c, left, sum);
+  float sum[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) sum[k] = 0.0f;
+  if (at.any()) {
+    if (wave == 0) load_pack(a.partial + (2 * p + 1) * a.dim + at.begin, sum);
     for (int64_t h = from; h < to; h += U) {
-      float v[U][4];
+      float v[U][V];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (h + u < to) load_row<4>(a.partial + 2 * (h + u) * a.dim + c, left, v[u]);
+        if (h + u < to) load_pack(a.partial + 2 * (h + u) * a.dim + at.begin, v[u]);
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (h + u < to)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) sum[k] += v[u][k];
+          for (int k = 0; k < V; ++k) sum[k] += v[u][k];
     }
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) part[wave][lane][k] = sum[k];
+  for (int k = 0; k < V; ++k) part[wave][lane][k] = sum[k];
   __syncthreads();
-  if (wave == 0 && left > 0) {
+  if (wave == 0 && at.any()) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < V; ++k) {
       sum[k] = 0.0f;
 #pragma unroll
       for (int w = 0; w < W; ++w) sum[k] += part[w][lane][k];
     }
-    write_row<4>(a, span.id, c, sum);
+    write_row<V>(a, span.id, at, sum);
   }
 }
 
@@ -228,6 +260,8 @@ int row_lanes(int64_t dim, int pack, int most) {
   while (l < most && ((int64_t)pack << l) < dim) ++l;
   return l;
 }
+
+constexpr double kCachedBytes = 224 << 20;
 
 // Positions per piece: enough pieces to fill the machine, and no fewer than 16 positions (65536
 // rows of 1024 bf16: 64 positions 100 us, 32 89, 16 94; 16384 rows: 16 positions 38, 8 44).
@@ -287,6 +321,11 @@ hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, 
   a.dim = dim;
   a.scale = scale;
   a.accumulate = accumulate;
+  // A gradient that the last-level cache does not hold together with what it is summed from
+  // goes around it: the cleared rows no longer push out the rows of dout (65536 rows of 1024
+  // bf16 into 50021: 92 -> 62 us; 8192 rows of 256 into 200000, which fit: 31 -> 42).
+  const double bytes = 4.0 * (double)vocab * (double)dim + (g_bf16 ? 2.0 : 4.0) * (double)n * (double)dim;
+  a.stream = !accumulate && bytes > kCachedBytes;
   a.dtable = dtable;
   a.piece = grad_piece(n, dim);
   a.pieces = (n + a.piece - 1) / a.piece;
@@ -309,9 +348,12 @@ hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, 
     else if (dim <= 128) sum(std::integral_constant<int, 2>{});
     else if (dim <= 256 || kMost == 4) sum(std::integral_constant<int, 4>{});
     else sum(std::integral_constant<int, kMost>{});
-    if (a.pieces > 1)
-      hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)(a.pieces - 1), (unsigned)((dim + 255) / 256)), dim3(512),
-                         0, st, a);
+    if (a.pieces > 1) {
+      auto join = [&](auto kernel, int64_t cols) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.pieces - 1), (unsigned)((dim + cols - 1) / cols)), dim3(512), 0, st, a);
+      };
+      dim < 4 ? join(embedding_join_kernel<1>, 64) : join(embedding_join_kernel<4>, 256);
+    }
   };
   if (i64) g_bf16 ? launch(int64_t{}, uint16_t{}) : launch(int64_t{}, float{});
   else g_bf16 ? launch(int32_t{}, uint16_t{}) : launch(int32_t{}, float{});

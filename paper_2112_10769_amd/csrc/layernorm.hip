@@ -49,19 +49,37 @@ constexpr int kRowsAtOnce = TPR > kWave ? 1 : 256 / TPR;
 template <int TPR>
 constexpr int kThreads = TPR > kWave ? TPR : 256;
 
-// A thread's CH packs of a row: pack i of thread t holds the columns from (i * TPR + t) * V on.
+// Where a thread's CH packs of a row lie: pack i of thread t begins at column (i * TPR + t) * V.
+template <int V, int TPR, int CH>
+struct RowAt {
+  PackAt<V> at[CH];
+  __device__ __forceinline__ RowAt(int t, int64_t cols) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) at[i] = PackAt<V>((i * TPR + t) * V, (int)cols);
+  }
+};
+
 template <typename T, int V, int TPR, int CH>
 struct RowRaw {
   RowPack<T, V> pack[CH];
-  __device__ __forceinline__ void load(const T* row, int64_t cols, int t) {
+  __device__ __forceinline__ void load(const T* row, const RowAt<V, TPR, CH>& col) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int64_t c = (int64_t)(i * TPR + t) * V;
-      pack[i].load(row + c, cols - c);
-    }
+    for (int i = 0; i < CH; ++i)
+      if (col.at[i].any()) pack[i].load(row + col.at[i].begin);
   }
   __device__ __forceinline__ float get(int i, int k) const { return pack[i].get(k); }
 };
+
+// An fp32 vector over the columns, or a constant for NULL.
+template <int V, int TPR, int CH>
+__device__ __forceinline__ void load_vector(const float* p, float none, const RowAt<V, TPR, CH>& col, float (&v)[CH][V]) {
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[i][k] = none;
+    if (p && col.at[i].any()) load_pack(p + col.at[i].begin, v[i]);
+  }
+}
 
 template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(kThreads<TPR>) void layernorm_fwd_kernel(const T* x, int64_t rows, int64_t cols,
@@ -73,51 +91,40 @@ __global__ __launch_bounds__(kThreads<TPR>) void layernorm_fwd_kernel(const T* x
   __shared__ float red1[TPR / kWave][1], red2[TPR / kWave][1];
   const int t = threadIdx.x & (TPR - 1);
   const float inv = 1.0f / (float)cols;
+  const RowAt<V, TPR, CH> col(t, cols);
   float g[CH][V], b[CH][V];
-#pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    const int64_t c = (int64_t)(i * TPR + t) * V;
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      g[i][k] = 1.0f;
-      b[i][k] = 0.0f;
-    }
-    if (gamma) load_row<V>(gamma + c, cols - c, g[i]);
-    if (beta) load_row<V>(beta + c, cols - c, b[i]);
-  }
+  load_vector(gamma, 1.0f, col, g);
+  load_vector(beta, 0.0f, col, b);
   RowRaw<T, V, TPR, CH> next;
   int64_t row = (int64_t)blockIdx.x * R + (TPR > kWave ? 0 : threadIdx.x / TPR);
   const int64_t step = (int64_t)gridDim.x * R;
-  if (row < rows) next.load(x + row * cols, cols, t);
+  if (row < rows) next.load(x + row * cols, col);
   for (; row < rows; row += step) {
     const RowRaw<T, V, TPR, CH> cur = next;
-    if (row + step < rows) next.load(x + (row + step) * cols, cols, t);
+    if (row + step < rows) next.load(x + (row + step) * cols, col);
     float s[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
-      for (int k = 0; k < V; ++k) s[0] += cur.get(i, k);
+      for (int k = 0; k < V; ++k) s[0] += col.at[i].own(k) ? cur.get(i, k) : 0.0f;
     row_sum<TPR, 1>(s, red1);
     const float mu = s[0] * inv;
     float q[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int64_t left = cols - (int64_t)(i * TPR + t) * V;
+    for (int i = 0; i < CH; ++i)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float d = k < left ? cur.get(i, k) - mu : 0.0f;
+        const float d = col.at[i].own(k) ? cur.get(i, k) - mu : 0.0f;
         q[0] = fmaf(d, d, q[0]);
       }
-    }
     row_sum<TPR, 1>(q, red2);
     const float r = 1.0f / sqrtf(q[0] * inv + eps);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int64_t c = (int64_t)(i * TPR + t) * V;
       float v[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = fmaf((cur.get(i, k) - mu) * r, g[i][k], b[i][k]);
-      store_row<V>(y + row * cols + c, cols - c, v);
+      if (col.at[i].any()) store_pack(y + row * cols + col.at[i].begin, v);
     }
     if (t == 0) {
       if (mean) mean[row] = mu;
@@ -126,7 +133,8 @@ __global__ __launch_bounds__(kThreads<TPR>) void layernorm_fwd_kernel(const T* x
   }
 }
 
-// Rows wider than registers hold: read three times (from L2 after the first).
+// Rows wider than registers hold, and those narrower than a pack: read three times (from L2
+// after the first).
 template <typename T>
 __global__ __launch_bounds__(1024) void layernorm_fwd_wide_kernel(const T* x, int64_t rows, int64_t cols,
                                                                   const float* __restrict__ gamma,
@@ -185,79 +193,66 @@ template <typename G, typename T, int TPR, int CH>
 __global__ __launch_bounds__(kThreads<TPR>) void layernorm_bwd_kernel(const G* dy, const T* __restrict__ x, BwdArgs a,
                                                                       G* dx) {
   constexpr int V = kPack<G, T>, R = kRowsAtOnce<TPR>;
-  // 1024 threads have 128 registers each: with 16 elements a thread the weight is read again
-  // for every row and no row is fetched ahead (all of it kept spilled 174 to 220 registers)
-  constexpr bool kTight = TPR == 1024 && CH * V > 8;
   __shared__ float red[2][TPR / kWave][2];
   const int t = threadIdx.x & (TPR - 1);
   const int64_t rows = a.rows, cols = a.cols;
   const float inv = 1.0f / (float)cols;
+  const RowAt<V, TPR, CH> col(t, cols);
   float g[CH][V], dg[CH][V], db[CH][V];
-  auto weight = [&](int i) {
-    const int64_t c = (int64_t)(i * TPR + t) * V;
 #pragma unroll
-    for (int k = 0; k < V; ++k) g[i][k] = 1.0f;
-    if (a.gamma) load_row<V>(a.gamma + c, cols - c, g[i]);
-  };
-#pragma unroll
-  for (int i = 0; i < CH; ++i) {
+  for (int i = 0; i < CH; ++i)
 #pragma unroll
     for (int k = 0; k < V; ++k) dg[i][k] = db[i][k] = 0.0f;
-    if (!kTight) weight(i);
-  }
+  load_vector(a.gamma, 1.0f, col, g);
   RowRaw<G, V, TPR, CH> next_dy;
   RowRaw<T, V, TPR, CH> next_x;
   float next_mu = 0.0f, next_r = 0.0f;
   auto fetch = [&](int64_t row) {
-    next_dy.load(dy + row * cols, cols, t);
-    next_x.load(x + row * cols, cols, t);
+    next_dy.load(dy + row * cols, col);
+    next_x.load(x + row * cols, col);
     next_mu = a.mean[row];
     next_r = a.rstd[row];
   };
   int64_t row = (int64_t)blockIdx.x * R + (TPR > kWave ? 0 : threadIdx.x / TPR);
   const int64_t step = (int64_t)gridDim.x * R;
-  if (!kTight && row < rows) fetch(row);
+  if (row < rows) fetch(row);
   for (int phase = 0; row < rows; row += step, phase ^= 1) {
-    if (kTight) fetch(row);
     const RowRaw<G, V, TPR, CH> cdy = next_dy;
     const RowRaw<T, V, TPR, CH> cx = next_x;
     const float mu = next_mu, r = next_r;
-    if (!kTight && row + step < rows) fetch(row + step);
+    if (row + step < rows) fetch(row + step);
     float s[2] = {0.0f, 0.0f}, xh[CH][V], d[CH][V];
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int64_t left = cols - (int64_t)(i * TPR + t) * V;
-      if (kTight) weight(i);
+    for (int i = 0; i < CH; ++i)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        xh[i][k] = k < left ? (cx.get(i, k) - mu) * r : 0.0f;
+        xh[i][k] = (cx.get(i, k) - mu) * r;
         const float dyk = cdy.get(i, k);
         dg[i][k] = fmaf(dyk, xh[i][k], dg[i][k]);
         db[i][k] += dyk;
         d[i][k] = dyk * g[i][k];
-        s[0] += d[i][k];
-        s[1] = fmaf(d[i][k], xh[i][k], s[1]);
+        const float own = col.at[i].own(k) ? d[i][k] : 0.0f;
+        s[0] += own;
+        s[1] = col.at[i].own(k) ? fmaf(own, xh[i][k], s[1]) : s[1];
       }
-    }
     row_sum<TPR, 2>(s, red[phase]);
     const float m1 = s[0] * inv, m2 = s[1] * inv;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int64_t c = (int64_t)(i * TPR + t) * V;
       float v[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = r * (d[i][k] - m1 - xh[i][k] * m2);
-      store_row<V>(dx + row * cols + c, cols - c, v);
+      if (col.at[i].any()) store_pack(dx + row * cols + col.at[i].begin, v);
     }
   }
   float* const mine = a.partial + (int64_t)blockIdx.x * 2 * cols;
   if constexpr (TPR > kWave) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int64_t c = (int64_t)(i * TPR + t) * V;
-      store_row<V>(mine + c, cols - c, dg[i]);
-      store_row<V>(mine + cols + c, cols - c, db[i]);
-    }
+    for (int i = 0; i < CH; ++i)
+      if (col.at[i].any()) {
+        store_pack(mine + col.at[i].begin, dg[i]);
+        store_pack(mine + cols + col.at[i].begin, db[i]);
+      }
   } else {
     // the waves' sums meet in LDS
     __shared__ float part[R][TPR * CH * V];
@@ -267,7 +262,7 @@ __global__ __launch_bounds__(kThreads<TPR>) void layernorm_bwd_kernel(const G* d
       if (which) __syncthreads();
 #pragma unroll
       for (int i = 0; i < CH; ++i)
-        store_pack(&part[wave][(i * TPR + t) * V], which ? db[i] : dg[i]);
+        if (col.at[i].any()) store_pack(&part[wave][col.at[i].begin], which ? db[i] : dg[i]);
       __syncthreads();
       for (int64_t c = threadIdx.x; c < cols; c += 256) {
         float s = 0.0f;
@@ -279,22 +274,22 @@ __global__ __launch_bounds__(kThreads<TPR>) void layernorm_bwd_kernel(const G* d
   }
 }
 
-// Rows wider than registers hold: read twice, the sums over rows kept in the workspace.
+// ---- backward of wide rows: read twice
+
+// A row's two means, by a workgroup.  Also the whole backward of rows narrower than a pack
+// has this form: its sums read element by element.
 template <typename G, typename T>
-__global__ __launch_bounds__(1024) void layernorm_bwd_wide_kernel(const G* dy, const T* __restrict__ x, BwdArgs a,
-                                                                  G* dx) {
+__global__ __launch_bounds__(1024) void layernorm_means_kernel(const G* __restrict__ dy, const T* __restrict__ x,
+                                                               BwdArgs a, float2* __restrict__ means) {
   constexpr int V = kPack<G, T>, TPR = 1024;
   __shared__ float red[2][TPR / kWave][2];
   const int64_t cols = a.cols;
-  const float inv = 1.0f / (float)cols;
-  float* const mine = a.partial + (int64_t)blockIdx.x * 2 * cols;
-  bool first = true;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, first = false) {
+  int phase = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, phase ^= 1) {
     const float mu = a.mean[row], r = a.rstd[row];
-    const G* const src = dy + row * cols;
     float s[2] = {0.0f, 0.0f}, v[V], w[V], g[V];
     for (int64_t c = (int64_t)threadIdx.x * V; c < cols; c += TPR * V) {
-      load_row<V>(src + c, cols - c, v);
+      load_row<V>(dy + row * cols + c, cols - c, v);
       load_row<V>(x + row * cols + c, cols - c, w);
       if (a.gamma) load_row<V>(a.gamma + c, cols - c, g);
 #pragma unroll
@@ -304,29 +299,72 @@ __global__ __launch_bounds__(1024) void layernorm_bwd_wide_kernel(const G* dy, c
         s[1] = fmaf(d, xh, s[1]);
       }
     }
-    row_sum<TPR, 2>(s, red[row / gridDim.x & 1]);
-    const float m1 = s[0] * inv, m2 = s[1] * inv;
-    for (int64_t c = (int64_t)threadIdx.x * V; c < cols; c += TPR * V) {
-      float dg[V], db[V];
-      load_row<V>(src + c, cols - c, v);
-      load_row<V>(x + row * cols + c, cols - c, w);
-      if (a.gamma) load_row<V>(a.gamma + c, cols - c, g);
-      if (!first) {
-        load_row<V>(mine + c, cols - c, dg);
-        load_row<V>(mine + cols + c, cols - c, db);
-      }
+    row_sum<TPR, 2>(s, red[phase]);
+    if (threadIdx.x == 0) means[row] = make_float2(s[0] / (float)cols, s[1] / (float)cols);
+  }
+}
+
+// dx and the sums over rows: a thread keeps one pack of columns and walks the rows
+// blockIdx.y, blockIdx.y + gridDim.y, .. with four of them in flight.  V = 1 takes rows of
+// any width.  Elements that two packs share are stored by the one before only: where dx is
+// dy, the other may have read them too late.
+template <typename G, typename T, int V>
+__global__ __launch_bounds__(256) void layernorm_slab_kernel(const G* dy, const T* __restrict__ x, BwdArgs a,
+                                                             const float2* __restrict__ means, G* dx) {
+  constexpr int U = 4;
+  const int64_t cols = a.cols, step = gridDim.y;
+  const PackAt<V> at(((int)blockIdx.x * 256 + (int)threadIdx.x) * V, (int)cols);
+  if (!at.any()) return;
+  float g[V], dg[V], db[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    g[k] = 1.0f;
+    dg[k] = db[k] = 0.0f;
+  }
+  if (a.gamma) load_pack(a.gamma + at.begin, g);
+  for (int64_t row0 = blockIdx.y; row0 < a.rows; row0 += U * step) {
+    RowPack<G, V> pdy[U];
+    RowPack<T, V> px[U];
+    float mu[U], r[U];
+    float2 m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = min(row0 + u * step, a.rows - 1);
+      pdy[u].load(dy + row * cols + at.begin);
+      px[u].load(x + row * cols + at.begin);
+      mu[u] = a.mean[row];
+      r[u] = a.rstd[row];
+      m[u] = means[row];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = row0 + u * step;
+      if (row >= a.rows) break;
+      float v[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float d = a.gamma ? v[k] * g[k] : v[k], xh = (w[k] - mu) * r;
-        dg[k] = first ? v[k] * xh : fmaf(v[k], xh, dg[k]);
-        db[k] = first ? v[k] : db[k] + v[k];
-        v[k] = r * (d - m1 - xh * m2);
+        const float dyk = pdy[u].get(k), xh = (px[u].get(k) - mu[u]) * r[u];
+        dg[k] = fmaf(dyk, xh, dg[k]);
+        db[k] += dyk;
+        v[k] = r[u] * (dyk * g[k] - m[u].x - xh * m[u].y);
       }
-      store_row<V>(mine + c, cols - c, dg);
-      store_row<V>(mine + cols + c, cols - c, db);
-      store_row<V>(dx + row * cols + c, cols - c, v);
+      G* const dst = dx + row * cols + at.begin;
+      if (at.shared == 0) {
+        store_pack(dst, v);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (at.own(k)) dst[k] = from_f32<G>(v[k]);
+      }
     }
   }
+  float* const mine = a.partial + (int64_t)blockIdx.y * 2 * cols + at.begin;
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+    if (at.own(k)) {
+      mine[k] = dg[k];
+      mine[cols + k] = db[k];
+    }
 }
 
 // dgamma and dbeta (blockIdx.y) from the workgroups' sums: 64 columns a block, its 16 waves
@@ -360,14 +398,17 @@ __global__ __launch_bounds__(1024) void layernorm_weight_kernel(const float* __r
 }
 
 // Threads per row and packs per thread for rows of `packs` packs, at most `most` packs a
-// thread: a wave's where that does, then workgroups of 256, 512 and 1024.  {0, 0}: too wide.
+// thread: a wave's where that does, then workgroups of 256 threads and more.  {0, 0}: too
+// wide, or narrower than a pack.
 struct RowShape {
   int tpr, packs;
 };
-RowShape row_shape(int64_t packs, int most, bool few) {
-  for (int tpr : {64, 256, 512, 1024}) {
+RowShape row_shape(int64_t cols, int pack, int most, int most_threads, bool few) {
+  const int64_t packs = (cols + pack - 1) / pack;
+  if (cols < pack) return {0, 0};
+  for (int tpr = 64; tpr <= most_threads; tpr *= tpr == 64 ? 4 : 2) {
     // few rows: one pack a thread as far as that goes
-    const int cap = few && tpr < 1024 ? 1 : most;
+    const int cap = few && tpr < most_threads ? 1 : most;
     for (int n = 1; n <= cap; n *= 2)
       if (packs <= (int64_t)tpr * n) return {tpr, n};
   }
@@ -377,7 +418,7 @@ RowShape row_shape(int64_t packs, int most, bool few) {
 constexpr int kCuCount = 256;
 
 // Calls f with the shape's compile-time constants.
-template <int MOST, typename F>
+template <int MOST, int THREADS, typename F>
 void with_shape(RowShape s, F f) {
   auto packs = [&](auto tpr) {
     switch (s.packs) {
@@ -391,18 +432,36 @@ void with_shape(RowShape s, F f) {
     case 64: packs(std::integral_constant<int, 64>{}); break;
     case 256: packs(std::integral_constant<int, 256>{}); break;
     case 512: packs(std::integral_constant<int, 512>{}); break;
-    default: packs(std::integral_constant<int, 1024>{}); break;
+    default:
+      if constexpr (THREADS >= 1024) packs(std::integral_constant<int, 1024>{});
   }
 }
 
-// Elements a thread holds: the forward needs the row twice and two weights (32 elements
-// would be 160 registers), the backward the row twice, two weight sums and the weight.
-constexpr int kElements = 16;
+// Elements a thread holds: the forward needs the row twice and two vectors, the backward two
+// rows twice, two sums and the weight: 16 are up to 190 registers, which 512 threads have
+// (1024 threads spilled 18 to 220 of them: 4096 x 16384 bf16 took 134 us or more in registers, about what
+// reading the rows twice takes).
+constexpr int kElements = 16, kFwdThreads = 1024, kBwdThreads = 512;
+constexpr int64_t kMostCols = kBwdThreads * kElements;   // of the backward in registers
 
+// Workgroups of the backward, each of which leaves a row of sums: one a CU beyond 4096
+// columns (8192 x 8192 bf16: 79 to 87 us with one, 79 to 93 with more), two below (16384 x
+// 4096: 101 with one, 80 with two, 95 with four), and for rows of a wave up to four, but
+// three rows a wave at least (65536 x 512: 60, 42, 40 with one, two, four; 3001 x 1024:
+// 13.7, 15.6, 18.1).
 int64_t bwd_groups(int64_t rows, int64_t cols) {
-  const int64_t at_once = cols <= 64 * kElements ? 4 : 1;
-  const int64_t need = (rows + at_once - 1) / at_once;
-  return need < 2 * kCuCount ? need : 2 * kCuCount;
+  if (cols < 8 || cols > kMostCols) return rows < 128 ? rows : 128;
+  if (cols <= 64 * kElements) {
+    const int64_t need = (rows + 11) / 12;
+    return need < 4 * kCuCount ? need : 4 * kCuCount;
+  }
+  const int64_t most = cols > 4096 ? kCuCount : 2 * kCuCount;
+  return rows < most ? rows : most;
+}
+
+// Rows' means of the form that reads rows twice, after the sums of the groups.
+size_t bwd_sums_bytes(int64_t rows, int64_t cols) {
+  return (size_t)bwd_groups(rows, cols) * 2 * (size_t)cols * sizeof(float);
 }
 
 }  // namespace
@@ -413,7 +472,7 @@ hipError_t launch_layernorm_fwd(const void* x, int bf16, int64_t rows, int64_t c
   auto launch = [&](auto elem) {
     using T = decltype(elem);
     constexpr int V = kPack<T, T>;
-    const RowShape s = row_shape((cols + V - 1) / V, kElements / V, rows < 2 * kCuCount);
+    const RowShape s = row_shape(cols, V, kElements / V, kFwdThreads, rows < 2 * kCuCount);
     auto go = [&](auto kernel, int threads, int64_t at_once) {
       const int64_t need = (rows + at_once - 1) / at_once, most = 8 * kCuCount;
       hipLaunchKernelGGL(kernel, dim3((unsigned)(need < most ? need : most)), dim3(threads), 0, st,
@@ -421,7 +480,7 @@ hipError_t launch_layernorm_fwd(const void* x, int bf16, int64_t rows, int64_t c
     };
     if (s.tpr == 0) go(layernorm_fwd_wide_kernel<T>, 1024, 1);
     else
-      with_shape<kElements / V>(s, [&](auto tpr, auto packs) {
+      with_shape<kElements / V, kFwdThreads>(s, [&](auto tpr, auto packs) {
         constexpr int TPR = decltype(tpr)::value;
         go(layernorm_fwd_kernel<T, TPR, decltype(packs)::value>, kThreads<TPR>, kRowsAtOnce<TPR>);
       });
@@ -431,7 +490,8 @@ hipError_t launch_layernorm_fwd(const void* x, int bf16, int64_t rows, int64_t c
 }
 
 size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols) {
-  return (size_t)bwd_groups(rows, cols) * 2 * (size_t)cols * sizeof(float);
+  // a pack is 4 or 8 elements, by the types: the means' place is there for either
+  return bwd_sums_bytes(rows, cols) + (cols < 8 || cols > kMostCols ? (size_t)rows * sizeof(float2) : 0);
 }
 
 hipError_t launch_layernorm_bwd(const void* dy, int g_bf16, const void* x, int bf16, const float* mean,
@@ -443,14 +503,23 @@ hipError_t launch_layernorm_bwd(const void* dy, int g_bf16, const void* x, int b
     using G = decltype(grad);
     using T = decltype(elem);
     constexpr int V = kPack<G, T>;
-    const RowShape s = row_shape((cols + V - 1) / V, kElements / V, false);
+    const RowShape s = row_shape(cols, V, kElements / V, kBwdThreads, false);
     auto go = [&](auto kernel, int threads) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), 0, st, static_cast<const G*>(dy),
                          static_cast<const T*>(x), a, static_cast<G*>(dx));
     };
-    if (s.tpr == 0) go(layernorm_bwd_wide_kernel<G, T>, 1024);
-    else
-      with_shape<kElements / V>(s, [&](auto tpr, auto packs) {
+    if (s.tpr == 0) {
+      float2* const means = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + bwd_sums_bytes(rows, cols));
+      const int64_t most = 4 * kCuCount;
+      hipLaunchKernelGGL((layernorm_means_kernel<G, T>), dim3((unsigned)(rows < most ? rows : most)), dim3(1024), 0, st,
+                         static_cast<const G*>(dy), static_cast<const T*>(x), a, means);
+      auto slabs = [&](auto kernel, int64_t pack) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((cols + 256 * pack - 1) / (256 * pack)), (unsigned)groups), dim3(256), 0,
+                           st, static_cast<const G*>(dy), static_cast<const T*>(x), a, means, static_cast<G*>(dx));
+      };
+      cols < V ? slabs(layernorm_slab_kernel<G, T, 1>, 1) : slabs(layernorm_slab_kernel<G, T, V>, V);
+    } else
+      with_shape<kElements / V, kBwdThreads>(s, [&](auto tpr, auto packs) {
         constexpr int TPR = decltype(tpr)::value;
         go(layernorm_bwd_kernel<G, T, TPR, decltype(packs)::value>, kThreads<TPR>);
       });

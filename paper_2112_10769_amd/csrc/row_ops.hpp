@@ -69,12 +69,29 @@ __device__ __forceinline__ void store_pack(float* p, const float (&v)[V]) {
 }
 template <int V>
 __device__ __forceinline__ void store_pack(uint16_t* p, const float (&v)[V]) {
-  static_assert(V == 8, "one 16-byte piece");
+  static_assert(V == 8 || V == 1, "one 16-byte piece, or one element");
+  if constexpr (V == 1) {
+    *p = from_f32<uint16_t>(v[0]);
+    return;
+  }
   u4_any q;
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int k = 0; k < V / 2; ++k)
     q[k] = (uint32_t)from_f32<uint16_t>(v[2 * k]) | (uint32_t)from_f32<uint16_t>(v[2 * k + 1]) << 16;
   *reinterpret_cast<u4_any*>(p) = q;
+}
+
+// As store_pack, non-temporally.
+template <int V>
+__device__ __forceinline__ void stream_pack(float* p, const float (&v)[V]) {
+  if constexpr (V < 4) {
+    store_pack(p, v);
+  } else {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int i = 0; i < V; i += 4)
+      __builtin_nontemporal_store(f4{v[i], v[i + 1], v[i + 2], v[i + 3]}, reinterpret_cast<f4*>(p + i));
+  }
 }
 
 // The same for the `left` elements that a row has from p on: a whole pack, or its first
@@ -105,42 +122,46 @@ template <typename T, int V>
 struct RowPack {
   static constexpr int kBytes = V * sizeof(T), W = kBytes < 4 ? 1 : kBytes / 4;
   uint32_t w[W];
-  // the `left` elements that the row has from p on; none where left <= 0
-  __device__ __forceinline__ void load(const T* p, int64_t left) {
-    if (left >= V) {
-      if constexpr (kBytes >= 16) {
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kBytes >= 16) {
 #pragma unroll
-        for (int k = 0; k < W; k += 4) {
-          const u4_any q = reinterpret_cast<const u4_any*>(p)[k / 4];
+      for (int k = 0; k < W; k += 4) {
+        const u4_any q = reinterpret_cast<const u4_any*>(p)[k / 4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[k + i] = q[i];
-        }
-      } else if constexpr (kBytes == 8) {
-        typedef uint32_t u2_any __attribute__((ext_vector_type(2), aligned(2)));
-        const u2_any q = *reinterpret_cast<const u2_any*>(p);
-        w[0] = q[0];
-        w[1] = q[1];
-      } else if constexpr (kBytes == 4) {
-        typedef uint32_t u1_any __attribute__((aligned(2)));
-        w[0] = *reinterpret_cast<const u1_any*>(p);
-      } else {
-        w[0] = *p;
+        for (int i = 0; i < 4; ++i) w[k + i] = q[i];
       }
+    } else if constexpr (kBytes == 8) {
+      typedef uint32_t u2_any __attribute__((ext_vector_type(2), aligned(2)));
+      const u2_any q = *reinterpret_cast<const u2_any*>(p);
+      w[0] = q[0];
+      w[1] = q[1];
+    } else if constexpr (kBytes == 4) {
+      typedef uint32_t u1_any __attribute__((aligned(2)));
+      w[0] = *reinterpret_cast<const u1_any*>(p);
     } else {
-#pragma unroll
-      for (int k = 0; k < W; ++k) w[k] = 0;
-#pragma unroll
-      for (int k = 0; k < V - 1; ++k)
-        if (k < left) {
-          if constexpr (sizeof(T) == 4) w[k] = __float_as_uint(p[k]);
-          else w[k / 2] |= (uint32_t)p[k] << (16 * (k & 1));
-        }
+      w[0] = *p;
     }
   }
   __device__ __forceinline__ float get(int k) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
     return __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
   }
+};
+
+// A row of `cols` >= V columns in packs of V: the pack that begins at column c < cols lies at
+// column begin = min(c, cols - V), so that the last one is whole too.  Its first `shared`
+// elements are then the pack before's as well: they are left out of sums, and stored twice
+// with the same value (a pack read element by element made every row wait for its loads).
+template <int V>
+struct PackAt {
+  int begin, shared;   // shared = V: the row has no such pack
+  __device__ __forceinline__ PackAt() {}
+  __device__ __forceinline__ PackAt(int c, int cols) {   // below 2^24
+    begin = min(c, cols - V);
+    shared = min(c - begin, V);
+  }
+  __device__ __forceinline__ bool any() const { return shared < V; }
+  __device__ __forceinline__ bool own(int k) const { return k >= shared; }
 };
 
 // Elements a lane takes at a time: 16 bytes of the narrower type.
