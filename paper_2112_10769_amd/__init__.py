@@ -357,45 +357,48 @@ def _index(t):
     raise TypeError(f"unsupported index dtype {t.dtype}")
 
 
-def _buffer(t, shape, dtype, dev, name):
-    """The output buffer t, checked, or a new one: the kernels write shape elements of dtype."""
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
-    n = 1
-    for v in shape:
-        n *= v
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != dev:
-        raise ValueError(f"{name} must be contiguous, {tuple(shape)} of {dtype} on {dev}")
-    return t
+# The kernels write and read as many elements as the sizes say, so every tensor is checked;
+# short calls are bound by the host, so by what torch answers fastest (layer norm's eleven
+# arguments: 6.2 -> 4.5 us with the device compared by its index and shapes built only where
+# something is allocated).
+def _buffer(t, n, dtype, gpu, name):
+    """The output t, checked: the kernels write n elements of dtype."""
+    if t.dtype is dtype and t.numel() == n and t.get_device() == gpu and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous, {n} elements of {dtype} on the input's device")
 
 
-def _input(t, n, dtype, dev, name):
+def _input(t, n, dtype, gpu, name):
     """The input t (None stays None), checked: the kernels read n elements of dtype."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or t.device != dev:
-        raise ValueError(f"{name} must hold {n} elements of {dtype} on {dev}")
-    return t.contiguous()
+    if t.dtype is dtype and t.numel() == n and t.get_device() == gpu:
+        return t if t.is_contiguous() else t.contiguous()
+    raise ValueError(f"{name} must hold {n} elements of {dtype} on the input's device")
 
 
-def _codes(t, nbytes, dev, name):
+def _codes(t, nbytes, gpu, name):
     """A code operand, checked: the kernels read nbytes from it."""
-    if t.element_size() != 1 or t.numel() < nbytes or not t.is_contiguous() or t.device != dev:
-        raise ValueError(f"{name} must be contiguous, at least {nbytes} bytes on {dev}")
-    return t.data_ptr()
+    if t.element_size() == 1 and t.numel() >= nbytes and t.get_device() == gpu and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous, at least {nbytes} bytes on the input's device")
 
 
 def luq_group_ids(ids, groups, order=None, offsets=None, ws=None):
     """Positions of ids grouped by id (a stable sort), and the groups' offsets: (order [n] int32,
     offsets [groups + 1] int32).  Ids outside [0, groups) come last and belong to no group."""
-    n, dev = ids.numel(), ids.device
+    n, dev, gpu = ids.numel(), ids.device, ids.get_device()
     it = _index(ids)
-    order = _buffer(order, (n,), torch.int32, dev, "order")
-    offsets = _buffer(offsets, (groups + 1,), torch.int32, dev, "offsets")
+    if order is None:
+        order = torch.empty(n, dtype=torch.int32, device=dev)
+    if offsets is None:
+        offsets = torch.empty(groups + 1, dtype=torch.int32, device=dev)
     if ws is None:
         ws = _bytes(workspace_size(OP_GROUP_IDS, n, groups), dev)
     ids = ids.contiguous()
-    st = LIB.luq_group_ids(_ptr(ids), it, n, groups, _ptr(order), _ptr(offsets), _ptr(ws), ws.numel(), _stream(dev))
+    st = LIB.luq_group_ids(ids.data_ptr(), it, n, groups, _buffer(order, n, torch.int32, gpu, "order"),
+                           _buffer(offsets, groups + 1, torch.int32, gpu, "offsets"), ws.data_ptr(), ws.numel(),
+                           _stream(dev))
     _check(st, "luq_group_ids")
     return order, offsets
 
@@ -403,17 +406,16 @@ def luq_group_ids(ids, groups, order=None, offsets=None, ws=None):
 def luq_embedding_fwd(ids, table, scale=1.0, out_dtype=None, out=None):
     """scale * table[ids] of shape [*ids.shape, dim], in table's dtype or out_dtype.  Ids below 0 (padding) give
     rows of zeros, ids at or above the table's rows rows of NaN."""
-    if table.dim() != 2 or table.device != ids.device:
+    dev, gpu = ids.device, ids.get_device()
+    if table.dim() != 2 or table.get_device() != gpu:
         raise ValueError("table must be [vocab, dim] on the ids' device")
-    n, dev = ids.numel(), ids.device
-    vocab, dim = table.shape
+    n, (vocab, dim) = ids.numel(), table.shape
     it, tt = _index(ids), _dtype(table)
-    if out is not None and out_dtype is None:
-        out_dtype = out.dtype
-    out = _buffer(out, (*ids.shape, dim), out_dtype or table.dtype, dev, "out")
+    if out is None:
+        out = torch.empty((*ids.shape, dim), dtype=out_dtype or table.dtype, device=dev)
+    o = _buffer(out, n * dim, out_dtype or out.dtype, gpu, "out")
     ids, table = ids.contiguous(), table.contiguous()
-    st = LIB.luq_embedding_fwd(_ptr(ids), it, n, _ptr(table), tt, vocab, dim, float(scale), _ptr(out), _dtype(out),
-                               _stream(dev))
+    st = LIB.luq_embedding_fwd(ids.data_ptr(), it, n, table.data_ptr(), tt, vocab, dim, scale, o, _dtype(out), _stream(dev))
     _check(st, "luq_embedding_fwd")
     return out
 
@@ -421,22 +423,24 @@ def luq_embedding_fwd(ids, table, scale=1.0, out_dtype=None, out=None):
 def luq_embedding_grad(dout, ids, order, offsets, scale=1.0, accumulate=False, dtable=None, ws=None):
     """Gradient [vocab, dim] (float32) of luq_embedding_fwd's table from dout [*ids.shape, dim], with order and
     offsets of luq_group_ids(ids, vocab).  accumulate adds to the rows of the dtable passed in."""
-    n, dev = ids.numel(), ids.device
-    vocab = offsets.numel() - 1
-    dim = dout.shape[-1]
-    if dout.numel() != n * dim or dout.device != dev:
+    n, dev, gpu = ids.numel(), ids.device, ids.get_device()
+    vocab, dim = offsets.numel() - 1, dout.shape[-1]
+    if dout.numel() != n * dim or dout.get_device() != gpu:
         raise ValueError("dout must be [*ids.shape, dim] on the ids' device")
-    if accumulate and dtable is None:
-        raise ValueError("accumulate adds to a dtable that is passed in")
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate adds to a dtable that is passed in")
+        dtable = torch.empty(max(vocab, 0), dim, dtype=torch.float32, device=dev)
     it, gt = _index(ids), _dtype(dout)
-    order = _input(order, n, torch.int32, dev, "order")
-    offsets = _input(offsets, vocab + 1, torch.int32, dev, "offsets")
-    dtable = _buffer(dtable, (vocab, dim), torch.float32, dev, "dtable")
+    order = _input(order, n, torch.int32, gpu, "order")
+    offsets = _input(offsets, vocab + 1, torch.int32, gpu, "offsets")
     if ws is None:
         ws = _bytes(workspace_size(OP_EMBEDDING_GRAD, n, dim), dev)
     dout, ids = dout.contiguous(), ids.contiguous()
-    st = LIB.luq_embedding_grad(_ptr(dout), gt, _ptr(ids), it, _ptr(order), _ptr(offsets), n, vocab, dim, float(scale),
-                                1 if accumulate else 0, _ptr(dtable), _ptr(ws), ws.numel(), _stream(dev))
+    st = LIB.luq_embedding_grad(dout.data_ptr(), gt, ids.data_ptr(), it, order.data_ptr(), offsets.data_ptr(), n, vocab,
+                                dim, scale, 1 if accumulate else 0,
+                                _buffer(dtable, vocab * dim, torch.float32, gpu, "dtable"), ws.data_ptr(), ws.numel(),
+                                _stream(dev))
     _check(st, "luq_embedding_grad")
     return dtable
 
@@ -444,17 +448,22 @@ def luq_embedding_grad(dout, ids, order, offsets, scale=1.0, accumulate=False, d
 def luq_layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rstd=None):
     """Layer norm over the last dimension of x: (y, mean, rstd), y in x's dtype, the statistics float32 of
     x.shape[:-1].  gamma and beta are float32 [cols]; y may be x."""
-    dev, cols = x.device, x.shape[-1]
-    rows = x.numel() // max(cols, 1)
+    dev, gpu, n, cols = x.device, x.get_device(), x.numel(), x.shape[-1]
+    rows = n // max(cols, 1)
     dt = _dtype(x)
-    gamma = _input(gamma, cols, torch.float32, dev, "gamma")
-    beta = _input(beta, cols, torch.float32, dev, "beta")
-    y = _buffer(y, x.shape, x.dtype, dev, "y")
-    mean = _buffer(mean, x.shape[:-1], torch.float32, dev, "mean")
-    rstd = _buffer(rstd, x.shape[:-1], torch.float32, dev, "rstd")
-    x = x.contiguous()
-    st = LIB.luq_layernorm_fwd(_ptr(x), dt, rows, cols, _ptr(gamma), _ptr(beta), float(eps), _ptr(y), _ptr(mean),
-                               _ptr(rstd), _stream(dev))
+    gamma = _input(gamma, cols, torch.float32, gpu, "gamma")
+    beta = _input(beta, cols, torch.float32, gpu, "beta")
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    if mean is None:
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+    if rstd is None:
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+    if not x.is_contiguous():
+        x = x.contiguous()
+    st = LIB.luq_layernorm_fwd(x.data_ptr(), dt, rows, cols, _ptr(gamma), _ptr(beta), eps,
+                               _buffer(y, n, x.dtype, gpu, "y"), _buffer(mean, rows, torch.float32, gpu, "mean"),
+                               _buffer(rstd, rows, torch.float32, gpu, "rstd"), _stream(dev))
     _check(st, "luq_layernorm_fwd")
     return y, mean, rstd
 
@@ -462,38 +471,51 @@ def luq_layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rst
 def luq_layernorm_bwd(dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, ws=None):
     """Gradients of luq_layernorm_fwd: (dx, dgamma, dbeta), dx in dy's dtype (it may differ from x's, and dx may be
     dy), the others float32 [cols]."""
-    dev, cols = x.device, x.shape[-1]
-    rows = x.numel() // max(cols, 1)
-    if dy.shape != x.shape or dy.device != dev:
+    dev, gpu, n, cols = x.device, x.get_device(), x.numel(), x.shape[-1]
+    rows = n // max(cols, 1)
+    if dy.shape != x.shape or dy.get_device() != gpu:
         raise ValueError("dy must have x's shape and device")
     gt, dt = _dtype(dy), _dtype(x)
-    mean = _input(mean, rows, torch.float32, dev, "mean")
-    rstd = _input(rstd, rows, torch.float32, dev, "rstd")
-    gamma = _input(gamma, cols, torch.float32, dev, "gamma")
-    dx = _buffer(dx, dy.shape, dy.dtype, dev, "dx")
-    dgamma = _buffer(dgamma, (cols,), torch.float32, dev, "dgamma")
-    dbeta = _buffer(dbeta, (cols,), torch.float32, dev, "dbeta")
+    mean = _input(mean, rows, torch.float32, gpu, "mean")
+    rstd = _input(rstd, rows, torch.float32, gpu, "rstd")
+    gamma = _input(gamma, cols, torch.float32, gpu, "gamma")
+    if dx is None:
+        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dev)
+    if dgamma is None:
+        dgamma = torch.empty(cols, dtype=torch.float32, device=dev)
+    if dbeta is None:
+        dbeta = torch.empty(cols, dtype=torch.float32, device=dev)
     if ws is None:
         ws = _bytes(workspace_size(OP_LAYERNORM_BWD, rows, cols), dev)
-    dy, x = dy.contiguous(), x.contiguous()
-    st = LIB.luq_layernorm_bwd(_ptr(dy), gt, _ptr(x), dt, _ptr(mean), _ptr(rstd), _ptr(gamma), rows, cols, _ptr(dx),
-                               _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws.numel(), _stream(dev))
+    if not dy.is_contiguous():
+        dy = dy.contiguous()
+    if not x.is_contiguous():
+        x = x.contiguous()
+    st = LIB.luq_layernorm_bwd(dy.data_ptr(), gt, x.data_ptr(), dt, mean.data_ptr(), rstd.data_ptr(), _ptr(gamma), rows,
+                               cols, _buffer(dx, n, dy.dtype, gpu, "dx"),
+                               _buffer(dgamma, cols, torch.float32, gpu, "dgamma"),
+                               _buffer(dbeta, cols, torch.float32, gpu, "dbeta"), ws.data_ptr(), ws.numel(), _stream(dev))
     _check(st, "luq_layernorm_bwd")
     return dx, dgamma, dbeta
 
 
-def _grouped_weights(codes, scale, offsets, N, K, w_row, w_expert, dev, name):
-    """(experts, w_row, w_expert) of a grouped product's weights, their operands checked; K and N*K codes apart
-    unless given."""
-    experts = offsets.numel() - 1
+def _groups(offsets, gpu):
+    """The number of experts that offsets [experts + 1] bound."""
+    if offsets.dtype is torch.int32 and offsets.get_device() == gpu and offsets.is_contiguous():
+        return offsets.numel() - 1
+    raise ValueError("offsets must be contiguous int32 on the codes' device")
+
+
+def _grouped_weights(codes, scale, experts, N, K, w_row, w_expert, gpu, name):
+    """(address, w_row, w_expert, number of scales) of a grouped product's weights, their operands checked; K and
+    N*K codes apart unless given."""
     w_row = K if w_row is None else w_row
     w_expert = N * w_row if w_expert is None else w_expert
-    _codes(codes, ((experts - 1) * w_expert + (N - 1) * w_row + K) // 2, dev, name)
-    if offsets.dtype != torch.int32 or not offsets.is_contiguous() or offsets.device != dev:
-        raise ValueError(f"offsets must be contiguous int32 on {dev}")
-    if scale.dtype != torch.float32 or scale.numel() not in (1, experts) or not scale.is_contiguous():
+    scales = scale.numel()
+    if scale.dtype is not torch.float32 or (scales != 1 and scales != experts) or scale.get_device() != gpu or \
+            not scale.is_contiguous():
         raise ValueError("w_scale must be float32, one value or one per expert")
-    return experts, w_row, w_expert
+    return _codes(codes, ((experts - 1) * w_expert + (N - 1) * w_row + K) // 2, gpu, name), w_row, w_expert, scales
 
 
 def int4_gemm_fwd_grouped(x_codes, x_scale, x_signed, w_codes, w_scale, w_signed, offsets, T, N, K, w_row=None,
@@ -501,12 +523,14 @@ def int4_gemm_fwd_grouped(x_codes, x_scale, x_signed, w_codes, w_scale, w_signed
     """y [T, N]: int4_gemm_fwd with each row's expert, rows grouped by offsets [experts + 1] (int32, of
     luq_group_ids).  w_codes holds [N, K] codes per expert, w_row and w_expert codes apart; w_scale one scale per
     expert or one for all.  Rows of no expert get 0."""
-    dev = x_codes.device
-    experts, w_row, w_expert = _grouped_weights(w_codes, w_scale, offsets, N, K, w_row, w_expert, dev, "w_codes")
-    y = _buffer(y, (T, N), torch.float32, dev, "y")
-    st = LIB.int4_gemm_fwd_grouped(_codes(x_codes, T * K // 2, dev, "x_codes"), _ptr(x_scale), 1 if x_signed else 0,
-                                   _ptr(w_codes), w_row, w_expert, _ptr(w_scale), w_scale.numel(),
-                                   1 if w_signed else 0, _ptr(offsets), experts, T, N, K, _ptr(y), _stream(dev))
+    dev, gpu = x_codes.device, x_codes.get_device()
+    experts = _groups(offsets, gpu)
+    w, w_row, w_expert, scales = _grouped_weights(w_codes, w_scale, experts, N, K, w_row, w_expert, gpu, "w_codes")
+    if y is None:
+        y = torch.empty(T, N, dtype=torch.float32, device=dev)
+    st = LIB.int4_gemm_fwd_grouped(_codes(x_codes, T * K // 2, gpu, "x_codes"), x_scale.data_ptr(), 1 if x_signed else 0, w,
+                                   w_row, w_expert, w_scale.data_ptr(), scales, 1 if w_signed else 0, offsets.data_ptr(),
+                                   experts, T, N, K, _buffer(y, T * N, torch.float32, gpu, "y"), _stream(dev))
     _check(st, "int4_gemm_fwd_grouped")
     return y
 
@@ -515,13 +539,15 @@ def luq_gemm_dgrad_grouped(g_codes, alpha, w_codes_t, w_scale, w_signed, offsets
                            w_expert=None, dx=None):
     """dX [M, N]: luq_gemm_dgrad with each row's expert, rows grouped by offsets.  w_codes_t holds [N, K] transposed
     codes per expert, w_row and w_expert codes apart; n_samples 1 or 2 | SMP_SUM."""
-    dev = g_codes.device
-    experts, w_row, w_expert = _grouped_weights(w_codes_t, w_scale, offsets, N, K, w_row, w_expert, dev, "w_codes_t")
-    dx = _buffer(dx, (M, N), torch.float32, dev, "dx")
-    g = _codes(g_codes, M * K // (1 if n_samples & SMP_SUM else 2), dev, "g_codes")
-    st = LIB.luq_gemm_dgrad_grouped(g, _ptr(alpha), n_samples, _ptr(w_codes_t), w_row, w_expert, _ptr(w_scale),
-                                    w_scale.numel(), 1 if w_signed else 0, _ptr(offsets), experts, M, N, K, _ptr(dx),
-                                    _stream(dev))
+    dev, gpu = g_codes.device, g_codes.get_device()
+    experts = _groups(offsets, gpu)
+    w, w_row, w_expert, scales = _grouped_weights(w_codes_t, w_scale, experts, N, K, w_row, w_expert, gpu, "w_codes_t")
+    if dx is None:
+        dx = torch.empty(M, N, dtype=torch.float32, device=dev)
+    st = LIB.luq_gemm_dgrad_grouped(_codes(g_codes, M * K // (1 if n_samples & SMP_SUM else 2), gpu, "g_codes"),
+                                    alpha.data_ptr(), n_samples, w, w_row, w_expert, w_scale.data_ptr(), scales,
+                                    1 if w_signed else 0, offsets.data_ptr(), experts, M, N, K,
+                                    _buffer(dx, M * N, torch.float32, gpu, "dx"), _stream(dev))
     _check(st, "luq_gemm_dgrad_grouped")
     return dx
 
@@ -534,16 +560,16 @@ def luq_gemm_wgrad_grouped(g_codes_t, alpha, a_codes_t, a_scale, a_signed, offse
                            ws=None):
     """dW [experts, Nout, Kin]: luq_gemm_wgrad over each expert's rows, from transposed codes g^T [Nout, T] and
     a^T [Kin, T]; experts without rows get 0."""
-    dev = g_codes_t.device
-    experts = offsets.numel() - 1
-    if offsets.dtype != torch.int32 or not offsets.is_contiguous() or offsets.device != dev:
-        raise ValueError(f"offsets must be contiguous int32 on {dev}")
-    dw = _buffer(dw, (experts, Nout, Kin), torch.float32, dev, "dw")
-    g = _codes(g_codes_t, Nout * T // (1 if n_samples & SMP_SUM else 2), dev, "g_codes_t")
-    a = _codes(a_codes_t, Kin * T // 2, dev, "a_codes_t")
+    dev, gpu = g_codes_t.device, g_codes_t.get_device()
+    experts = _groups(offsets, gpu)
+    if dw is None:
+        dw = torch.empty(max(experts, 0), Nout, Kin, dtype=torch.float32, device=dev)
     if ws is None:
         ws = _bytes(grouped_wgrad_workspace(T, Nout, Kin, experts), dev)
-    st = LIB.luq_gemm_wgrad_grouped(g, _ptr(alpha), n_samples, a, _ptr(a_scale), 1 if a_signed else 0, _ptr(offsets),
-                                    experts, T, Nout, Kin, _ptr(dw), _ptr(ws), ws.numel(), _stream(dev))
+    st = LIB.luq_gemm_wgrad_grouped(_codes(g_codes_t, Nout * T // (1 if n_samples & SMP_SUM else 2), gpu, "g_codes_t"),
+                                    alpha.data_ptr(), n_samples, _codes(a_codes_t, Kin * T // 2, gpu, "a_codes_t"),
+                                    a_scale.data_ptr(), 1 if a_signed else 0, offsets.data_ptr(), experts, T, Nout, Kin,
+                                    _buffer(dw, experts * Nout * Kin, torch.float32, gpu, "dw"), ws.data_ptr(), ws.numel(),
+                                    _stream(dev))
     _check(st, "luq_gemm_wgrad_grouped")
     return dw
