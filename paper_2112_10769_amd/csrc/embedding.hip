@@ -76,7 +76,6 @@ struct GradArgs {
   int64_t n, vocab, dim;
   float scale;
   int accumulate;
-  int stream;          // the table's rows are stored non-temporally
   float* dtable;
   Span* spans;         // [pieces]
   float* partial;      // [pieces][2][dim]: heads and tails
@@ -88,10 +87,9 @@ struct GradArgs {
 
 // The elements of a pack that are its own.
 template <int V>
-__device__ __forceinline__ void store_own(float* row, const PackAt<V>& at, const float (&v)[V], int stream) {
+__device__ __forceinline__ void store_own(float* row, const PackAt<V>& at, const float (&v)[V]) {
   if (at.shared == 0) {
-    if (stream) stream_pack(row + at.begin, v);
-    else store_pack(row + at.begin, v);
+    store_pack(row + at.begin, v);
   } else {
 #pragma unroll
     for (int k = 0; k < V; ++k)
@@ -112,7 +110,7 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int64_t id, const P
 #pragma unroll
     for (int k = 0; k < V; ++k) sum[k] += old[k];
   }
-  store_own(row, at, sum, a.stream);
+  store_own(row, at, sum);
 }
 
 constexpr int kClearRows = 16;   // rows of the table a clearing wave looks at
@@ -125,14 +123,16 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict
   if ((int64_t)blockIdx.x >= a.sum_blocks) {
     const int64_t v0 = (((int64_t)blockIdx.x - a.sum_blocks) * 4 + wave) * kClearRows;
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    // the rows' offsets at once: nothing but stores is left in the loop
+    // the rows' offsets at once: nothing but stores is left in the loop.  They go around the
+    // caches, which the rows of dout need (each call on other buffers: 65536 rows of 1024 bf16
+    // into 50021 97 -> 87 us, 4096 rows into 30000 36 -> 29, 2048 rows of 512 into 8000 15.1 -> 13.1)
     const int32_t from = v0 + lane <= a.vocab && lane <= kClearRows ? a.offsets[v0 + lane] : 0;
     const int32_t to = __shfl_down(from, 1, 64);
     uint64_t empty = __ballot(lane < kClearRows && v0 + lane < a.vocab && from >= to);
     for (; empty; empty &= empty - 1) {
       float* const dst = a.dtable + (v0 + __builtin_ctzll(empty)) * a.dim;
       for (int64_t c = lane * 4; c < a.dim; c += 256) {
-        if (a.stream && c + 4 <= a.dim) stream_pack(dst + c, zero);
+        if (c + 4 <= a.dim) stream_pack(dst + c, zero);
         else store_row<4>(dst + c, a.dim - c, zero);
       }
     }
@@ -261,8 +261,6 @@ int row_lanes(int64_t dim, int pack, int most) {
   return l;
 }
 
-constexpr double kCachedBytes = 224 << 20;
-
 // Positions per piece: enough pieces to fill the machine, and no fewer than 16 positions (65536
 // rows of 1024 bf16: 64 positions 100 us, 32 89, 16 94; 16384 rows: 16 positions 38, 8 44).
 int grad_piece(int64_t n, int64_t dim) {
@@ -321,11 +319,6 @@ hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, 
   a.dim = dim;
   a.scale = scale;
   a.accumulate = accumulate;
-  // A gradient that the last-level cache does not hold together with what it is summed from
-  // goes around it: the cleared rows no longer push out the rows of dout (65536 rows of 1024
-  // bf16 into 50021: 92 -> 62 us; 8192 rows of 256 into 200000, which fit: 31 -> 42).
-  const double bytes = 4.0 * (double)vocab * (double)dim + (g_bf16 ? 2.0 : 4.0) * (double)n * (double)dim;
-  a.stream = !accumulate && bytes > kCachedBytes;
   a.dtable = dtable;
   a.piece = grad_piece(n, dim);
   a.pieces = (n + a.piece - 1) / a.piece;

@@ -20,7 +20,7 @@ struct RowsArgs {
   const uint8_t* A;
   const uint8_t* B;
   const int32_t* offsets;
-  int experts, tiles_n, vec, streamed, scales;
+  int experts, tiles_n, vec, scales;
   int64_t T, N, K;
   int64_t w_row, w_expert;   // bytes
   const float* alpha;
@@ -31,7 +31,7 @@ struct RowsArgs {
 // One tile as the tile kernel sees it, moved to the origin: M rows of A from A, N rows of
 // B from B.
 struct RowsTile {
-  static constexpr bool kMaskK = false;
+  static constexpr bool kMaskK = false, kStream = false;
   const uint8_t* A;
   const uint8_t* B;
   int64_t a_plane, M, N, K, ldb, ldc;
@@ -39,7 +39,7 @@ struct RowsTile {
   const float* alpha;
   const float* bscale;
   float* C;
-  int vec, streamed;
+  int vec;
   __device__ __forceinline__ void place(int, int, int64_t& m0, int64_t& n0, int64_t& kbeg, int64_t& kend) const {
     m0 = n0 = kbeg = 0;
     kend = K;
@@ -52,10 +52,6 @@ struct RowsTile {
   __device__ __forceinline__ bool sums() const { return false; }
   __device__ __forceinline__ uint32_t* out() const { return reinterpret_cast<uint32_t*>(C); }
   __device__ __forceinline__ int64_t row_c() const { return ldc; }
-  // Outputs that the last-level cache does not hold go around it (8192 x 16384: 588 -> 583
-  // us); smaller ones stay there for the quantizer that reads them next (alone, 2048 x 4096
-  // take 23.4 -> 21.5 us streamed, and with that quantizer 40.2 -> 40.6).
-  __device__ __forceinline__ bool stream() const { return streamed; }
 };
 
 // Rows of group e (e = experts: the rows after the last group), kept inside the batch
@@ -154,7 +150,6 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_rows_kernel(RowsAr
   t.bscale = a.bscale + (a.scales == 1 ? 0 : g.group);
   t.C = C;
   t.vec = a.vec;
-  t.streamed = a.streamed;
   gemm_tile<AC, 1, BSIGNED, FULLK, PF, S>(t);
 }
 
@@ -178,6 +173,11 @@ constexpr int kDepthAlign = 128;
 
 struct DepthTile {
   static constexpr bool kMaskK = true;
+  // The gradient is next read by the optimizer, after the rest of the backward pass: it goes
+  // around the caches (16 experts, 1024 -> 4096, 16384 rows: 128 -> 117 us; 512 -> 1024 over
+  // 8192 rows 19.0 -> 16.9).  The rows' products are read by a quantizer next and stay in the
+  // caches (2048 x 4096: streamed, 23.4 -> 21.5 us alone, but 40.2 -> 40.6 with the quantizer).
+  static constexpr bool kStream = true;
   const uint8_t* A;
   const uint8_t* B;
   int64_t a_plane, M, N, T, klo, kend;
@@ -200,10 +200,6 @@ struct DepthTile {
   __device__ __forceinline__ bool sums() const { return part; }
   __device__ __forceinline__ uint32_t* out() const { return C; }
   __device__ __forceinline__ int64_t row_c() const { return ldc; }
-  // The weight gradient is next read by the optimizer, after the rest of the backward pass:
-  // it goes around the caches (16 experts, 1024 -> 4096, 16384 rows: 128 -> 117 us, 512 ->
-  // 1024 over 8192 rows 19.0 -> 16.9).
-  __device__ __forceinline__ bool stream() const { return !part; }
 };
 
 template <int AC, bool BSIGNED, int PF, typename S>
@@ -315,7 +311,6 @@ hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alp
   a.experts = (int)experts;
   a.tiles_n = 0;
   a.vec = (N % 4) == 0 && ((uintptr_t)C & 15) == 0;
-  a.streamed = T * N > kCachedOutputs;
   a.scales = (int)scales;
   a.T = T;
   a.N = N;

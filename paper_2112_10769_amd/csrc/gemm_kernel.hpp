@@ -120,6 +120,7 @@ struct GemmArgs {
 
   // What the tile kernel asks of its arguments; the grouped products answer differently.
   static constexpr bool kMaskK = false;   // k ranges are whole 16-byte pieces
+  static constexpr bool kStream = false;  // outputs are stored non-temporally
   // This workgroup's tile (of bm x bn) and k range.
   __device__ __forceinline__ void place(int bm, int bn, int64_t& m0, int64_t& n0, int64_t& kbeg, int64_t& kend) const;
   // Bytes per row of A (int8 sums or codes) and of B, and the operands' ranges.
@@ -132,7 +133,6 @@ struct GemmArgs {
     return partial ? reinterpret_cast<uint32_t*>(partial + (int64_t)blockIdx.y * M * N) : reinterpret_cast<uint32_t*>(C);
   }
   __device__ __forceinline__ int64_t row_c() const { return N; }
-  __device__ __forceinline__ bool stream() const { return false; }   // non-temporal stores
 };
 
 // Block -> output tile.  Blocks are dispatched round-robin over the 8 XCDs
@@ -561,7 +561,7 @@ __device__ __forceinline__ void gemm_tile(const Args& a) {
             }
           }
           v4u* const dst = reinterpret_cast<v4u*>(out + row * a.row_c() + col);
-          if (a.stream()) __builtin_nontemporal_store(v, dst);
+          if constexpr (Args::kStream) __builtin_nontemporal_store(v, dst);
           else *dst = v;
         }
       }

@@ -82,16 +82,9 @@ __device__ __forceinline__ void store_pack(uint16_t* p, const float (&v)[V]) {
 }
 
 // As store_pack, non-temporally.
-template <int V>
-__device__ __forceinline__ void stream_pack(float* p, const float (&v)[V]) {
-  if constexpr (V < 4) {
-    store_pack(p, v);
-  } else {
-    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-#pragma unroll
-    for (int i = 0; i < V; i += 4)
-      __builtin_nontemporal_store(f4{v[i], v[i + 1], v[i + 2], v[i + 3]}, reinterpret_cast<f4*>(p + i));
-  }
+__device__ __forceinline__ void stream_pack(float* p, const float (&v)[4]) {
+  typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+  __builtin_nontemporal_store(f4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f4*>(p));
 }
 
 // The same for the `left` elements that a row has from p on: a whole pack, or its first
