@@ -35,7 +35,7 @@ typedef enum { LUQ_I32 = 0, LUQ_I64 = 1 } luq_index;
  *  offsets  out: [groups + 1] int32; group v is order[offsets[v]] ..
  *           order[offsets[v + 1] - 1].  offsets[0] = 0; offsets[groups] is the
  *           number of positions in a group.
- *  n        0 <= n <= 2^30;  groups  1 <= groups <= 2^28.
+ *  n        0 <= n <= 2^28;  groups  1 <= groups <= 2^28.
  *  ws       workspace of luq_workspace_size(LUQ_OP_GROUP_IDS, n, groups).
  *
  * The same result on every call, for any n (no atomics decide an order).  With the
@@ -56,7 +56,7 @@ luq_status luq_group_ids(const void* ids, luq_index it, int64_t n, int64_t group
  *         vocab is a data error and gives a row of NaN.
  *  table  [vocab][dim], type tt;  out  [n][dim], type ot.  The product is rounded
  *         to fp32, and once more to a bf16 out.
- *  n in [0, 2^30], vocab in [0, 2^28], dim in [1, 2^23].  No workspace.
+ *  n and vocab in [0, 2^28], dim in [1, 2^23].  No workspace.
  */
 luq_status luq_embedding_fwd(const void* ids, luq_index it, int64_t n, const void* table, luq_dtype tt,
                              int64_t vocab, int64_t dim, float scale, void* out, luq_dtype ot, void* stream);
@@ -73,7 +73,7 @@ luq_status luq_embedding_fwd(const void* ids, luq_index it, int64_t n, const voi
  *  dtable  [vocab][dim] fp32.  accumulate = 0: written whole, zeros in rows that no
  *          id names; 1: the sums are added to the rows that ids name, and no other row
  *          is touched (further batches of one step, a table shared with another layer).
- *  n in [0, 2^30], vocab in [1, 2^28], dim in [1, 2^23].
+ *  n in [0, 2^28], vocab in [1, 2^28], dim in [1, 2^23].
  *  ws      workspace of luq_workspace_size(LUQ_OP_EMBEDDING_GRAD, n, dim).
  */
 luq_status luq_embedding_grad(const void* dout, luq_dtype gt, const void* ids, luq_index it, const int32_t* order,

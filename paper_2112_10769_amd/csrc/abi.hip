@@ -30,7 +30,7 @@ luq_status hip_status(hipError_t e) {
 
 // Sizes of the operators of luq_lm.h: no tensor in memory is larger, and grids of these
 // stay below 2^32 threads.
-constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxGroups = (int64_t)1 << 28, kMaxCols = (int64_t)1 << 23;
+constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxIds = (int64_t)1 << 28, kMaxCols = (int64_t)1 << 23;
 constexpr int64_t kMaxElements = (int64_t)1 << 38;
 
 // p holds elements of `size` bytes.
@@ -114,10 +114,10 @@ static size_t gemm_workspace(int64_t M, int64_t N, int64_t K) {
 
 // Sizes that luq_group_ids and the row operators take.
 static bool group_sizes(int64_t n, int64_t groups) {
-  return n >= 0 && n <= kMaxRows && groups >= 1 && groups <= kMaxGroups;
+  return n >= 0 && n <= kMaxIds && groups >= 1 && groups <= kMaxIds;
 }
-static bool row_sizes(int64_t rows, int64_t cols) {
-  return rows >= 0 && rows <= kMaxRows && cols >= 1 && cols <= kMaxCols && rows * cols <= kMaxElements;
+static bool row_sizes(int64_t rows, int64_t cols, int64_t most = kMaxRows) {
+  return rows >= 0 && rows <= most && cols >= 1 && cols <= kMaxCols && rows * cols <= kMaxElements;
 }
 
 size_t luq_workspace_size(int op, int64_t d0, int64_t d1, int64_t d2) {
@@ -143,7 +143,7 @@ size_t luq_workspace_size(int op, int64_t d0, int64_t d1, int64_t d2) {
     case LUQ_OP_GROUP_IDS:
       return group_sizes(d0, d1) ? luq::group_ids_workspace_bytes(d0, d1) : 0;
     case LUQ_OP_EMBEDDING_GRAD:
-      return row_sizes(d0, d1) ? luq::embedding_grad_workspace_bytes(d0, d1) : 0;
+      return row_sizes(d0, d1, kMaxIds) ? luq::embedding_grad_workspace_bytes(d0, d1) : 0;
     case LUQ_OP_LAYERNORM_BWD:
       return row_sizes(d0, d1) ? luq::layernorm_bwd_workspace_bytes(d0, d1) : 0;
     default:
@@ -463,7 +463,7 @@ luq_status luq_group_ids(const void* ids, luq_index it, int64_t n, int64_t group
   g_last_error[0] = 0;
   luq_status st = check_index(fn, it);
   if (st != LUQ_OK) return st;
-  if (!group_sizes(n, groups)) return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30] and groups in [1, 2^28]", fn);
+  if (!group_sizes(n, groups)) return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^28] and groups in [1, 2^28]", fn);
   if (!offsets || (n > 0 && (!ids || !order))) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
   if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned4(order) || !aligned4(offsets))
     return fail(LUQ_ERR_ALIGN, "%s: ids, order or offsets misaligned", fn);
@@ -480,8 +480,8 @@ luq_status luq_embedding_fwd(const void* ids, luq_index it, int64_t n, const voi
   luq_status st = check_index(fn, it);
   if (st == LUQ_OK) st = check_types(fn, tt, ot);
   if (st != LUQ_OK) return st;
-  if (!row_sizes(n, dim) || vocab < 0 || vocab > kMaxGroups || vocab * dim > kMaxElements)
-    return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30], vocab in [0, 2^28], dim in [1, 2^23]", fn);
+  if (!row_sizes(n, dim, kMaxIds) || vocab < 0 || vocab > kMaxIds || vocab * dim > kMaxElements)
+    return fail(LUQ_ERR_SHAPE, "%s: n and vocab in [0, 2^28], dim in [1, 2^23]", fn);
   if (n == 0) return LUQ_OK;
   if (!ids || !out || (vocab > 0 && !table)) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
   if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned_to(table, elem_size(tt)) || !aligned_to(out, elem_size(ot)))
@@ -498,8 +498,8 @@ luq_status luq_embedding_grad(const void* dout, luq_dtype gt, const void* ids, l
   luq_status st = check_index(fn, it);
   if (st == LUQ_OK) st = check_types(fn, gt, gt);
   if (st != LUQ_OK) return st;
-  if (!row_sizes(n, dim) || vocab < 1 || vocab > kMaxGroups || vocab * dim > kMaxElements)
-    return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^30], vocab in [1, 2^28], dim in [1, 2^23]", fn);
+  if (!row_sizes(n, dim, kMaxIds) || vocab < 1 || vocab > kMaxIds || vocab * dim > kMaxElements)
+    return fail(LUQ_ERR_SHAPE, "%s: n in [0, 2^28], vocab in [1, 2^28], dim in [1, 2^23]", fn);
   if (accumulate != 0 && accumulate != 1) return fail(LUQ_ERR_PARAM, "%s: accumulate must be 0 or 1", fn);
   if (!offsets || !dtable || (n > 0 && (!dout || !ids || !order))) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
   if (!aligned_to(ids, it == LUQ_I64 ? 8 : 4) || !aligned_to(dout, elem_size(gt)) || !aligned4(order) ||

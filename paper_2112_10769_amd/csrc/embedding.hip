@@ -5,6 +5,7 @@
 // Both are bound by memory: the lookup reads and writes a row per id, the gradient reads a
 // row per id and writes the table once.  The gradient takes the positions grouped by id
 // (group_ids.hip), so that every row of the table has one writer and its sum one order.
+#include <algorithm>
 #include <type_traits>
 
 #include "luq_launch.hpp"
@@ -83,6 +84,7 @@ struct GradArgs {
   int64_t pieces;
   int slabs;           // slabs of 64 V columns
   int64_t sum_blocks;  // blocks that sum; those after them clear the rows of ids that do not occur
+  int clear_rows;      // rows of the table that a clearing wave looks at, at most 16
 };
 
 // The elements of a pack that are its own.
@@ -113,22 +115,20 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int64_t id, const P
   store_own(row, at, sum);
 }
 
-constexpr int kClearRows = 16;   // rows of the table a clearing wave looks at
-
 template <typename ID, typename GT, int V>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const GT* __restrict__ dout, const ID* __restrict__ ids,
                                                             GradArgs a) {
   constexpr int U = V * sizeof(GT) >= 16 ? 8 : 16;   // rows of a batch
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int64_t)blockIdx.x >= a.sum_blocks) {
-    const int64_t v0 = (((int64_t)blockIdx.x - a.sum_blocks) * 4 + wave) * kClearRows;
+    const int64_t v0 = (((int64_t)blockIdx.x - a.sum_blocks) * 4 + wave) * a.clear_rows;
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     // the rows' offsets at once: nothing but stores is left in the loop.  They go around the
     // caches, which the rows of dout need (each call on other buffers: 65536 rows of 1024 bf16
     // into 50021 97 -> 87 us, 4096 rows into 30000 36 -> 29, 2048 rows of 512 into 8000 15.1 -> 13.1)
-    const int32_t from = v0 + lane <= a.vocab && lane <= kClearRows ? a.offsets[v0 + lane] : 0;
+    const int32_t from = v0 + lane <= a.vocab && lane <= a.clear_rows ? a.offsets[v0 + lane] : 0;
     const int32_t to = __shfl_down(from, 1, 64);
-    uint64_t empty = __ballot(lane < kClearRows && v0 + lane < a.vocab && from >= to);
+    uint64_t empty = __ballot(lane < a.clear_rows && v0 + lane < a.vocab && from >= to);
     for (; empty; empty &= empty - 1) {
       float* const dst = a.dtable + (v0 + __builtin_ctzll(empty)) * a.dim;
       for (int64_t c = lane * 4; c < a.dim; c += 256) {
@@ -331,7 +331,9 @@ hipError_t launch_embedding_grad(const void* dout, int g_bf16, const void* ids, 
       constexpr int V = decltype(pack)::value;
       a.slabs = (int)((dim + 64 * V - 1) / (64 * V));
       a.sum_blocks = (a.pieces * a.slabs + 3) / 4;
-      const int64_t clear = accumulate ? 0 : (vocab + 4 * kClearRows - 1) / (4 * kClearRows);
+      // 32 KB a wave, or a row (16 rows of 7136: 28 us for 381 rows of the table)
+      a.clear_rows = dim < 8192 ? (int)std::min<int64_t>(16, 8192 / dim) : 1;
+      const int64_t clear = accumulate ? 0 : (vocab + 4 * a.clear_rows - 1) / (4 * a.clear_rows);
       if (a.sum_blocks + clear > 0)
         hipLaunchKernelGGL((embedding_sum_kernel<ID, GT, V>), dim3((unsigned)(a.sum_blocks + clear)), dim3(256), 0, st,
                            static_cast<const GT*>(dout), static_cast<const ID*>(ids), a);

@@ -78,6 +78,20 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortPass a, 
   __shared__ uint32_t scratch[kSortWaves];
   __shared__ uint32_t totals[kSortThreads], befores[kSortThreads];
   const int bins = 1 << a.bits, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int64_t lo = (int64_t)blockIdx.x * a.per, hi = min(lo + a.per, a.n);
+  // wave w ranks the keys [w * 64 * kItems, ...) of a piece, 64 at a time; the next piece's
+  // are read ahead, the first one's while the histograms come
+  uint32_t next_key[kItems];
+  int32_t next_pos[kItems];
+  auto fetch = [&](int64_t piece) {
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int64_t i = piece + (wave * kItems + k) * kWave + lane;
+      next_key[k] = i < hi ? load_key<SRC>(a, i) : 0;
+      next_pos[k] = i < hi && a.pos ? a.pos[i] : (int32_t)i;
+    }
+  };
+  fetch(lo);
   // where this block's keys of digit d begin: all smaller digits, then the blocks before
   // (the block's threads share the blocks of a digit, 16 histograms in flight each)
   const int d0 = threadIdx.x, shares = kSortThreads >> a.bits, share = threadIdx.x >> a.bits;
@@ -103,19 +117,23 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortPass a, 
     }
   const uint32_t smaller = block_prefix(total, scratch);
   if (d0 < bins) base[d0] = smaller + before;
-  const int64_t lo = (int64_t)blockIdx.x * a.per, hi = min(lo + a.per, a.n);
   for (int64_t piece = lo; piece < hi; piece += kPiece) {
     for (int w = 0; w < kSortWaves; ++w)
       if (d0 < bins) count[w][d0] = 0;
     __syncthreads();
-    // wave w ranks the keys [w * 64 * kItems, ...) of the piece, 64 at a time
     uint32_t key[kItems], rank[kItems];
+    int32_t pos[kItems];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      key[k] = next_key[k];
+      pos[k] = next_pos[k];
+    }
+    if (piece + kPiece < hi) fetch(piece + kPiece);
     volatile uint32_t* mine = count[wave];
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
       const int64_t i = piece + (wave * kItems + k) * kWave + lane;
       const bool in = i < hi;
-      key[k] = in ? load_key<SRC>(a, i) : 0;
       const uint32_t d = (key[k] >> a.shift) & (bins - 1);
       uint64_t same = __ballot(in);
       for (int bit = 0; bit < a.bits; ++bit) {
@@ -145,7 +163,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortPass a, 
       if (i < hi) {
         const uint32_t at = count[wave][(key[k] >> a.shift) & (bins - 1)] + rank[k];
         out_keys[at] = key[k];
-        out_pos[at] = a.pos ? a.pos[i] : (int32_t)i;
+        out_pos[at] = pos[k];
       }
     }
     __syncthreads();
@@ -170,17 +188,26 @@ __device__ __forceinline__ void fill_offsets(bool first, int64_t prev, int64_t k
   }
 }
 
-// The offsets from the sorted keys: thread p fills those between its key and the one
-// before; one past the end those after the last key.
-__global__ __launch_bounds__(256) void group_offsets_kernel(const uint32_t* __restrict__ keys, int64_t n, int64_t groups,
+// The offsets from the sorted keys: a block takes 64 of them into LDS, and its 256 threads
+// fill the offsets from the key before its first up to its last, each by bisection (few keys
+// a block: rare ids lie far apart).  One key past the end is `groups`.
+constexpr int kOffsetKeys = 64;
+
+__global__ __launch_bounds__(256) void group_offsets_kernel(const uint32_t* __restrict__ keys, int64_t n, uint32_t groups,
                                                             int32_t* offsets) {
-  const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  int64_t prev = -1, key = -1;
-  if (p <= n) {
-    prev = p > 0 ? (int64_t)keys[p - 1] : -1;
-    key = p < n ? (int64_t)keys[p] : groups;
+  __shared__ uint32_t k[kOffsetKeys];
+  const int64_t p0 = (int64_t)blockIdx.x * kOffsetKeys, p = p0 + threadIdx.x;
+  if (threadIdx.x < kOffsetKeys) k[threadIdx.x] = p < n ? keys[p] : groups;
+  const int64_t prev = p0 > 0 ? (int64_t)keys[p0 - 1] : -1;
+  __syncthreads();
+  const int64_t last = k[kOffsetKeys - 1];
+  for (int64_t v = prev + 1 + threadIdx.x; v <= last; v += 256) {
+    int at = 0;   // keys below v; the last is not
+#pragma unroll
+    for (int d = kOffsetKeys / 2; d >= 1; d >>= 1)
+      if (k[at + d - 1] < (uint32_t)v) at += d;
+    offsets[v] = (int32_t)(p0 + at);
   }
-  fill_offsets(prev < key, prev, key, (int32_t)p, offsets);
 }
 
 // Few ids: a block ranks 16 positions, each by 64 threads that compare it with a 64th of
@@ -300,8 +327,8 @@ hipError_t launch_group_ids(const void* ids, int i64, int64_t n, int64_t groups,
       sorted = keys;
     }
   }
-  hipLaunchKernelGGL(group_offsets_kernel, dim3((unsigned)(n / 256 + 1)), dim3(256), 0, st, sorted, n, groups,
-                     offsets);
+  hipLaunchKernelGGL(group_offsets_kernel, dim3((unsigned)(n / kOffsetKeys + 1)), dim3(256), 0, st, sorted, n,
+                     (uint32_t)groups, offsets);
   return hipGetLastError();
 }
 
