@@ -3,7 +3,7 @@
  * serving steps around the 4-bit products of luq.h.
  *
  * The paper keeps the first layer and the normalisations in high precision
- * (Section 6, experimental details); these are the embedding lookup and layer
+ * (Appendix A.4); these are the embedding lookup and layer
  * norm below.  Layers of experts take the 4-bit products of Eqs. forward,
  * backward and update on rows grouped by expert, in groups of any sizes.
  *

@@ -155,6 +155,31 @@ def test_accumulate(L, dim):
     U.within(got[named], ref[named] + 0.5, bound[named] + U.U * (np.abs(ref[named]) + 0.5 + bound[named]), dim)
 
 
+@pytest.mark.parametrize("dim", [1, 3, 70, 600])
+def test_gradient_of_no_ids(L, dim):
+    """Zeros are written, or with accumulate nothing is."""
+    ids = torch.empty(0, dtype=torch.int64, device="cuda")
+    announce("embedding_grad no ids", dim)
+    order, offsets = L.luq_group_ids(ids, 33)
+    table = torch.full((33, dim), 2.0, device="cuda")
+    dout = torch.empty(0, dim, device="cuda")
+    L.luq_embedding_grad(dout, ids, order, offsets, 1.0, accumulate=True, dtable=table)
+    assert (table == 2).all()
+    assert (L.luq_embedding_grad(dout, ids, order, offsets, 1.0, dtable=table) == 0).all()
+
+
+@pytest.mark.parametrize("vocab,dim", [(381, 7136), (5, 40000), (70000, 3)])
+def test_tables_of_extreme_shape(L, vocab, dim):
+    n = 189
+    rng = np.random.default_rng(vocab)
+    ids = _ids("padded", n, vocab, rng)
+    dout = _tensor((n, dim), torch.bfloat16, 6)
+    announce("embedding_grad shape", vocab, dim)
+    got = _grad(L, ids, vocab, dout, 1.0, dtable=torch.full((vocab, dim), float("nan"), device="cuda"))
+    ref, bound = U.embedding_grad(host(dout.float()), ids, vocab, 1.0)
+    U.within(host(got), ref, bound, (vocab, dim))
+
+
 def test_gradient_values(L):
     """A NaN or infinity reaches its own row only, and none of a padded position does; zeros are written
     over whatever the buffer held."""

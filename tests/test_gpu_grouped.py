@@ -298,6 +298,22 @@ def test_experts_beyond_32_bits(L):
     torch.cuda.empty_cache()
 
 
+def test_decreasing_offsets_stay_inside(L):
+    """Offsets that are no groups give some result inside the output, and no access outside it."""
+    announce("grouped decreasing offsets")
+    rng = np.random.default_rng(9)
+    codes, a, scale, w, w_scale = _rows_case(rng, [20] * 8, 0, 50, 64, "int4s", True, True)
+    flat = torch.full((160 * 50 + 64,), 7.0, device="cuda")
+    y = flat[32:32 + 160 * 50].view(160, 50)
+    offsets = to_dev(np.int32([0, 160, 0, 160, -5, 160, 3, 1 << 30, 0]))
+    L.int4_gemm_fwd_grouped(to_dev(codes), _dev(scale), True, to_dev(U.pack(w)), _dev(w_scale), True, offsets, 160, 50, 64, y=y)
+    dw = torch.zeros(8, 6, 10, device="cuda")
+    L.luq_gemm_wgrad_grouped(to_dev(U.luq_pack(U.luq_fields(rng, (6, 160)))), _dev(1.0),
+                             to_dev(U.pack(U.int4_values(rng, (10, 160), True))), _dev(1.0), True, offsets, 160, 6, 10, dw=dw)
+    torch.cuda.synchronize()
+    assert (flat[:32] == 7).all() and (flat[32 + 160 * 50:] == 7).all()
+
+
 def test_offsets_are_kept_inside(L):
     """Offsets beyond the batch are taken as its end."""
     announce("grouped offsets past the end")
