@@ -178,13 +178,15 @@ struct DepthArgs {
 // as the stages of an ungrouped product are: the codes before the group are cleared.
 constexpr int kDepthAlign = 128;
 
+// STREAM: the gradient is next read by the optimizer, after the rest of the backward pass, and
+// goes around the caches (16 experts, 1024 -> 4096, 16384 rows: 128 -> 117 us; 512 -> 1024
+// over 8192 rows 19.0 -> 16.9) where its rows are whole 128-byte lines: parts of a line must
+// meet in L2 (17 experts, 2744 -> 3648 over 96 rows: 251 us streamed, 152 not).  The rows'
+// products are read by a quantizer next and stay in the caches (2048 x 4096: streamed, 23.4 ->
+// 21.5 us alone, but 40.2 -> 40.6 with the quantizer).
+template <bool STREAM>
 struct DepthTile {
-  static constexpr bool kMaskK = true;
-  // The gradient is next read by the optimizer, after the rest of the backward pass: it goes
-  // around the caches (16 experts, 1024 -> 4096, 16384 rows: 128 -> 117 us; 512 -> 1024 over
-  // 8192 rows 19.0 -> 16.9).  The rows' products are read by a quantizer next and stay in the
-  // caches (2048 x 4096: streamed, 23.4 -> 21.5 us alone, but 40.2 -> 40.6 with the quantizer).
-  static constexpr bool kStream = true;
+  static constexpr bool kMaskK = true, kStream = STREAM;
   const uint8_t* A;
   const uint8_t* B;
   int64_t a_plane, M, N, T, klo, kend;
@@ -209,7 +211,7 @@ struct DepthTile {
   __device__ __forceinline__ int64_t row_c() const { return ldc; }
 };
 
-template <int AC, bool BSIGNED, int PF, typename S>
+template <int AC, bool BSIGNED, int PF, typename S, bool STREAM>
 __global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_depth_kernel(DepthArgs a) {
   // Groups differ in length, so each of the 8 XCDs takes an eighth of every group's tiles (a
   // run of whole groups for each left XCDs waiting for the one with the longest)
@@ -230,7 +232,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_depth_kernel(Depth
     hi = min(hi, from + chunk);
     lo = min(max(lo, from), hi);
   }
-  DepthTile t;
+  DepthTile<STREAM> t;
   t.A = a.A + m0 * (AC == kAcSum2 ? a.T : a.T >> 1);
   t.B = a.B + n0 * (a.T >> 1);
   t.a_plane = 0;
@@ -284,8 +286,11 @@ void launch_depth_tile(DepthArgs a, hipStream_t st) {
   a.tiles_m = (int)((a.M + S::BM - 1) / S::BM);
   a.tiles_n = (int)((a.N + S::BN - 1) / S::BN);
   const dim3 grid((unsigned)(((int64_t)a.tiles_m * a.tiles_n + 7) / 8 * 8 * a.experts), (unsigned)a.splits);
-  hipLaunchKernelGGL((grouped_depth_kernel<AC, BSIGNED, prefetch_depth<S, AC, 1, BSIGNED, true>(), S>), grid,
-                     dim3(S::THREADS), 0, st, a);
+  constexpr int kPf = prefetch_depth<S, AC, 1, BSIGNED, true>();
+  if (!a.partial && a.N % 32 == 0 && ((uintptr_t)a.C & 127) == 0)
+    hipLaunchKernelGGL((grouped_depth_kernel<AC, BSIGNED, kPf, S, true>), grid, dim3(S::THREADS), 0, st, a);
+  else
+    hipLaunchKernelGGL((grouped_depth_kernel<AC, BSIGNED, kPf, S, false>), grid, dim3(S::THREADS), 0, st, a);
 }
 
 template <int AC, bool BSIGNED>
