@@ -187,6 +187,11 @@ struct BwdArgs {
   const float* gamma;
   int64_t rows, cols;
   float* partial;   // [workgroups][2][cols]: each workgroup's sums for dgamma and dbeta
+  float* dgamma;    // where a single workgroup's sums go instead; either may be null
+  float* dbeta;
+  __device__ __forceinline__ float* sums(int64_t group, int64_t groups, int which) const {
+    return groups == 1 ? (which ? dbeta : dgamma) : partial + (2 * group + which) * cols;
+  }
 };
 
 template <typename G, typename T, int TPR, int CH>
@@ -245,13 +250,14 @@ __global__ __launch_bounds__(kThreads<TPR>) void layernorm_bwd_kernel(const G* d
       if (col.at[i].any()) store_pack(dx + row * cols + col.at[i].begin, v);
     }
   }
-  float* const mine = a.partial + (int64_t)blockIdx.x * 2 * cols;
   if constexpr (TPR > kWave) {
+    float* const sum_g = a.sums(blockIdx.x, gridDim.x, 0);
+    float* const sum_b = a.sums(blockIdx.x, gridDim.x, 1);
 #pragma unroll
     for (int i = 0; i < CH; ++i)
       if (col.at[i].any()) {
-        store_pack(mine + col.at[i].begin, dg[i]);
-        store_pack(mine + cols + col.at[i].begin, db[i]);
+        if (sum_g) store_pack(sum_g + col.at[i].begin, dg[i]);
+        if (sum_b) store_pack(sum_b + col.at[i].begin, db[i]);
       }
   } else {
     // the waves' sums meet in LDS
@@ -264,12 +270,14 @@ __global__ __launch_bounds__(kThreads<TPR>) void layernorm_bwd_kernel(const G* d
       for (int i = 0; i < CH; ++i)
         if (col.at[i].any()) store_pack(&part[wave][col.at[i].begin], which ? db[i] : dg[i]);
       __syncthreads();
-      for (int64_t c = threadIdx.x; c < cols; c += 256) {
-        float s = 0.0f;
+      float* const mine = a.sums(blockIdx.x, gridDim.x, which);
+      if (mine)
+        for (int64_t c = threadIdx.x; c < cols; c += 256) {
+          float s = 0.0f;
 #pragma unroll
-        for (int w = 0; w < R; ++w) s += part[w][c];
-        mine[which * cols + c] = s;
-      }
+          for (int w = 0; w < R; ++w) s += part[w][c];
+          mine[c] = s;
+        }
     }
   }
 }
@@ -358,12 +366,13 @@ __global__ __launch_bounds__(256) void layernorm_slab_kernel(const G* dy, const 
       }
     }
   }
-  float* const mine = a.partial + (int64_t)blockIdx.y * 2 * cols + at.begin;
+  float* const sum_g = a.sums(blockIdx.y, gridDim.y, 0);
+  float* const sum_b = a.sums(blockIdx.y, gridDim.y, 1);
 #pragma unroll
   for (int k = 0; k < V; ++k)
     if (at.own(k)) {
-      mine[k] = dg[k];
-      mine[cols + k] = db[k];
+      if (sum_g) sum_g[at.begin + k] = dg[k];
+      if (sum_b) sum_b[at.begin + k] = db[k];
     }
 }
 
@@ -448,9 +457,15 @@ constexpr int64_t kMostCols = kBwdThreads * kElements;   // of the backward in r
 // columns (8192 x 8192 bf16: 79 to 87 us with one, 79 to 93 with more), two below (16384 x
 // 4096: 101 with one, 80 with two, 95 with four), and for rows of a wave up to four, but
 // three rows a wave at least (65536 x 512: 60, 42, 40 with one, two, four; 3001 x 1024:
-// 13.7, 15.6, 18.1).
+// 13.7, 15.6, 18.1).  A single workgroup writes the gradients itself, without the second
+// launch, and takes 4 rows (2 x 8000 bf16: 12.0 to 9.1 us a call; 4 x 4096 12.5 to
+// 9.5; 8 x 8192 12.0 to 14.4) or, of the form that reads twice, 8 (8 x 100000: 30 to 18).
 int64_t bwd_groups(int64_t rows, int64_t cols) {
-  if (cols < 8 || cols > kMostCols) return rows < 128 ? rows : 128;
+  if (cols < 8 || cols > kMostCols) {
+    if (rows > 0 && rows <= 8) return 1;
+    return rows < 128 ? rows : 128;
+  }
+  if (rows > 0 && rows <= 4) return 1;
   if (cols <= 64 * kElements) {
     const int64_t need = (rows + 11) / 12;
     return need < 4 * kCuCount ? need : 4 * kCuCount;
@@ -497,7 +512,7 @@ size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols) {
 hipError_t launch_layernorm_bwd(const void* dy, int g_bf16, const void* x, int bf16, const float* mean,
                                 const float* rstd, const float* gamma, int64_t rows, int64_t cols, void* dx,
                                 float* dgamma, float* dbeta, void* ws, hipStream_t st) {
-  const BwdArgs a{mean, rstd, gamma, rows, cols, static_cast<float*>(ws)};
+  const BwdArgs a{mean, rstd, gamma, rows, cols, static_cast<float*>(ws), dgamma, dbeta};
   const int64_t groups = bwd_groups(rows, cols);
   auto launch = [&](auto grad, auto elem) {
     using G = decltype(grad);
@@ -528,7 +543,7 @@ hipError_t launch_layernorm_bwd(const void* dy, int g_bf16, const void* x, int b
     if (g_bf16) bf16 ? launch(uint16_t{}, uint16_t{}) : launch(uint16_t{}, float{});
     else bf16 ? launch(float{}, uint16_t{}) : launch(float{}, float{});
   }
-  if (dgamma || dbeta)
+  if ((dgamma || dbeta) && groups != 1)
     hipLaunchKernelGGL(layernorm_weight_kernel, dim3((unsigned)((cols + kWave - 1) / kWave), 2), dim3(1024), 0, st,
                        a.partial, groups, cols, dgamma, dbeta);
   return hipGetLastError();

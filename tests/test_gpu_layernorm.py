@@ -80,6 +80,31 @@ def test_many_rows(L, rows, cols):
         U.within(host(g), r, b, (rows, cols, name))
 
 
+@pytest.mark.parametrize("rows", [1, 3, 4, 5, 8, 9, 12, 13, 40])
+@pytest.mark.parametrize("cols", [5, 700, 3000, 12000])
+def test_few_rows(L, rows, cols):
+    """One workgroup's sums are the gradients; outputs that are not asked for are left alone."""
+    x, gamma, beta, dy = _inputs(rows, cols, "bf16", "f32")
+    _, mean, rstd = L.luq_layernorm_fwd(x, gamma, beta)
+    announce("layernorm_bwd few rows", rows, cols)
+    ref, bound = U.layernorm_grad(host(dy), host(x.float()), host(mean), host(rstd), host(gamma), False)
+    full = torch.full((2, cols + 4), float("nan"), device="cuda")
+    got = L.luq_layernorm_bwd(dy, x, mean, rstd, gamma, dgamma=full[0, :cols], dbeta=full[1, :cols])
+    for g, r, b in zip(got, ref, bound):
+        U.within(host(g), r, b, (rows, cols))
+    assert torch.isnan(full[:, cols:]).all()
+    ws = torch.empty(L.workspace_size(L.OP_LAYERNORM_BWD, rows, cols), dtype=torch.uint8, device="cuda")
+    dx, db = torch.empty_like(dy), torch.empty(cols, device="cuda")
+    p = lambda t: t.data_ptr()  # noqa: E731
+    for dgamma, dbeta in ((None, p(db)), (p(db), None), (None, None)):
+        db.fill_(float("nan"))
+        st = L.LIB.luq_layernorm_bwd(p(dy), 0, p(x), 1, p(mean), p(rstd), p(gamma), rows, cols, p(dx), dgamma, dbeta, p(ws),
+                                     ws.numel(), torch.cuda.current_stream().cuda_stream)
+        assert st == 0 and torch.equal(dx, got[0])
+        if dbeta or dgamma:
+            assert torch.equal(db, got[2] if dbeta else got[1])
+
+
 def test_without_weight_and_bias(L):
     x, gamma, beta, dy = _inputs(9, 300, "f32")
     for g, b in ((None, None), (gamma, None), (None, beta)):
