@@ -264,11 +264,15 @@ int row_lanes(int64_t dim, int pack, int most) {
 }
 
 // Positions per piece: enough pieces to fill the machine, and no fewer than 16 positions (65536
-// rows of 1024 bf16: 64 positions 100 us, 32 89, 16 94; 16384 rows: 16 positions 38, 8 44).
+// rows of 1024 bf16: 64 positions 100 us, 32 89, 16 94; 16384 rows: 16 positions 38, 8 44), or 8
+// where 16 leave most of it idle and a piece's chain of loads and stores is what the launch
+// waits for (4000 rows of 2048 fp32: 16 positions 28.3 us, 8 26.2, 4 30.8; 300 of 4096: 24.6,
+// 22.2, 22.6; 8000 of 512 24.4, 23.1; but 30000 of 256 33.8, 34.6).
 int grad_piece(int64_t n, int64_t dim) {
   const int64_t waves_per_piece = (dim + 255) / 256;
   int piece = 64;
   while (piece > 16 && n / piece * waves_per_piece < 8192) piece /= 2;
+  if (piece == 16 && n < 16384 && n / 16 * waves_per_piece < 2048) piece = 8;
   return piece;
 }
 
