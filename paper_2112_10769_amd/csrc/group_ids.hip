@@ -192,17 +192,72 @@ __device__ __forceinline__ void fill_offsets(bool first, int64_t prev, int64_t k
 
 // The offsets from the sorted keys: a block takes 64 of them into LDS, and its 256 threads
 // fill the offsets from the key before its first up to its last, each by bisection (few keys
-// a block: rare ids lie far apart).  One key past the end is `groups`.
-constexpr int kOffsetKeys = 64;
+// a block: rare ids lie far apart).  One key past the end is `groups`.  Where these offsets are
+// more than kWideOffsets, the first blocks fill them instead: a wave for every kSpread ids
+// finds where its ids' keys are (the whole sort with one block for each wide range, and so:
+// 65536 ids of 50021, most of them small, 52 and 27 us; all alike 39 and 26; of 2^20 442 and
+// 33; evenly spread 23 both).
+constexpr int kOffsetKeys = 64, kWideOffsets = 4096, kSpread = 1024;
+static_assert(kOffsetKeys == kWave && kSpread < kWideOffsets, "see spread_offsets");
+
+// Offsets of the ids [v0, v0 + kSpread) among those of wide ranges.  There are two such ranges
+// at most, those of the first and the last id, as any other lies between these.
+__device__ __forceinline__ void spread_offsets(const uint32_t* __restrict__ keys, int64_t n, uint32_t groups, int64_t v0,
+                                               int32_t* offsets) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t v1 = min(v0 + kSpread - 1, (int64_t)groups);
+  // keys below v0 and below v1, by probes of 64 keys each
+  int64_t at[2] = {0, 0}, left[2] = {n, n};
+  while (left[0] > 0 || left[1] > 0) {
+    uint32_t key[2];
+    int64_t step[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      step[i] = (left[i] + kWave - 1) / kWave;
+      const int64_t p = (lane + 1) * step[i] - 1;
+      key[i] = p >= 0 && p < left[i] ? keys[at[i] + p] : 0xFFFFFFFFu;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t below = __popcll(__ballot((int64_t)key[i] < (i ? v1 : v0))) * step[i];
+      at[i] += below;
+      left[i] = max((int64_t)0, min(step[i] - 1, left[i] - below));
+    }
+  }
+  int64_t done = -1;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t p0 = at[i] / kOffsetKeys * kOffsetKeys;
+    if (p0 == done) break;
+    done = p0;
+    const uint32_t key = p0 + lane < n ? keys[p0 + lane] : groups;
+    const int64_t prev = p0 > 0 ? (int64_t)keys[p0 - 1] : -1, last = (uint32_t)__shfl((int)key, kOffsetKeys - 1, kWave);
+    if (last - prev <= kWideOffsets) continue;
+    const int64_t end = min(last, v1);
+    for (int64_t v = max(prev + 1, v0); v <= end; v += kWave) {
+      int below = 0;   // of the keys; the last is not
+#pragma unroll
+      for (int d = kOffsetKeys / 2; d >= 1; d >>= 1)
+        if ((int64_t)(uint32_t)__shfl((int)key, below + d - 1, kWave) < v + lane) below += d;
+      if (v + lane <= end) offsets[v + lane] = (int32_t)(p0 + below);
+    }
+  }
+}
 
 __global__ __launch_bounds__(256) void group_offsets_kernel(const uint32_t* __restrict__ keys, int64_t n, uint32_t groups,
-                                                            int32_t* offsets) {
+                                                            int32_t* offsets, int spread_blocks) {
+  if ((int)blockIdx.x < spread_blocks) {
+    const int64_t v0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * kSpread;
+    if (v0 <= (int64_t)groups) spread_offsets(keys, n, groups, v0, offsets);
+    return;
+  }
   __shared__ uint32_t k[kOffsetKeys];
-  const int64_t p0 = (int64_t)blockIdx.x * kOffsetKeys, p = p0 + threadIdx.x;
+  const int64_t p0 = ((int64_t)blockIdx.x - spread_blocks) * kOffsetKeys, p = p0 + threadIdx.x;
   if (threadIdx.x < kOffsetKeys) k[threadIdx.x] = p < n ? keys[p] : groups;
   const int64_t prev = p0 > 0 ? (int64_t)keys[p0 - 1] : -1;
   __syncthreads();
   const int64_t last = k[kOffsetKeys - 1];
+  if (last - prev > kWideOffsets) return;
   for (int64_t v = prev + 1 + threadIdx.x; v <= last; v += 256) {
     int at = 0;   // keys below v; the last is not
 #pragma unroll
@@ -329,8 +384,10 @@ hipError_t launch_group_ids(const void* ids, int i64, int64_t n, int64_t groups,
       sorted = keys;
     }
   }
-  hipLaunchKernelGGL(group_offsets_kernel, dim3((unsigned)(n / kOffsetKeys + 1)), dim3(256), 0, st, sorted, n,
-                     (uint32_t)groups, offsets);
+  // no range is wide if all ids together are not
+  const int spread = groups + 1 > kWideOffsets ? (int)(groups / (4 * kSpread) + 1) : 0;
+  hipLaunchKernelGGL(group_offsets_kernel, dim3((unsigned)(spread + n / kOffsetKeys + 1)), dim3(256), 0, st, sorted, n,
+                     (uint32_t)groups, offsets, spread);
   return hipGetLastError();
 }
 

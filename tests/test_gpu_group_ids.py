@@ -48,6 +48,20 @@ def test_distributions(L, kind):
     _check(L, ids, groups, what=kind)
 
 
+@pytest.mark.parametrize("groups", [4095, 4096, 4097, 262143, 300007, (1 << 21) + 5])
+@pytest.mark.parametrize("n", [1, 300, 8192, 8193, 20001])
+def test_gaps(L, n, groups):
+    """Ids in few places, with wide stretches of the table between, before and after them."""
+    rng = np.random.default_rng(n + groups)
+    for places in (1, 2, 5, 70):
+        at = rng.integers(0, groups, places)
+        for width in (1, 3, 900, 5000):
+            ids = np.clip(at[rng.integers(0, places, n)] + rng.integers(0, width, n), -1, groups)
+            _check(L, ids, groups, np.int32, (places, width))
+    for first, step in ((0, groups // 64), (groups - 1, 0), (groups, 0), (0, 0)):
+        _check(L, np.minimum(first + step * np.arange(n), groups), groups, np.int64, (first, step))
+
+
 def test_extreme_ids(L):
     big = np.array([2 ** 62, -2 ** 62, 2 ** 32, 2 ** 32 + 3, 3, -1, 2 ** 31, 7, 3, 8, 0], dtype=np.int64)
     _check(L, big, 8)
