@@ -10,7 +10,7 @@
 //
 // Ids outside [0, groups) get the key `groups`, which sorts last.
 //
-// Bound by latency: 509 ids take 4.2 us, 65536 of 50021 25 us in five launches of 4 to 6.
+// Bound by latency: 509 ids take 3.5 us, 65536 of 50021 25 us in five launches of 4 to 6.
 #include "luq_device.hpp"
 #include "luq_launch.hpp"
 
