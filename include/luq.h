@@ -135,7 +135,8 @@ size_t luq_workspace_size(int op, int64_t d0, int64_t d1, int64_t d2);
  * the device and in stream order, whether its maximum was finite.
  *
  *  ws      the workspace passed to that call (device memory, 16-byte
- *          aligned).
+ *          aligned, of the size that luq_workspace_size answers for a tensor
+ *          that is not empty: the status word is its last).
  *  stream  the stream the call was enqueued on: the word is copied to the
  *          host after it and the stream is synchronized (so this call may
  *          not be captured into a HIP graph).
@@ -145,8 +146,9 @@ size_t luq_workspace_size(int op, int64_t d0, int64_t d1, int64_t d2);
  * estimate), LUQ_ERR_NULL / LUQ_ERR_ALIGN for a bad ws, LUQ_ERR_HIP if the
  * copy fails, or LUQ_ERR_WORKSPACE if ws holds no quantizer status (no
  * quantizer has written it, or another operation reused it since).  An
- * int4_quantize call with clip > 0 takes no maximum and writes LUQ_OK when
- * it is given a workspace (none otherwise).
+ * int4_quantize call with clip > 0 takes no maximum, and an empty tensor has a
+ * finite one, 0: such calls write the status when they are given a workspace of
+ * the size above, and nothing into a smaller one.
  */
 luq_status luq_query_status(const void* ws, void* stream);
 
@@ -188,7 +190,8 @@ luq_status luq_query_status(const void* ws, void* stream);
  *           returns LUQ_ERR_NONFINITE).
  *  maxabs   out: 1 float, max|g| (non-finite when g is), or NULL.
  *  ws       workspace of luq_workspace_size(LUQ_OP_QUANTIZE_GRAD, rows*cols)
- *           (may be NULL when rows*cols = 0); receives the status word.
+ *           (may be NULL or of any size when rows*cols = 0); receives the
+ *           status word (luq_query_status).
  */
 luq_status luq_quantize_grad(const void* g, luq_dtype dt, int64_t rows, int64_t cols, int R,
                              uint64_t seed, uint32_t counter, int n_samples, uint8_t* codes,
@@ -250,7 +253,7 @@ luq_status luq_quantize_grad_noalloc(const void* g, luq_dtype dt, int64_t rows, 
  *           e.g., with the maxabs of luq_quantize_grad on an earlier step).
  *  alpha    out: 1 float, the alpha used.
  *  maxabs   out: 1 float, max|g| of this tensor (NaN if g has a NaN), or NULL.
- *  ws       workspace of luq_workspace_size(LUQ_OP_QUANTIZE_GRAD, rows*cols).
+ *  ws       workspace as for luq_quantize_grad.
  *
  * Errors as for luq_quantize_grad; LUQ_ERR_PARAM for eta outside [0, 1],
  * LUQ_ERR_NULL for a NULL state.
@@ -278,7 +281,8 @@ luq_status luq_quantize_grad_hindsight(const void* g, luq_dtype dt, int64_t rows
  *           NULL, not both).
  *  scale    out: 1 float s.
  *  ws       workspace of luq_workspace_size(LUQ_OP_INT4_QUANTIZE, rows*cols)
- *           (may be NULL when clip > 0); receives the status word.
+ *           (may be NULL or of any size when clip > 0 or rows*cols = 0);
+ *           receives the status word (luq_query_status).
  */
 luq_status int4_quantize(const void* x, luq_dtype dt, int64_t rows, int64_t cols, int is_signed,
                          float clip, uint8_t* codes, uint8_t* codes_t, float* scale, void* ws,

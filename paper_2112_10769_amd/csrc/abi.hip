@@ -151,6 +151,13 @@ size_t luq_workspace_size(int op, int64_t d0, int64_t d1, int64_t d2) {
   }
 }
 
+// The workspace that a quantizer leaves its status in.  An empty tensor, or a given clip
+// value, needs none: what is passed there may be of any size, and one that does not hold the
+// status word (it lies behind the partial maxima) is not written.
+static void* status_workspace(void* ws, size_t ws_bytes) {
+  return ws_bytes >= luq::quant_workspace_bytes(0) && aligned4(ws) ? ws : nullptr;
+}
+
 // Checks of luq_quantize_grad's arguments other than the workspace; R loses
 // the LUQ_ALPHA_PW2 flag, which goes to *pw2.
 static luq_status quantize_grad_checks(const char* fn, const void* g, luq_dtype dt, int64_t rows, int64_t cols,
@@ -191,8 +198,8 @@ luq_status luq_quantize_grad(const void* g, luq_dtype dt, int64_t rows, int64_t 
     if (!aligned16(ws)) return fail(LUQ_ERR_ALIGN, "%s: ws must be 16-byte aligned", fn);
   }
   return hip_status(luq::launch_luq_quantize(g, dt == LUQ_BF16, rows, cols, R, pw2, seed, counter,
-                                             n_samples, codes, codes_t, alpha, maxabs, ws,
-                                             static_cast<hipStream_t>(stream)));
+                                             n_samples, codes, codes_t, alpha, maxabs,
+                                             status_workspace(ws, ws_bytes), static_cast<hipStream_t>(stream)));
 }
 
 luq_status luq_quantize_grad_noalloc(const void* g, luq_dtype dt, int64_t rows, int64_t cols, int R,
@@ -240,7 +247,8 @@ luq_status luq_quantize_grad_hindsight(const void* g, luq_dtype dt, int64_t rows
   if (!aligned4(alpha) || !aligned4(maxabs) || !aligned4(state))
     return fail(LUQ_ERR_ALIGN, "%s: alpha / maxabs / state misaligned", fn);
   return hip_status(luq::launch_luq_quantize_hindsight(g, dt == LUQ_BF16, rows, cols, R, pw2, seed, counter, n_samples,
-                                                       eta, codes, codes_t, state, alpha, maxabs, ws,
+                                                       eta, codes, codes_t, state, alpha, maxabs,
+                                                       status_workspace(ws, ws_bytes),
                                                        static_cast<hipStream_t>(stream)));
 }
 
@@ -266,7 +274,7 @@ luq_status int4_quantize(const void* x, luq_dtype dt, int64_t rows, int64_t cols
   }
   if (!aligned4(scale)) return fail(LUQ_ERR_ALIGN, "%s: scale misaligned", "int4_quantize");
   return hip_status(luq::launch_int4_quantize(x, dt == LUQ_BF16, rows, cols, is_signed ? 1 : 0,
-                                              clip, codes, codes_t, scale, ws,
+                                              clip, codes, codes_t, scale, status_workspace(ws, ws_bytes),
                                               static_cast<hipStream_t>(stream)));
 }
 

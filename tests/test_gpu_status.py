@@ -125,3 +125,46 @@ def test_status_of_an_unwritten_workspace_is_refused(L):
     with pytest.raises(L.LuqError) as e:
         L.query_status(ws)
     assert e.value.status == 5
+
+
+def _guarded(nbytes):
+    """A workspace of nbytes inside a larger buffer, and the check of what a call left there: nothing outside the
+    workspace, and nothing at all in one that is too small for the status word."""
+    buf = torch.full((1 << 18,), 0xA5, dtype=torch.uint8, device="cuda:0")
+    start = 4096
+
+    def untouched(inside):
+        b = host(buf)
+        outside = np.concatenate([b[:start], b[start + nbytes:]])
+        return (outside == 0xA5).all() and (not inside or (b == 0xA5).all())
+    return buf[start:start + nbytes], untouched
+
+
+SHORT = [0, 1, 16, 4096, 65536, 65540, 65543]   # a quantizer's workspace has 65544 bytes
+
+
+@pytest.mark.parametrize("nbytes", SHORT + [65544, 70000])
+@pytest.mark.parametrize("call", ["luq", "hindsight", "int4", "int4 clip"])
+def test_status_stays_inside_the_workspace(L, call, nbytes):
+    """Empty tensors and a given clip value need no workspace: one of any size is not written beyond its end."""
+    ws, untouched = _guarded(nbytes)
+    empty = torch.zeros(0, dtype=torch.float32, device="cuda:0")
+    announce("status word", call, nbytes)
+    if call == "luq":
+        _, _, alpha, maxabs = L.luq_quantize_grad(empty, ws=ws)
+        assert host(alpha)[0] == 0 and host(maxabs)[0] == 0
+    elif call == "hindsight":
+        state = torch.tensor([3.0], dtype=torch.float32, device="cuda:0")
+        _, _, alpha, maxabs = L.luq_quantize_grad_hindsight(empty, state, eta=0.25, ws=ws)
+        assert host(maxabs)[0] == 0 and host(state)[0] == np.float32(0.25) * np.float32(3.0)
+    elif call == "int4":
+        assert host(L.int4_quantize(empty, ws=ws)[2])[0] == 0
+    else:
+        for n in (1000, 1 << 17):
+            x = torch.linspace(-3, 3, n, device="cuda:0")
+            codes, _, scale = L.int4_quantize(x, clip=2.0, ws=ws)
+            want, _, want_scale = L.int4_quantize(x, clip=2.0, ws=_ws(L, n))
+            assert torch.equal(codes, want) and torch.equal(scale, want_scale)
+    assert untouched(nbytes in SHORT)
+    if nbytes not in SHORT:
+        assert L.query_status(ws) == L.LUQ_OK
