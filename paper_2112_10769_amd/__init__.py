@@ -18,6 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libluq.so")
 
 LUQ_OK = 0
+LUQ_ERR_WORKSPACE = 5
 LUQ_ERR_NONFINITE = 8
 LUQ_F32, LUQ_BF16 = 0, 1
 LUQ_I32, LUQ_I64 = 0, 1
@@ -154,6 +155,8 @@ def query_status(ws):
     """Status of the last quantizer call that used the workspace tensor ws
     (synchronizes torch's current stream): LUQ_OK or LUQ_ERR_NONFINITE;
     raises LuqError for anything else."""
+    if ws.numel() * ws.element_size() < workspace_size(OP_QUANTIZE_GRAD, 1):
+        raise LuqError(LUQ_ERR_WORKSPACE, "luq_query_status", "ws is smaller than a quantizer's workspace")
     st = LIB.luq_query_status(_ptr(ws), _stream(ws.device))
     if st not in (LUQ_OK, LUQ_ERR_NONFINITE):
         _check(st, "luq_query_status")

@@ -362,3 +362,13 @@ def test_fp6_carrier_rejects_on_the_host():
     assert dg(luq.CARRIER_FP6 | luq.SMP_SUM | 2) == 4
     assert dg(luq.CARRIER_FP6 | 1, ws_bytes=16) == 5
     assert dg(luq.CARRIER_FP6 | 1, K=48) == 2
+
+
+def test_query_status_refuses_short_workspaces():
+    """The status word is the last of a quantizer's workspace: it is not read from a shorter one."""
+    import torch
+    full = luq.workspace_size(luq.OP_QUANTIZE_GRAD, 1)
+    for n in (0, 1, 16, 65540, full - 1):
+        with pytest.raises(luq.LuqError) as e:
+            luq.query_status(torch.zeros(n, dtype=torch.uint8))
+        assert e.value.status == luq.LUQ_ERR_WORKSPACE
