@@ -380,6 +380,13 @@ def _input(t, n, dtype, gpu, name):
     raise ValueError(f"{name} must hold {n} elements of {dtype} on the input's device")
 
 
+def _scalar(t, gpu, name):
+    """The scale t, checked: the kernels read one float32 from the device."""
+    if t.dtype is torch.float32 and t.numel() == 1 and t.get_device() == gpu:
+        return t.data_ptr()
+    raise ValueError(f"{name} must be one float32 on the codes' device")
+
+
 def _codes(t, nbytes, gpu, name):
     """A code operand, checked: the kernels read nbytes from it."""
     if t.element_size() == 1 and t.numel() >= nbytes and t.get_device() == gpu and t.is_contiguous():
@@ -531,9 +538,9 @@ def int4_gemm_fwd_grouped(x_codes, x_scale, x_signed, w_codes, w_scale, w_signed
     w, w_row, w_expert, scales = _grouped_weights(w_codes, w_scale, experts, N, K, w_row, w_expert, gpu, "w_codes")
     if y is None:
         y = torch.empty(T, N, dtype=torch.float32, device=dev)
-    st = LIB.int4_gemm_fwd_grouped(_codes(x_codes, T * K // 2, gpu, "x_codes"), x_scale.data_ptr(), 1 if x_signed else 0, w,
-                                   w_row, w_expert, w_scale.data_ptr(), scales, 1 if w_signed else 0, offsets.data_ptr(),
-                                   experts, T, N, K, _buffer(y, T * N, torch.float32, gpu, "y"), _stream(dev))
+    st = LIB.int4_gemm_fwd_grouped(_codes(x_codes, T * K // 2, gpu, "x_codes"), _scalar(x_scale, gpu, "x_scale"),
+                                   1 if x_signed else 0, w, w_row, w_expert, w_scale.data_ptr(), scales,
+                                   1 if w_signed else 0, offsets.data_ptr(), experts, T, N, K, _buffer(y, T * N, torch.float32, gpu, "y"), _stream(dev))
     _check(st, "int4_gemm_fwd_grouped")
     return y
 
@@ -548,8 +555,8 @@ def luq_gemm_dgrad_grouped(g_codes, alpha, w_codes_t, w_scale, w_signed, offsets
     if dx is None:
         dx = torch.empty(M, N, dtype=torch.float32, device=dev)
     st = LIB.luq_gemm_dgrad_grouped(_codes(g_codes, M * K // (1 if n_samples & SMP_SUM else 2), gpu, "g_codes"),
-                                    alpha.data_ptr(), n_samples, w, w_row, w_expert, w_scale.data_ptr(), scales,
-                                    1 if w_signed else 0, offsets.data_ptr(), experts, M, N, K,
+                                    _scalar(alpha, gpu, "alpha"), n_samples, w, w_row, w_expert, w_scale.data_ptr(),
+                                    scales, 1 if w_signed else 0, offsets.data_ptr(), experts, M, N, K,
                                     _buffer(dx, M * N, torch.float32, gpu, "dx"), _stream(dev))
     _check(st, "luq_gemm_dgrad_grouped")
     return dx
@@ -570,9 +577,10 @@ def luq_gemm_wgrad_grouped(g_codes_t, alpha, a_codes_t, a_scale, a_signed, offse
     if ws is None:
         ws = _bytes(grouped_wgrad_workspace(T, Nout, Kin, experts), dev)
     st = LIB.luq_gemm_wgrad_grouped(_codes(g_codes_t, Nout * T // (1 if n_samples & SMP_SUM else 2), gpu, "g_codes_t"),
-                                    alpha.data_ptr(), n_samples, _codes(a_codes_t, Kin * T // 2, gpu, "a_codes_t"),
-                                    a_scale.data_ptr(), 1 if a_signed else 0, offsets.data_ptr(), experts, T, Nout, Kin,
-                                    _buffer(dw, experts * Nout * Kin, torch.float32, gpu, "dw"), ws.data_ptr(), ws.numel(),
-                                    _stream(dev))
+                                    _scalar(alpha, gpu, "alpha"), n_samples,
+                                    _codes(a_codes_t, Kin * T // 2, gpu, "a_codes_t"),
+                                    _scalar(a_scale, gpu, "a_scale"), 1 if a_signed else 0, offsets.data_ptr(), experts,
+                                    T, Nout, Kin, _buffer(dw, experts * Nout * Kin, torch.float32, gpu, "dw"),
+                                    ws.data_ptr(), ws.numel(), _stream(dev))
     _check(st, "luq_gemm_wgrad_grouped")
     return dw

@@ -357,3 +357,17 @@ def test_unaligned_output_and_graph(L):
         kept = dw.clone()
         step()
         assert torch.equal(kept, dw), sizes
+
+
+def test_scales_on_the_host_are_refused(L):
+    """Before anything is launched: the kernels would read a host address."""
+    dev = torch.device("cuda:0")
+    codes, one = torch.zeros(64, dtype=torch.uint8, device=dev), torch.ones(1, device=dev)
+    offsets, host_one = torch.zeros(4, dtype=torch.int32, device=dev), torch.ones(1)
+    announce("scales on the host")
+    for call in (lambda: L.int4_gemm_fwd_grouped(codes, host_one, True, codes, one, True, offsets, 1, 1, 32),
+                 lambda: L.luq_gemm_dgrad_grouped(codes, host_one, codes, one, True, offsets, 1, 1, 32),
+                 lambda: L.luq_gemm_wgrad_grouped(codes, host_one, codes, one, True, offsets, 32, 1, 1),
+                 lambda: L.luq_gemm_wgrad_grouped(codes, one, codes, host_one, True, offsets, 32, 1, 1)):
+        with pytest.raises(ValueError, match="float32"):
+            call()

@@ -208,3 +208,18 @@ def test_binding_checks_buffers():
         luq.luq_gemm_wgrad_grouped(codes, one, codes, one, True, offsets.long(), 32, 1, 1)
     with pytest.raises(ValueError):
         luq.luq_gemm_wgrad_grouped(codes, one, codes, one, True, offsets, 32, 5, 1)
+
+
+@pytest.mark.parametrize("bad", [torch.ones(1, dtype=torch.float64), torch.ones(1, dtype=torch.bfloat16), torch.ones(2),
+                                 torch.ones(0)])
+def test_binding_checks_scales(bad):
+    """One float32 on the codes' device, for every scale of the grouped products."""
+    codes, one, offsets = torch.zeros(64, dtype=torch.uint8), torch.ones(1), torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="x_scale"):
+        luq.int4_gemm_fwd_grouped(codes, bad, True, codes, one, True, offsets, 1, 1, 32)
+    with pytest.raises(ValueError, match="alpha"):
+        luq.luq_gemm_dgrad_grouped(codes, bad, codes, one, True, offsets, 1, 1, 32)
+    with pytest.raises(ValueError, match="alpha"):
+        luq.luq_gemm_wgrad_grouped(codes, bad, codes, one, True, offsets, 32, 1, 1)
+    with pytest.raises(ValueError, match="a_scale"):
+        luq.luq_gemm_wgrad_grouped(codes, one, codes, bad, True, offsets, 32, 1, 1)
