@@ -387,6 +387,13 @@ def _scalar(t, gpu, name):
     raise ValueError(f"{name} must be one float32 on the codes' device")
 
 
+def _workspace(t, gpu):
+    """The workspace t, checked: the kernels write its bytes; the library compares their number with its need."""
+    if t.get_device() == gpu and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("ws must be contiguous, on the input's device")
+
+
 def _codes(t, nbytes, gpu, name):
     """A code operand, checked: the kernels read nbytes from it."""
     if t.element_size() == 1 and t.numel() >= nbytes and t.get_device() == gpu and t.is_contiguous():
@@ -407,7 +414,7 @@ def luq_group_ids(ids, groups, order=None, offsets=None, ws=None):
         ws = _bytes(workspace_size(OP_GROUP_IDS, n, groups), dev)
     ids = ids.contiguous()
     st = LIB.luq_group_ids(ids.data_ptr(), it, n, groups, _buffer(order, n, torch.int32, gpu, "order"),
-                           _buffer(offsets, groups + 1, torch.int32, gpu, "offsets"), ws.data_ptr(), ws.numel(),
+                           _buffer(offsets, groups + 1, torch.int32, gpu, "offsets"), _workspace(ws, gpu), ws.numel(),
                            _stream(dev))
     _check(st, "luq_group_ids")
     return order, offsets
@@ -449,7 +456,7 @@ def luq_embedding_grad(dout, ids, order, offsets, scale=1.0, accumulate=False, d
     dout, ids = dout.contiguous(), ids.contiguous()
     st = LIB.luq_embedding_grad(dout.data_ptr(), gt, ids.data_ptr(), it, order.data_ptr(), offsets.data_ptr(), n, vocab,
                                 dim, scale, 1 if accumulate else 0,
-                                _buffer(dtable, vocab * dim, torch.float32, gpu, "dtable"), ws.data_ptr(), ws.numel(),
+                                _buffer(dtable, vocab * dim, torch.float32, gpu, "dtable"), _workspace(ws, gpu), ws.numel(),
                                 _stream(dev))
     _check(st, "luq_embedding_grad")
     return dtable
@@ -504,7 +511,7 @@ def luq_layernorm_bwd(dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta
     st = LIB.luq_layernorm_bwd(dy.data_ptr(), gt, x.data_ptr(), dt, mean.data_ptr(), rstd.data_ptr(), _ptr(gamma), rows,
                                cols, _buffer(dx, n, dy.dtype, gpu, "dx"),
                                _buffer(dgamma, cols, torch.float32, gpu, "dgamma"),
-                               _buffer(dbeta, cols, torch.float32, gpu, "dbeta"), ws.data_ptr(), ws.numel(), _stream(dev))
+                               _buffer(dbeta, cols, torch.float32, gpu, "dbeta"), _workspace(ws, gpu), ws.numel(), _stream(dev))
     _check(st, "luq_layernorm_bwd")
     return dx, dgamma, dbeta
 
@@ -581,6 +588,6 @@ def luq_gemm_wgrad_grouped(g_codes_t, alpha, a_codes_t, a_scale, a_signed, offse
                                     _codes(a_codes_t, Kin * T // 2, gpu, "a_codes_t"),
                                     _scalar(a_scale, gpu, "a_scale"), 1 if a_signed else 0, offsets.data_ptr(), experts,
                                     T, Nout, Kin, _buffer(dw, experts * Nout * Kin, torch.float32, gpu, "dw"),
-                                    ws.data_ptr(), ws.numel(), _stream(dev))
+                                    _workspace(ws, gpu), ws.numel(), _stream(dev))
     _check(st, "luq_gemm_wgrad_grouped")
     return dw

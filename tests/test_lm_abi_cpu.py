@@ -223,3 +223,31 @@ def test_binding_checks_scales(bad):
         luq.luq_gemm_wgrad_grouped(codes, bad, codes, one, True, offsets, 32, 1, 1)
     with pytest.raises(ValueError, match="a_scale"):
         luq.luq_gemm_wgrad_grouped(codes, one, codes, bad, True, offsets, 32, 1, 1)
+
+
+def _with_workspace(ws, dev):
+    """A call of every operator that takes a workspace, its other operands in order."""
+    def t(*shape, dtype=torch.float32):
+        return torch.zeros(*shape, dtype=dtype, device=dev)
+    ids, order, offsets = t(5, dtype=torch.int64), t(5, dtype=torch.int32), t(4, dtype=torch.int32)
+    codes = t(64, dtype=torch.uint8)
+    return (lambda: luq.luq_group_ids(ids, 3, ws=ws), lambda: luq.luq_embedding_grad(t(5, 2), ids, order, offsets, ws=ws),
+            lambda: luq.luq_layernorm_bwd(t(4, 6), t(4, 6), t(4), t(4), ws=ws),
+            lambda: luq.luq_gemm_wgrad_grouped(codes, t(1), codes, t(1), True, offsets, 32, 1, 1, ws=ws))
+
+
+def test_binding_checks_workspaces():
+    """A strided workspace: its bytes are not the ones behind its address."""
+    for call in _with_workspace(torch.zeros(1 << 16, 2, dtype=torch.uint8)[:, 0], "cpu"):
+        with pytest.raises(ValueError, match="ws must be"):
+            call()
+
+
+@pytest.mark.gpu
+def test_workspaces_on_the_host_are_refused():
+    """Before anything is launched: the kernels would write to a host address."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    for call in _with_workspace(torch.zeros(1 << 20, dtype=torch.uint8), "cuda:0"):
+        with pytest.raises(ValueError, match="ws must be"):
+            call()
