@@ -45,9 +45,10 @@ def route(p, y):
 
 def dispatch(experts, n_experts, tokens):
     """Rows sorted by expert: each row's (token, place in the flat list of choices), padded with -1 and 0 to whole
-    16-byte pieces of codes, and the experts' bounds."""
+    16-byte pieces of codes (long batches: whole stages of the weight gradient), and the experts' bounds."""
     order, offsets = L.luq_group_ids(experts.reshape(-1), n_experts)
-    rows = -(-order.numel() // 32) * 32
+    whole = 32 if order.numel() <= 1 << 18 else 128
+    rows = -(-order.numel() // whole) * whole
     pad = rows - order.numel()
     token = torch.nn.functional.pad(order // TOP, (0, pad), value=-1)
     return token, torch.nn.functional.pad(order, (0, pad)).long(), offsets

@@ -165,7 +165,8 @@ size_t luq_grouped_wgrad_workspace(int64_t T, int64_t Nout, int64_t Kin, int64_t
  *
  *  g_codes_t  [Nout][T] LUQ codes, or int8 sums with LUQ_SMP_SUM | 2;
  *  a_codes_t  [Kin][T] INT4 codes; dw [experts][Nout][Kin] fp32.
- *  T a multiple of 32 in [32, 2^18]: rows are padded at the end of the batch, after
+ *  T a multiple of 32 in [32, 2^18], or of 128 up to 2^22 (longer reductions are split,
+ *  their int32 sums added in 64 bits): rows are padded at the end of the batch, after
  *  offsets[experts]; what the padding holds does not matter.  Nout, Kin >= 1.
  *  ws         workspace of luq_grouped_wgrad_workspace(T, Nout, Kin, experts).
  */

@@ -576,7 +576,7 @@ def grouped_wgrad_workspace(T, Nout, Kin, experts):
 def luq_gemm_wgrad_grouped(g_codes_t, alpha, a_codes_t, a_scale, a_signed, offsets, T, Nout, Kin, n_samples=1, dw=None,
                            ws=None):
     """dW [experts, Nout, Kin]: luq_gemm_wgrad over each expert's rows, from transposed codes g^T [Nout, T] and
-    a^T [Kin, T]; experts without rows get 0."""
+    a^T [Kin, T], T a multiple of 32 (of 128 beyond 2^18); experts without rows get 0."""
     dev, gpu = g_codes_t.device, g_codes_t.get_device()
     experts = _groups(offsets, gpu)
     if dw is None:

@@ -614,11 +614,11 @@ luq_status luq_gemm_dgrad_grouped(const uint8_t* g_codes, const float* alpha, in
                       offsets, experts, T, N, K, dx, stream);
 }
 
-// Sizes of luq_gemm_wgrad_grouped.  T is at most the int32-exact length of a reduction.
+// Sizes of luq_gemm_wgrad_grouped.
 static bool grouped_wgrad_sizes(int64_t T, int64_t Nout, int64_t Kin, int64_t experts) {
-  return T >= 32 && (T & 31) == 0 && T <= (1 << 18) && Nout >= 1 && Nout <= kMaxRows && Kin >= 1 && Kin <= kMaxRows &&
+  return T >= 32 && (T & 31) == 0 && Nout >= 1 && Nout <= kMaxRows && Kin >= 1 && Kin <= kMaxRows &&
          experts >= 1 && experts <= kMaxExperts && Nout * Kin <= kMaxElements / experts &&
-         grid_fits(((Nout + 31) / 32 + 7) * experts, Kin);
+         luq::grouped_depth_fits(T, experts * Nout * Kin) && grid_fits(((Nout + 31) / 32 + 7) * experts, Kin);
 }
 
 size_t luq_grouped_wgrad_workspace(int64_t T, int64_t Nout, int64_t Kin, int64_t experts) {
@@ -636,7 +636,7 @@ luq_status luq_gemm_wgrad_grouped(const uint8_t* g_codes_t, const float* alpha, 
   if (st != LUQ_OK) return st;
   if (experts < 1 || experts > kMaxExperts) return fail(LUQ_ERR_SHAPE, "%s: experts in [1, 4096]", fn);
   if (!grouped_wgrad_sizes(T, Nout, Kin, experts))
-    return fail(LUQ_ERR_SHAPE, "%s: T must be a multiple of 32 in [32, 2^18], Nout and Kin positive", fn);
+    return fail(LUQ_ERR_SHAPE, "%s: T must be a multiple of 32 in [32, 2^18] or of 128 up to 2^22, Nout and Kin positive", fn);
   if (!g_codes_t || !alpha || !a_codes_t || !a_scale || !offsets || !dw) return fail(LUQ_ERR_NULL, "%s: NULL operand", fn);
   if (!aligned16(g_codes_t) || !aligned16(a_codes_t) || !aligned4(alpha) || !aligned4(a_scale) || !aligned4(offsets) ||
       !aligned4(dw))

@@ -225,7 +225,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_depth_kernel(Depth
   const int64_t m0 = (int64_t)(first + in % size) * S::BM, n0 = (int64_t)(in / size) * S::BN;
   int lo, hi;
   group_bounds(a.offsets, a.experts, (int)a.T, e, lo, hi);
-  if (a.splits > 1) {   // whole stages a split
+  if (a.splits > 1) {   // whole stages a split, at most kMaxExactK
     const int kb = lo & ~(kDepthAlign - 1), stages = (hi - kb + S::BK - 1) / S::BK;
     const int chunk = (stages + a.splits - 1) / a.splits * S::BK;
     const int from = kb + (int)blockIdx.y * chunk;
@@ -338,6 +338,12 @@ hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alp
     case GroupedA::kInt4S: return b_signed ? launch_rows<kAcInt4S, true>(a, st) : launch_rows<kAcInt4S, false>(a, st);
     default: return b_signed ? launch_rows<kAcInt4U, true>(a, st) : launch_rows<kAcInt4U, false>(a, st);
   }
+}
+
+bool grouped_depth_fits(int64_t T, int64_t outputs) {
+  if (T <= kMaxExactK) return true;
+  // the launch that adds the splits takes 4 outputs a thread of whole groups of 4, or one
+  return T <= kMostDepth && T % kDepthAlign == 0 && outputs < (int64_t)1 << (outputs % 4 == 0 ? 34 : 32);
 }
 
 size_t grouped_depth_workspace_bytes(int64_t T, int64_t M, int64_t N, int64_t experts) {

@@ -38,6 +38,12 @@ struct DepthPlan {
   int splits;
 };
 
+// One group may have all T rows, so a batch beyond the int32-exact length takes at least
+// T / kMaxExactK splits: a chunk of any group's stages is then within that length, which
+// every stage depth divides.
+constexpr int kMostSplits = 16;
+constexpr int64_t kMostDepth = kMostSplits * kMaxExactK;
+
 // As plan_rows, for a group of the mean length plus half a stage (its ends lie anywhere in
 // one), split where the tiles leave CUs idle.  Over 300 drawn shapes the choice loses 2.9%
 // in the geometric mean against the best of eight tiles in 1 to 16 splits, 18% at the 95th
@@ -49,9 +55,11 @@ static DepthPlan plan_depth(int64_t T, int64_t M, int64_t N, int64_t experts) {
   for (GemmTile t : {kTile256x256, kTile128x256, kTile128x128, kTile64x128, kTile32x64, kTile64x64k1}) {
     const TileCost& c = kTileCost[kPlanOne][t];
     const int64_t tiles = experts * (((M - 1) >> c.lm) + 1) * (((N - 1) >> c.ln) + 1);
-    for (int splits = 1; splits <= 16; splits *= 2) {
+    int least_splits = 1;
+    while (least_splits * kMaxExactK < T) least_splits *= 2;
+    for (int splits = least_splits; splits <= kMostSplits; splits *= 2) {
       const float k = (float)T / (float)experts + 64.0f;
-      if (splits > 1 && (splits * tiles >= 2 * kCus || k < (float)(splits << c.lk))) break;
+      if (splits > least_splits && (splits * tiles >= 2 * kCus || k < (float)(splits << c.lk))) break;
       const int64_t stages = ((int64_t)(k / (float)splits) >> c.lk) + 1;
       float cost = tile_time(c, kPlanOne, tiles * splits, (float)(stages << c.lk) * (1.0f / 128));
       if (outputs > kCachedOutputs && c.ln < 7) cost *= kNarrowBeyondCache;

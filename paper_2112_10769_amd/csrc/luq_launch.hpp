@@ -112,7 +112,9 @@ hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alp
                                int64_t w_expert, const float* bscale, int64_t scales, int b_signed,
                                const int32_t* offsets, int64_t experts, int64_t T, int64_t N, int64_t K, float* C,
                                hipStream_t st);
-// C [experts][M][N], the reduction over T grouped.
+// C [experts][M][N], the reduction over T grouped.  Beyond the int32-exact length the
+// reduction is split, and whole stages are asked for.
+bool grouped_depth_fits(int64_t T, int64_t outputs);
 size_t grouped_depth_workspace_bytes(int64_t T, int64_t M, int64_t N, int64_t experts);
 hipError_t launch_grouped_depth(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B,
                                 const float* bscale, int b_signed, const int32_t* offsets, int64_t experts, int64_t T,

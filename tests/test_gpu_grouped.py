@@ -266,6 +266,32 @@ def test_longest_exact_depth(L):
     assert (got[0] == 0).all() and (got[1] == np.float32(-64 * 7 * T)).all()
 
 
+@pytest.mark.parametrize("kind", ["luq", "sums"])
+@pytest.mark.parametrize("T", [(1 << 18) + 128, (1 << 19) + 384, 1 << 22])
+def test_batches_beyond_the_exact_depth(L, T, kind):
+    """Split so that no int32 sum passes its range, whichever expert has the rows: all in one, the largest codes of one
+    sign throughout; and groups that begin and end at any row."""
+    Nout, Kin = 3, 5
+    announce("grouped beyond the exact depth", T, kind)
+    # 64 either way: a code of R = 6, and the sum of two of R = 5
+    codes = U.luq_pack(np.full((Nout, T), 7)) if kind == "luq" else np.full((Nout, T), 64, dtype=np.int8)
+    top, samples = 64, 1 if kind == "luq" else 2
+    a = U.pack(np.full((Kin, T), 15))
+    cut = T // 3 + 17
+    for sizes in ([0, T], [T, 0], [cut, 0, T - cut], [5, T - 6], [T // 8] * 8):
+        offsets = _offsets(sizes)
+        got = host(L.luq_gemm_wgrad_grouped(to_dev(codes), _dev(0.75), to_dev(a), _dev(0.5), False, to_dev(offsets), T, Nout,
+                                            Kin, n_samples=1 if kind == "luq" else L.SMP_SUM | 2))
+        for e, rows in enumerate(sizes):
+            ref = epilogue_replica(np.full((Nout, Kin), float(top * 15 * rows)), np.float32(0.75), samples, np.float32(0.5))
+            assert np.array_equal(got[e], ref), (sizes, e)
+
+
+def test_batch_beyond_the_exact_depth_of_random_codes(L):
+    _check_depth(L, [1, 100000, 0, 150001, 40036], 67, 33, "luq", True)
+    _check_depth(L, [270000, 77], 130, 40, "sums", False)
+
+
 # ---- beyond 32 bits, streams, bounds -------------------------------------------------------
 
 

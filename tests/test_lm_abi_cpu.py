@@ -251,3 +251,10 @@ def test_workspaces_on_the_host_are_refused():
     for call in _with_workspace(torch.zeros(1 << 20, dtype=torch.uint8), "cuda:0"):
         with pytest.raises(ValueError, match="ws must be"):
             call()
+
+
+@pytest.mark.parametrize("T,status", [((1 << 18) + 128, NULL), (1 << 19, NULL), (1 << 22, NULL), ((1 << 18) + 96, SHAPE),
+                                      ((1 << 22) + 128, SHAPE)])
+def test_wgrad_grouped_takes_long_batches(T, status):
+    """Beyond the int32-exact length whole stages, as far as 32-bit offsets of a tile's rows go."""
+    assert _call("luq_gemm_wgrad_grouped", WGRAD, dict(T=T, g=NUL)) == status

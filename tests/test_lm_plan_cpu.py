@@ -65,6 +65,19 @@ def test_depth_shapes_reach_every_tile(plans):
     assert any(s > 1 for _, s in got) and any(s == 1 for _, s in got)
 
 
+def test_long_batches_are_split(plans):
+    """A chunk of the stages of a group that has the whole batch is int32-exact."""
+    rng = random.Random(4)
+    shapes = [(T, rng.randint(1, 3000), rng.randint(1, 3000), rng.randint(1, 40))
+              for T in ((1 << 18) + 128, 1 << 19, (1 << 19) + 128, (1 << 21) - 128, 1 << 22)
+              for _ in range(20)]
+    for (T, M, N, E), (tile, splits) in zip(shapes, plans([("d", *s) for s in shapes])):
+        stages = -(-T // DEPTH[tile])
+        assert -(-stages // splits) * DEPTH[tile] <= 1 << 18, (T, M, N, E, tile, splits)
+        assert luq.grouped_wgrad_workspace(T, M, N, E) == 4 * splits * E * M * N
+    assert luq.grouped_wgrad_workspace((1 << 22) + 128, 1, 1, 1) == 0
+
+
 def test_workspace_is_the_plans(plans):
     rng = random.Random(3)
     shapes = [(32 * rng.randint(1, 1 << rng.randint(0, 13)), rng.randint(1, 3000), rng.randint(1, 3000), rng.randint(1, 40))
