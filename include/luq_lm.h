@@ -132,7 +132,8 @@ luq_status luq_layernorm_bwd(const void* dy, luq_dtype gt, const void* x, luq_dt
  * for the expert e that row m belongs to; rows at or after offsets[experts] get 0.
  *
  *  x_codes [T][K] INT4 codes, w_codes per expert [N][K]; y [T][N] fp32.
- *  T >= 0, T <= 2^30; N >= 1; K a multiple of 32 in [32, 2^17] (the int32-exact length).
+ *  T >= 0, T <= 2^30; 1 <= N <= 2^30; T * N <= 2^36 (256 GiB of outputs), and below 2^23
+ *  tiles of 256 x 256.  K a multiple of 32 in [32, 2^17] (the int32-exact length).
  *  w_row >= K, w_row <= 2^22.  No workspace.
  */
 luq_status int4_gemm_fwd_grouped(const uint8_t* x_codes, const float* x_scale, int x_signed,
@@ -167,7 +168,9 @@ size_t luq_grouped_wgrad_workspace(int64_t T, int64_t Nout, int64_t Kin, int64_t
  *  a_codes_t  [Kin][T] INT4 codes; dw [experts][Nout][Kin] fp32.
  *  T a multiple of 32 in [32, 2^18], or of 128 up to 2^22 (longer reductions are split,
  *  their int32 sums added in 64 bits): rows are padded at the end of the batch, after
- *  offsets[experts]; what the padding holds does not matter.  Nout, Kin >= 1.
+ *  offsets[experts]; what the padding holds does not matter.  Nout, Kin in [1, 2^30], at
+ *  most 2^36 outputs in below 2^23 tiles of 256 x 256 (2^34 beyond 2^18 rows, 2^32 if they
+ *  are no multiple of 4).
  *  ws         workspace of luq_grouped_wgrad_workspace(T, Nout, Kin, experts).
  */
 luq_status luq_gemm_wgrad_grouped(const uint8_t* g_codes_t, const float* alpha, int n_samples,

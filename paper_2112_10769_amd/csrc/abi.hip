@@ -555,13 +555,6 @@ luq_status luq_layernorm_bwd(const void* dy, luq_dtype gt, const void* x, luq_dt
 
 constexpr int64_t kMaxExperts = 4096;
 
-// A grid has below 2^32 threads: 2^23 workgroups of 512, whichever tile is chosen (32 rows
-// and columns at least).
-static bool grid_fits(int64_t row_tiles, int64_t cols) {
-  const int64_t col_tiles = (cols + 31) / 32;
-  return row_tiles < ((int64_t)1 << 23) / col_tiles;
-}
-
 static luq_status grouped_rows(const char* fn, luq::GroupedA kind, int64_t max_k, const uint8_t* A, const float* alpha,
                                const uint8_t* B, int64_t w_row, int64_t w_expert, const float* bscale,
                                int64_t w_scales, int b_signed, const int32_t* offsets, int64_t experts, int64_t T,
@@ -575,7 +568,8 @@ static luq_status grouped_rows(const char* fn, luq::GroupedA kind, int64_t max_k
   if (w_expert < 0 || (w_expert & 31) || w_expert > ((int64_t)1 << 48))
     return fail(LUQ_ERR_SHAPE, "%s: w_expert must be a non-negative multiple of 32", fn);
   if (w_scales != 1 && w_scales != experts) return fail(LUQ_ERR_SHAPE, "%s: one weight scale, or one per expert", fn);
-  if (!grid_fits(T / 32 + (experts < T ? experts : T) + 1, N)) return fail(LUQ_ERR_SHAPE, "%s: too many tiles", fn);
+  if (!luq::grouped_rows_fit(T, N, experts))
+    return fail(LUQ_ERR_SHAPE, "%s: more than 2^36 outputs or 2^23 tiles", fn);
   if (T == 0) return LUQ_OK;
   if (!A || !alpha || !B || !bscale || !offsets || !C) return fail(LUQ_ERR_NULL, "%s: NULL operand", fn);
   if (!aligned16(A) || !aligned16(B) || !aligned4(alpha) || !aligned4(bscale) || !aligned4(offsets) || !aligned4(C))
@@ -618,7 +612,7 @@ luq_status luq_gemm_dgrad_grouped(const uint8_t* g_codes, const float* alpha, in
 static bool grouped_wgrad_sizes(int64_t T, int64_t Nout, int64_t Kin, int64_t experts) {
   return T >= 32 && (T & 31) == 0 && Nout >= 1 && Nout <= kMaxRows && Kin >= 1 && Kin <= kMaxRows &&
          experts >= 1 && experts <= kMaxExperts && Nout * Kin <= kMaxElements / experts &&
-         luq::grouped_depth_fits(T, experts * Nout * Kin) && grid_fits(((Nout + 31) / 32 + 7) * experts, Kin);
+         luq::grouped_depth_fits(T, Nout, Kin, experts);
 }
 
 size_t luq_grouped_wgrad_workspace(int64_t T, int64_t Nout, int64_t Kin, int64_t experts) {

@@ -256,12 +256,9 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void grouped_depth_kernel(Depth
 // ---- launch ------------------------------------------------------------------------------
 
 template <typename S, int AC, bool BSIGNED>
-void launch_rows_tile(RowsArgs a, hipStream_t st) {
+void launch_rows_tile(RowsArgs a, GemmTile tile, hipStream_t st) {
   a.tiles_n = (int)((a.N + S::BN - 1) / S::BN);
-  // whole tiles of T rows, and one partly filled tile for each group that can have rows
-  // and for the rows of no group
-  const int64_t groups = a.experts < a.T ? a.experts : a.T;
-  const dim3 grid((unsigned)((a.T / S::BM + groups + 1) * a.tiles_n));
+  const dim3 grid((unsigned)rows_grid(tile, a.T, a.N, a.experts));
   if (a.K % S::BK == 0)
     hipLaunchKernelGGL((grouped_rows_kernel<AC, BSIGNED, true, prefetch_depth<S, AC, 1, BSIGNED, true>(), S>), grid, dim3(S::THREADS), 0, st, a);
   else
@@ -270,22 +267,23 @@ void launch_rows_tile(RowsArgs a, hipStream_t st) {
 
 template <int AC, bool BSIGNED>
 hipError_t launch_rows(const RowsArgs& a, hipStream_t st) {
-  switch (plan_rows(a.T, a.N, a.K, a.experts)) {
-    case kTile256x256: launch_rows_tile<Tile256x256, AC, BSIGNED>(a, st); break;
-    case kTile128x128: launch_rows_tile<Tile128x128, AC, BSIGNED>(a, st); break;
-    case kTile64x128: launch_rows_tile<Tile64x128, AC, BSIGNED>(a, st); break;
-    case kTile32x64: launch_rows_tile<Tile32x64, AC, BSIGNED>(a, st); break;
-    case kTile32x32: launch_rows_tile<Tile32x32, AC, BSIGNED>(a, st); break;
-    default: launch_rows_tile<Tile64x64k1, AC, BSIGNED>(a, st); break;
+  const GemmTile tile = plan_rows(a.T, a.N, a.K, a.experts);
+  switch (tile) {
+    case kTile256x256: launch_rows_tile<Tile256x256, AC, BSIGNED>(a, tile, st); break;
+    case kTile128x128: launch_rows_tile<Tile128x128, AC, BSIGNED>(a, tile, st); break;
+    case kTile64x128: launch_rows_tile<Tile64x128, AC, BSIGNED>(a, tile, st); break;
+    case kTile32x64: launch_rows_tile<Tile32x64, AC, BSIGNED>(a, tile, st); break;
+    case kTile32x32: launch_rows_tile<Tile32x32, AC, BSIGNED>(a, tile, st); break;
+    default: launch_rows_tile<Tile64x64k1, AC, BSIGNED>(a, tile, st); break;
   }
   return hipGetLastError();
 }
 
 template <typename S, int AC, bool BSIGNED>
-void launch_depth_tile(DepthArgs a, hipStream_t st) {
+void launch_depth_tile(DepthArgs a, GemmTile tile, hipStream_t st) {
   a.tiles_m = (int)((a.M + S::BM - 1) / S::BM);
   a.tiles_n = (int)((a.N + S::BN - 1) / S::BN);
-  const dim3 grid((unsigned)(((int64_t)a.tiles_m * a.tiles_n + 7) / 8 * 8 * a.experts), (unsigned)a.splits);
+  const dim3 grid((unsigned)depth_grid(tile, a.M, a.N, a.experts), (unsigned)a.splits);
   constexpr int kPf = prefetch_depth<S, AC, 1, BSIGNED, true>();
   if (!a.partial && a.N % 32 == 0 && ((uintptr_t)a.C & 127) == 0)
     hipLaunchKernelGGL((grouped_depth_kernel<AC, BSIGNED, kPf, S, true>), grid, dim3(S::THREADS), 0, st, a);
@@ -297,12 +295,12 @@ template <int AC, bool BSIGNED>
 hipError_t launch_depth(DepthArgs a, GemmTile tile, hipStream_t st) {
   a.vec = (a.N % 4) == 0 && (((uintptr_t)(a.partial ? (void*)a.partial : (void*)a.C)) & 15) == 0;
   switch (tile) {
-    case kTile256x256: launch_depth_tile<Tile256x256, AC, BSIGNED>(a, st); break;
-    case kTile128x256: launch_depth_tile<Tile128x256, AC, BSIGNED>(a, st); break;
-    case kTile128x128: launch_depth_tile<Tile128x128, AC, BSIGNED>(a, st); break;
-    case kTile64x128: launch_depth_tile<Tile64x128, AC, BSIGNED>(a, st); break;
-    case kTile32x64: launch_depth_tile<Tile32x64, AC, BSIGNED>(a, st); break;
-    default: launch_depth_tile<Tile64x64k1, AC, BSIGNED>(a, st); break;
+    case kTile256x256: launch_depth_tile<Tile256x256, AC, BSIGNED>(a, tile, st); break;
+    case kTile128x256: launch_depth_tile<Tile128x256, AC, BSIGNED>(a, tile, st); break;
+    case kTile128x128: launch_depth_tile<Tile128x128, AC, BSIGNED>(a, tile, st); break;
+    case kTile64x128: launch_depth_tile<Tile64x128, AC, BSIGNED>(a, tile, st); break;
+    case kTile32x64: launch_depth_tile<Tile32x64, AC, BSIGNED>(a, tile, st); break;
+    default: launch_depth_tile<Tile64x64k1, AC, BSIGNED>(a, tile, st); break;
   }
   if (a.splits > 1)
     launch_split_reduce(a.partial, a.splits, a.experts * a.M * a.N,
@@ -311,6 +309,9 @@ hipError_t launch_depth(DepthArgs a, GemmTile tile, hipStream_t st) {
 }
 
 }  // namespace
+
+// fp32 outputs of 256 GiB; the largest tile has the fewest workgroups.
+static constexpr int64_t kMostOutputs = (int64_t)1 << 36;
 
 hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B, int64_t w_row,
                                int64_t w_expert, const float* bscale, int64_t scales, int b_signed,
@@ -340,7 +341,13 @@ hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alp
   }
 }
 
-bool grouped_depth_fits(int64_t T, int64_t outputs) {
+bool grouped_rows_fit(int64_t T, int64_t N, int64_t experts) {
+  return T * N <= kMostOutputs && rows_grid(kTile256x256, T, N, experts) < kMostWorkgroups;
+}
+
+bool grouped_depth_fits(int64_t T, int64_t M, int64_t N, int64_t experts) {
+  const int64_t outputs = experts * M * N;
+  if (outputs > kMostOutputs || depth_grid(kTile256x256, M, N, experts) >= kMostWorkgroups) return false;
   if (T <= kMaxExactK) return true;
   // the launch that adds the splits takes 4 outputs a thread of whole groups of 4, or one
   return T <= kMostDepth && T % kDepthAlign == 0 && outputs < (int64_t)1 << (outputs % 4 == 0 ? 34 : 32);

@@ -6,6 +6,22 @@
 
 namespace luq {
 
+// A grid has below 2^32 threads: 2^23 workgroups of 512.
+constexpr int64_t kMostWorkgroups = (int64_t)1 << 23;
+
+// Workgroups of a product of grouped rows: whole tiles of T rows, and one partly filled tile
+// for each group that can have rows and for the rows of no group.
+static int64_t rows_grid(GemmTile t, int64_t T, int64_t N, int64_t experts) {
+  const TileCost& c = kTileCost[kPlanOne][t];
+  return ((T >> c.lm) + (experts < T ? experts : T) + 1) * (((N - 1) >> c.ln) + 1);
+}
+
+// Workgroups of a split of the weight gradient: every group's tiles, in eighths for the XCDs.
+static int64_t depth_grid(GemmTile t, int64_t M, int64_t N, int64_t experts) {
+  const TileCost& c = kTileCost[kPlanOne][t];
+  return ((((M - 1) >> c.lm) + 1) * (((N - 1) >> c.ln) + 1) + 7) / 8 * 8 * experts;
+}
+
 // The tile with the least time by the ungrouped products' cost table.  The host knows the
 // mean group only; a group of m rows is taken to need m / BM + 0.6 tiles, and at least one
 // (with 1/2, groups of half a tile were taken to fill one each, which unequal ones exceed:
@@ -20,6 +36,7 @@ static GemmTile plan_rows(int64_t T, int64_t N, int64_t K, int64_t experts) {
   float least = 0.0f;
   for (GemmTile t : {kTile256x256, kTile128x128, kTile64x128, kTile32x64, kTile32x32, kTile64x64k1}) {
     const TileCost& c = kTileCost[kPlanOne][t];
+    if (rows_grid(t, T, N, experts) >= kMostWorkgroups) continue;
     const float tiles = mean / (float)(1 << c.lm) + 0.6f;
     const int64_t nb = (int64_t)(groups * (tiles > 1.0f ? tiles : 1.0f)) * (((N - 1) >> c.ln) + 1);
     const int64_t stages = ((K - 1) >> c.lk) + 1;
@@ -54,6 +71,7 @@ static DepthPlan plan_depth(int64_t T, int64_t M, int64_t N, int64_t experts) {
   const int64_t outputs = experts * M * N;
   for (GemmTile t : {kTile256x256, kTile128x256, kTile128x128, kTile64x128, kTile32x64, kTile64x64k1}) {
     const TileCost& c = kTileCost[kPlanOne][t];
+    if (depth_grid(t, M, N, experts) >= kMostWorkgroups) continue;
     const int64_t tiles = experts * (((M - 1) >> c.lm) + 1) * (((N - 1) >> c.ln) + 1);
     int least_splits = 1;
     while (least_splits * kMaxExactK < T) least_splits *= 2;

@@ -107,6 +107,8 @@ hipError_t launch_layernorm_bwd(const void* dy, int g_bf16, const void* x, int b
 
 // Products grouped by expert; the A operand's codes.
 enum class GroupedA { kLuq, kSums, kInt4S, kInt4U };
+// Sizes whose outputs and grid are not too large.
+bool grouped_rows_fit(int64_t T, int64_t N, int64_t experts);
 // C [T][N], the rows grouped; w_row and w_expert in codes.
 hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B, int64_t w_row,
                                int64_t w_expert, const float* bscale, int64_t scales, int b_signed,
@@ -114,7 +116,7 @@ hipError_t launch_grouped_rows(GroupedA kind, const uint8_t* A, const float* alp
                                hipStream_t st);
 // C [experts][M][N], the reduction over T grouped.  Beyond the int32-exact length the
 // reduction is split, and whole stages are asked for.
-bool grouped_depth_fits(int64_t T, int64_t outputs);
+bool grouped_depth_fits(int64_t T, int64_t M, int64_t N, int64_t experts);
 size_t grouped_depth_workspace_bytes(int64_t T, int64_t M, int64_t N, int64_t experts);
 hipError_t launch_grouped_depth(GroupedA kind, const uint8_t* A, const float* alpha, const uint8_t* B,
                                 const float* bscale, int b_signed, const int32_t* offsets, int64_t experts, int64_t T,

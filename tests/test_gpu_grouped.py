@@ -324,6 +324,24 @@ def test_experts_beyond_32_bits(L):
     torch.cuda.empty_cache()
 
 
+def test_outputs_beyond_the_small_tiles_grids(L):
+    """2^33 outputs: more 32 x 32 tiles than a grid has."""
+    T, N, K = 1 << 18, 1 << 15, 32
+    announce("grouped large output")
+    rng = np.random.default_rng(10)
+    w = U.int4_values(rng, (3, N, K), True)
+    a = U.int4_values(rng, (T, K), True)
+    cut = [0, 100001, 100001, T - 5]
+    y = L.int4_gemm_fwd_grouped(to_dev(U.pack(a)), _dev(1.0), True, to_dev(U.pack(w)), _dev([1, 1, 1]), True,
+                                to_dev(np.int32(cut)), T, N, K, y=torch.full((T, N), float("nan"), device="cuda"))
+    for lo, hi, e in ((0, 40, 0), (99980, 100001, 0), (100001, 100030, 2), (T - 40, T - 5, 2), (T - 5, T, -1)):
+        ref = _product(a[lo:hi], w[e]) if e >= 0 else np.zeros((hi - lo, N))
+        assert np.array_equal(host(y[lo:hi]), ref.astype(np.float32)), (lo, hi)
+    assert not torch.isnan(y.view(-1)[::1009]).any()
+    del y
+    torch.cuda.empty_cache()
+
+
 def test_decreasing_offsets_stay_inside(L):
     """Offsets that are no groups give some result inside the output, and no access outside it."""
     announce("grouped decreasing offsets")

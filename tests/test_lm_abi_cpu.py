@@ -258,3 +258,18 @@ def test_workspaces_on_the_host_are_refused():
 def test_wgrad_grouped_takes_long_batches(T, status):
     """Beyond the int32-exact length whole stages, as far as 32-bit offsets of a tile's rows go."""
     assert _call("luq_gemm_wgrad_grouped", WGRAD, dict(T=T, g=NUL)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=1 << 18, N=1 << 15), NULL), (dict(T=1 << 17, N=1 << 16, experts=64, w_scales=64), NULL), (dict(T=1 << 30, N=33), NULL),
+    (dict(T=1 << 20, N=1 << 16), NULL), (dict(T=(1 << 20) + 1, N=1 << 16), SHAPE), (dict(T=1, N=1 << 29), NULL),
+    (dict(T=4096, N=1 << 24, experts=4096, w_scales=1), SHAPE)])
+def test_grouped_rows_take_large_outputs(kw, status):
+    """Up to 2^36 outputs, with whatever tile has a grid for them."""
+    assert _call("int4_gemm_fwd_grouped", FWD, dict(kw, x=NUL)) == status
+
+
+@pytest.mark.parametrize("kw,status", [(dict(Nout=1 << 14, Kin=1 << 13, experts=128), NULL), (dict(Nout=1 << 18, Kin=1 << 18), SHAPE),
+                                       (dict(Nout=1 << 17, Kin=1 << 17), NULL)])
+def test_wgrad_grouped_takes_large_outputs(kw, status):
+    assert _call("luq_gemm_wgrad_grouped", WGRAD, dict(kw, g=NUL)) == status

@@ -78,6 +78,21 @@ def test_long_batches_are_split(plans):
     assert luq.grouped_wgrad_workspace((1 << 22) + 128, 1, 1, 1) == 0
 
 
+def test_grids_of_large_outputs(plans):
+    """Up to 2^36 outputs; a tile is only taken where its grid has below 2^32 threads."""
+    rng = random.Random(5)
+    rows, depths = [(1 << 18, 1 << 15, 32, 8), (1 << 17, 1 << 16, 4096, 64), (1 << 30, 33, 32, 1), (1 << 30, 64, 64, 4096),
+                    (1, 1 << 29, 32, 1), (1 << 20, 1 << 16, 64, 2)], [(64, 1 << 14, 1 << 13, 128), (64, 1 << 18, 1 << 18, 1)]
+    rows += [(2 ** rng.randint(13, 18), 2 ** rng.randint(12, 18), 2 ** rng.randint(5, 12), 2 ** rng.randint(0, 12))
+             for _ in range(200)]
+    for (T, N, K, E), (tile, _) in zip(rows, plans([("r", *s) for s in rows])):
+        m, n = (64, 64) if tile == "64x64k1" else map(int, tile.split("x"))
+        assert (T // m + min(E, T) + 1) * -(-N // n) < 1 << 23, (T, N, K, E, tile)
+    for (T, M, N, E), (tile, _) in zip(depths, plans([("d", *s) for s in depths])):
+        m, n = (64, 64) if tile == "64x64k1" else map(int, tile.split("x"))
+        assert -(-(-(-M // m) * -(-N // n)) // 8) * 8 * E < 1 << 23, (T, M, N, E, tile)
+
+
 def test_workspace_is_the_plans(plans):
     rng = random.Random(3)
     shapes = [(32 * rng.randint(1, 1 << rng.randint(0, 13)), rng.randint(1, 3000), rng.randint(1, 3000), rng.randint(1, 40))
