@@ -88,7 +88,8 @@ luq_status luq_embedding_grad(const void* dout, luq_dtype gt, const void* ids, l
  *  x, y         [rows][cols], type dt.  gamma, beta  [cols] fp32, or NULL for 1
  *               and 0.  mean, rstd  out: [rows] fp32, or NULL (serving).
  *  rows in [0, 2^30], cols in [1, 2^23]; eps >= 0 and finite.  Statistics are held in fp32, the
- *  variance from the differences to the mean.  y may be x.  No workspace.
+ *  variance from the differences to the mean, and a mean far from zero corrected by their
+ *  sum: a row of equal elements gives beta.  y may be x.  No workspace.
  */
 luq_status luq_layernorm_fwd(const void* x, luq_dtype dt, int64_t rows, int64_t cols, const float* gamma,
                              const float* beta, float eps, void* y, float* mean, float* rstd, void* stream);

@@ -252,3 +252,35 @@ def test_beyond_32_bits(L):
     U.within(host(dx[-1:].float()), ref[0], bound[0], "last row")
     del x, y, dx
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [1, 3, 5, 100, 777, 1000, 1001, 3001, 4096, 9000, 16391, 40001])
+def test_equal_elements_give_beta(L, cols, dt):
+    """Whatever the element: the mean is off by less than half a unit in its last place, so it is the element, and the
+    differences are zeros."""
+    values = torch.tensor([1000.0, -30000.0, 1000.1, 0.1, 7.7, -100.3, 1e-3, 123456.789], device="cuda").to(DT[dt])
+    x = values[:, None].repeat(1, cols)
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    gamma, beta = torch.randn(cols, device="cuda", generator=gen), torch.randn(cols, device="cuda", generator=gen)
+    announce("layernorm equal elements", cols, dt)
+    y, mean, rstd = L.luq_layernorm_fwd(x, gamma, beta, 1e-5)
+    assert torch.equal(mean, values.float())
+    assert torch.equal(y, beta.to(DT[dt]).repeat(len(values), 1))
+    assert (rstd - 1e-5 ** -0.5).abs().max() < 1e-3
+
+
+@pytest.mark.parametrize("cols", [1000, 4096, 20000])
+@pytest.mark.parametrize("mean", [1000.1, -30000.0])
+def test_mean_is_the_nearest(L, cols, mean):
+    """The mean's error is its rounding and that of the small differences' sum, not that of a sum of large terms: with u the
+    unit roundoff and k additions in a row, u |mean| + (k + 3) u (mean |x - m|), and m itself off by at most (k + 2) u mean |x|."""
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randn(20, cols, device="cuda", generator=gen) * 0.01 + mean
+    announce("layernorm mean", cols, mean)
+    _, got, rstd = (host(v).astype(np.float64) for v in L.luq_layernorm_fwd(x))
+    xd = host(x).astype(np.float64)
+    exact, k = xd.mean(1), cols / 64 + 16
+    spread = np.abs(xd - exact[:, None]).mean(1) + (k + 2) * U.U * np.abs(xd).mean(1)
+    bound = U.U * np.abs(exact) + (k + 3) * U.U * spread
+    assert (np.abs(got - exact) <= bound).all(), (np.abs(got - exact) / bound).max()
