@@ -317,10 +317,67 @@ __global__ __launch_bounds__(kThreads<TPR>) void layernorm_bwd_kernel(const G* d
   }
 }
 
+// ---- backward of rows of fewer than kNarrow columns: a thread a row
+//
+// With a column a thread 128 workgroups kept 5 threads each of 200000 x 5 busy, and each added
+// 1600 terms in a row (bf16 1611 us a call, 15 now; 4 x 4 fp32 4.4 and 5.0).
+
+constexpr int kNarrow = 8, kNarrowThreads = 256;
+
+template <typename G, typename T>
+__global__ __launch_bounds__(kNarrowThreads) void layernorm_narrow_bwd_kernel(const G* dy, const T* __restrict__ x,
+                                                                              BwdArgs a, G* dx) {
+  constexpr int N = kNarrow - 1, W = kNarrowThreads / kWave;
+  __shared__ float red[2][N][W];
+  const int cols = (int)a.cols;
+  const float inv = 1.0f / (float)cols;
+  float g[N], sum[2][N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    g[k] = a.gamma && k < cols ? a.gamma[k] : 1.0f;
+    sum[0][k] = sum[1][k] = 0.0f;
+  }
+  for (int64_t row = (int64_t)blockIdx.x * kNarrowThreads + threadIdx.x; row < a.rows;
+       row += (int64_t)gridDim.x * kNarrowThreads) {
+    const float mu = a.mean[row], r = a.rstd[row];
+    float d[N], xh[N], m1 = 0.0f, m2 = 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float dyk = k < cols ? to_f32(dy[row * cols + k]) : 0.0f;
+      xh[k] = k < cols ? (to_f32(x[row * cols + k]) - mu) * r : 0.0f;
+      sum[0][k] = fmaf(dyk, xh[k], sum[0][k]);
+      sum[1][k] += dyk;
+      d[k] = dyk * g[k];
+      m1 += d[k];
+      m2 = fmaf(d[k], xh[k], m2);
+    }
+    m1 *= inv;
+    m2 *= inv;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (k < cols) dx[row * cols + k] = from_f32<G>(r * (d[k] - m1 - xh[k] * m2));
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float s = wave_sum(sum[which][k]);
+      if ((threadIdx.x & (kWave - 1)) == 0) red[which][k][threadIdx.x / kWave] = s;
+    }
+  __syncthreads();
+  const int which = threadIdx.x / kWave, k = threadIdx.x & (kWave - 1);
+  if (which < 2 && k < cols) {
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) s += red[which][k][w];
+    float* const out = a.sums(blockIdx.x, gridDim.x, which);
+    if (out) out[k] = s;
+  }
+}
+
 // ---- backward of wide rows: read twice
 
-// A row's two means, by a workgroup.  Also the whole backward of rows narrower than a pack
-// has this form: its sums read element by element.
+// A row's two means, by a workgroup.
 template <typename G, typename T>
 __global__ __launch_bounds__(1024) void layernorm_means_kernel(const G* __restrict__ dy, const T* __restrict__ x,
                                                                BwdArgs a, float2* __restrict__ means) {
@@ -348,13 +405,12 @@ __global__ __launch_bounds__(1024) void layernorm_means_kernel(const G* __restri
 }
 
 // dx and the sums over rows: a thread keeps one pack of columns and walks the rows
-// blockIdx.y, blockIdx.y + gridDim.y, .. with four of them in flight.  V = 1 takes rows of
-// any width.  Elements that two packs share are stored by the one before only: where dx is
+// blockIdx.y, blockIdx.y + gridDim.y, .. with four of them in flight.  Elements that two packs share are stored by the one before only: where dx is
 // dy, the other may have read them too late.
-template <typename G, typename T, int V>
+template <typename G, typename T>
 __global__ __launch_bounds__(256) void layernorm_slab_kernel(const G* dy, const T* __restrict__ x, BwdArgs a,
                                                              const float2* __restrict__ means, G* dx) {
-  constexpr int U = 4;
+  constexpr int V = kPack<G, T>, U = 4;
   const int64_t cols = a.cols, step = gridDim.y;
   const PackAt<V> at(((int)blockIdx.x * 256 + (int)threadIdx.x) * V, (int)cols);
   if (!at.any()) return;
@@ -443,7 +499,7 @@ __global__ __launch_bounds__(1024) void layernorm_weight_kernel(const float* __r
 
 // Threads per row and packs per thread for rows of `packs` packs, at most `most` packs a
 // thread: a wave's where that does, then workgroups of 256 threads and more.  {0, 0}: too
-// wide, or narrower than a pack.
+// wide, or (forward) narrower than a pack.
 struct RowShape {
   int tpr, packs;
 };
@@ -495,18 +551,21 @@ constexpr int64_t kMostCols = kBwdThreads * kElements;   // of the backward in r
 // 13.7, 15.6, 18.1).  A single workgroup writes the gradients itself, without the second
 // launch, and takes 4 rows (2 x 8000 bf16: 12.0 to 9.1 us a call; 4 x 4096 12.5 to
 // 9.5; 8 x 8192 12.0 to 14.4) or, of the form that reads twice, 8 (8 x 100000: 30 to 18).
+// Many rows take more workgroups than that, so that no thread adds more than kMostRows terms
+// in a row: an fp32 sum of n like terms can be off by n / 2 units of its last place.
+constexpr int64_t kMostRows = 4096;
 int64_t bwd_groups(int64_t rows, int64_t cols) {
-  if (cols < 8 || cols > kMostCols) {
-    if (rows > 0 && rows <= 8) return 1;
-    return rows < 128 ? rows : 128;
-  }
-  if (rows > 0 && rows <= 4) return 1;
-  if (cols <= 64 * kElements) {
-    const int64_t need = (rows + 11) / 12;
-    return need < 4 * kCuCount ? need : 4 * kCuCount;
-  }
-  const int64_t most = cols > 4096 ? kCuCount : 2 * kCuCount;
-  return rows < most ? rows : most;
+  auto groups = [&](int64_t few, int64_t at_once, int64_t need, int64_t most) {
+    if (rows > 0 && rows <= few) return (int64_t)1;
+    const int64_t least = (rows + kMostRows * at_once - 1) / (kMostRows * at_once);
+    if (most < least) most = least;
+    return need < most ? need : most;
+  };
+  if (cols < kNarrow)
+    return groups(kNarrowThreads, kNarrowThreads, (rows + kNarrowThreads - 1) / kNarrowThreads, 4 * kCuCount);
+  if (cols > kMostCols) return groups(8, 1, rows, 128);
+  if (cols <= 64 * kElements) return groups(4, 4, (rows + 11) / 12, 4 * kCuCount);
+  return groups(4, 1, rows, cols > 4096 ? kCuCount : 2 * kCuCount);
 }
 
 // Rows' means of the form that reads rows twice, after the sums of the groups.
@@ -540,8 +599,7 @@ hipError_t launch_layernorm_fwd(const void* x, int bf16, int64_t rows, int64_t c
 }
 
 size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols) {
-  // a pack is 4 or 8 elements, by the types: the means' place is there for either
-  return bwd_sums_bytes(rows, cols) + (cols < 8 || cols > kMostCols ? (size_t)rows * sizeof(float2) : 0);
+  return bwd_sums_bytes(rows, cols) + (cols > kMostCols ? (size_t)rows * sizeof(float2) : 0);
 }
 
 hipError_t launch_layernorm_bwd(const void* dy, int g_bf16, const void* x, int bf16, const float* mean,
@@ -558,16 +616,16 @@ hipError_t launch_layernorm_bwd(const void* dy, int g_bf16, const void* x, int b
       hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), 0, st, static_cast<const G*>(dy),
                          static_cast<const T*>(x), a, static_cast<G*>(dx));
     };
-    if (s.tpr == 0) {
+    if (cols < kNarrow) {
+      go(layernorm_narrow_bwd_kernel<G, T>, kNarrowThreads);
+    } else if (s.tpr == 0) {
       float2* const means = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + bwd_sums_bytes(rows, cols));
       const int64_t most = 4 * kCuCount;
       hipLaunchKernelGGL((layernorm_means_kernel<G, T>), dim3((unsigned)(rows < most ? rows : most)), dim3(1024), 0, st,
                          static_cast<const G*>(dy), static_cast<const T*>(x), a, means);
-      auto slabs = [&](auto kernel, int64_t pack) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((cols + 256 * pack - 1) / (256 * pack)), (unsigned)groups), dim3(256), 0,
-                           st, static_cast<const G*>(dy), static_cast<const T*>(x), a, means, static_cast<G*>(dx));
-      };
-      cols < V ? slabs(layernorm_slab_kernel<G, T, 1>, 1) : slabs(layernorm_slab_kernel<G, T, V>, V);
+      hipLaunchKernelGGL((layernorm_slab_kernel<G, T>), dim3((unsigned)((cols + 256 * V - 1) / (256 * V)), (unsigned)groups),
+                         dim3(256), 0, st, static_cast<const G*>(dy), static_cast<const T*>(x), a, means,
+                         static_cast<G*>(dx));
     } else
       with_shape<kElements / V, kBwdThreads>(s, [&](auto tpr, auto packs) {
         constexpr int TPR = decltype(tpr)::value;

@@ -284,3 +284,26 @@ def test_mean_is_the_nearest(L, cols, mean):
     spread = np.abs(xd - exact[:, None]).mean(1) + (k + 2) * U.U * np.abs(xd).mean(1)
     bound = U.U * np.abs(exact) + (k + 3) * U.U * spread
     assert (np.abs(got - exact) <= bound).all(), (np.abs(got - exact) / bound).max()
+
+
+@pytest.mark.parametrize("rows,cols,chain", [
+    # additions in a row on the way to a column's sum: the rows of a thread, the threads and workgroups that it meets
+    (1 << 20, 1, 4 + 6 + 4 + 64 + 16), (1 << 20, 5, 4 + 6 + 4 + 64 + 16), ((1 << 20) + 77, 7, 5 + 6 + 4 + 65 + 16),
+    (1 << 27, 8, 4096 + 4 + 512 + 16)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_sums_over_many_rows(L, rows, cols, chain, dt):
+    """Like terms: every addition rounds the same way, by up to half a unit of a sum that grows.  dy is c throughout and x
+    gives xh = 1, so that both sums are rows * c; each addition is off by u of the sum at most, and of c once more."""
+    c = float(np.float32(1 + 0.98 * 2.0 ** -12 if cols < 8 else 1 + 0.98 * 2.0 ** -10))
+    announce("layernorm many rows", rows, cols, dt)
+    dy = torch.full((rows, cols), c, device="cuda")
+    x = torch.zeros(rows, cols, dtype=DT[dt], device="cuda")
+    mean, rstd = torch.full((rows,), -1.0, device="cuda"), torch.ones(rows, device="cuda")
+    _, dgamma, dbeta = L.luq_layernorm_bwd(dy, x, mean, rstd, dx=dy)
+    bound = (chain + 5) * U.U * rows * c
+    for g in (dgamma, dbeta):
+        U.within(host(g), np.full(cols, rows * c), bound, (rows, cols))
+    # dx = c - mean(c) - 1 * mean(c * 1), each mean off by 22 u and each operation by u
+    assert ((dy + c).abs() <= 64 * U.U * c).all()
+    del dy, x
+    torch.cuda.empty_cache()
