@@ -50,7 +50,7 @@
 extern "C" {
 #endif
 
-#define LUQ_ABI_VERSION 10
+#define LUQ_ABI_VERSION 11
 
 typedef int luq_status;
 enum {

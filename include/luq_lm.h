@@ -6,6 +6,10 @@
  * (Appendix A.4); these are the embedding lookup and layer
  * norm below.  Layers of experts take the 4-bit products of Eqs. forward,
  * backward and update on rows grouped by expert, in groups of any sizes.
+ * A step of training takes three things more: the choice of experts for
+ * every token, the loss of the last layer (kept in high precision as the
+ * first), whose table is the embedding's or its own, and the update of the
+ * weights.
  *
  * Conventions are those of luq.h (device pointers owned by the caller, work
  * enqueued on `stream`, no synchronisation, argument errors found on the host
@@ -178,6 +182,157 @@ luq_status luq_gemm_wgrad_grouped(const uint8_t* g_codes_t, const float* alpha, 
                                   const uint8_t* a_codes_t, const float* a_scale, int a_signed,
                                   const int32_t* offsets, int64_t experts, int64_t T, int64_t Nout, int64_t Kin,
                                   float* dw, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Choice of experts.  A row of logits l gives scores s: their softmax, or each one's
+ * sigmoid.  The choice goes by c = s + bias: with groups > 1 the experts are `groups`
+ * runs of equal length, a run's rank is its largest c (group_best = 1) or the sum of its
+ * two largest (2; of those there are), and the experts of the top_groups first runs
+ * remain; of these the top_k largest c are taken, the largest first.  Equal values:
+ * the lower index first.  c is compared as if exact (in 64 bits where it is a sum), so
+ * that a choice does not hang on the rounding of an exponential.
+ *   w_k = scale * s_k, or with renorm scale * s_k / (sum of the row's chosen s)
+ *
+ * A logit or a bias of -inf bars an expert.  Where fewer than top_k remain, the places
+ * left hold expert -1 and weight 0 (no group of luq_group_ids, padding of
+ * luq_embedding_fwd): a row of -inf, such as a padded position's, has none.  A row with
+ * a logit or c that is NaN or +inf is a data error: experts -1, weights NaN.
+ */
+typedef enum { LUQ_SOFTMAX = 0, LUQ_SIGMOID = 1 } luq_score;
+
+/*
+ * luq_route_fwd -- the experts of every token, and their weights.
+ *
+ *  logits   [T][experts], type dt.  bias  [experts] fp32, or NULL.
+ *  chosen   out: [T][top_k] int32;  weights  out: [T][top_k] fp32.
+ *  T in [0, 2^28], experts in [1, 4096], top_k in [1, 64]; groups in [1, 64] divides
+ *  experts; top_groups in [1, groups]; top_k is at most the experts of top_groups groups.
+ *  scale is finite.  No workspace.
+ */
+luq_status luq_route_fwd(const void* logits, luq_dtype dt, int64_t T, int64_t experts, int64_t top_k, luq_score score,
+                         const float* bias, int64_t groups, int64_t top_groups, int group_best, int renorm,
+                         float scale, int32_t* chosen, float* weights, void* stream);
+
+/*
+ * luq_route_bwd -- gradient of luq_route_fwd's logits from that of its weights; the choice
+ * itself has none.  With d_k = scale * dweights_k, or with renorm scale / S * (dweights_k -
+ * sum_j dweights_j s_j / S), S the sum of the chosen s, and e_i the sum of the d_k of expert i:
+ *   softmax: dl_i = s_i * (e_i - sum_j e_j s_j),   sigmoid: dl_i = s_i * (1 - s_i) * e_i
+ *
+ *  dweights [T][top_k] fp32; chosen as the forward call wrote it (an expert outside
+ *  [0, experts) has no weight and gives nothing; a row without any gets zeros).
+ *  dlogits  out: [T][experts], type dt; it may be logits.
+ */
+luq_status luq_route_bwd(const float* dweights, const void* logits, luq_dtype dt, const int32_t* chosen, int64_t T,
+                         int64_t experts, int64_t top_k, luq_score score, int renorm, float scale, void* dlogits,
+                         void* stream);
+
+/*
+ * Softmax cross entropy of the last layer, z[t][v] = scale * sum_d x[t][d] table[v][d],
+ * whose logits are not kept: the forward call leaves the logarithm of each row's sum of
+ * exponentials, and the backward call forms the products again, a piece of the
+ * vocabulary at a time.
+ *   lse_t = log sum_v exp z_tv
+ *   loss_t = lse_t - (1 - smoothing) * z_t,target - smoothing / V * sum_v z_tv
+ *
+ *  x        [T][D], type xt.  table  [V][D], type tt.  Both 16-byte aligned.
+ *  targets  [T]; one below 0 is padding: loss 0, no gradient, whatever its row of x holds.
+ *           One at or above V is a data error: loss NaN, no gradient.
+ *  T in [0, 2^21], V in [1, 2^28], D in [1, 2^17]; T * V at most 2^37, T * D and V * D at most
+ *  2^36; scale finite, smoothing in [0, 1].
+ *
+ * Products are those of bf16 matrix instructions with fp32 sums.  An fp32 tensor is taken
+ * as three bf16 terms (24 bits, fewer below 2^-110: a term is a multiple of 2^-133), of
+ * whose products those above 2^-24 are formed.
+ * In the backward call the logits' gradient is rounded to one bf16 term for a bf16 output,
+ * to two (16 bits) for an fp32 gradient of bf16 activations, and to three otherwise.
+ */
+
+/* Bytes of the workspace of the forward call (gt = -1) or of the backward call (gt: type
+ * of dtable); 0 if the sizes are refused. */
+size_t luq_cross_entropy_workspace(int64_t T, int64_t V, int64_t D, luq_dtype xt, luq_dtype tt, int gt);
+
+/*
+ * luq_cross_entropy_fwd -- the loss of every token.
+ *  loss, lse  out: [T] fp32; lse is 0 where the target is no row of the table.
+ */
+luq_status luq_cross_entropy_fwd(const void* x, luq_dtype xt, const void* table, luq_dtype tt, const void* targets,
+                                 luq_index it, int64_t T, int64_t V, int64_t D, float scale, float smoothing,
+                                 float* loss, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * luq_cross_entropy_bwd -- gradients of luq_cross_entropy_fwd: with
+ *   g_tv = dloss_t * scale * (exp(z_tv - lse_t) - (1 - smoothing) [v = target_t] - smoothing / V)
+ *   dx = g table,  dtable = g^T x
+ *
+ *  dloss    [T] fp32.  lse  [T] of the forward call, which had the same scale and smoothing.
+ *  dx       out: [T][D], type xt.
+ *  dtable   out: [V][D], type gt: fp32, or bf16 where the table is.  accumulate = 0: written
+ *           whole; 1: added to (a table shared with the embedding, whose lookup's gradient
+ *           is there already).
+ *  Sums are taken in a fixed order: the same result on every call.
+ */
+luq_status luq_cross_entropy_bwd(const float* dloss, const void* x, luq_dtype xt, const void* table, luq_dtype tt,
+                                 const void* targets, luq_index it, const float* lse, int64_t T, int64_t V, int64_t D,
+                                 float scale, float smoothing, int accumulate, void* dx, void* dtable, luq_dtype gt,
+                                 void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * AdamW over many tensors in one launch.  With g' = grad_scale * g, t the step and
+ * r = lr * lr_scale:
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
+ *   p = p - r * weight_decay * p - r * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ * States are fp32, or 8 bits: m and the root of v as e4m3 codes (OCP), of which 32
+ * consecutive elements share a power of two 2^(scale - 127) that leaves the largest
+ * magnitude in [128, 256).  They are rounded stochastically, to the code above with the
+ * probability of the fraction (in 2^-16), as LUQ rounds gradients: to the nearest code, a
+ * v that changes by a thousandth a step would never leave its own.  A root above 0 does
+ * not become 0; what is not finite becomes NaN, and is left out of its block's scale.
+ * The random words are Philox4x32-10 of the key seed and the counter (i >> 2 in two words,
+ * the tensor's place in the plan, t): element i takes word i & 3, its low half for m and
+ * its high half for v.  States begin as zeros (codes and scales 0).
+ */
+typedef struct {
+  float* p;             /* [n] weights, updated                                    */
+  const void* g;        /* [n] gradient, type gt                                   */
+  void* m;              /* [n] fp32, or codes                                      */
+  void* v;              /* [n] fp32 (v), or codes (its root)                       */
+  uint8_t* m_scale;     /* [ceil(n / 32)] with codes, else not looked at           */
+  uint8_t* v_scale;
+  void* copy;           /* out: [n] bf16 copy of the new weights, or NULL          */
+  int64_t n;            /* 0 <= n <= 2^35                                          */
+  float weight_decay;   /* finite                                                  */
+  float lr_scale;       /* finite                                                  */
+  int gt;               /* luq_dtype of g                                          */
+  int state_bits;       /* 32 or 8                                                 */
+} luq_adamw_tensor;
+
+/* Bytes of the plan for count tensors (at most 2^20) of n[0] .. n[count - 1] elements, at
+ * most 2^35 together; 0 if refused, or if there is nothing to do. */
+size_t luq_adamw_plan_bytes(const int64_t* n, int64_t count);
+
+/*
+ * luq_adamw_plan -- the work of a step, laid out once for tensors that keep their places.
+ * `tensors` and `plan` are HOST memory; the caller copies the plan to the device.  Tensors
+ * do not overlap; each is aligned to its elements.
+ * Errors: LUQ_ERR_NULL, LUQ_ERR_SHAPE, LUQ_ERR_DTYPE, LUQ_ERR_PARAM, LUQ_ERR_ALIGN,
+ * LUQ_ERR_WORKSPACE (plan_bytes is not luq_adamw_plan_bytes).
+ */
+luq_status luq_adamw_plan(const luq_adamw_tensor* tensors, int64_t count, void* plan, size_t plan_bytes);
+
+/*
+ * luq_adamw_step -- one step of the tensors of a plan.
+ *
+ *  plan        device memory, 16-byte aligned, as luq_adamw_plan wrote it for `count` tensors.
+ *  lr          [1] fp32 on the device;  step  [1] int64 on the device, t >= 1 (less counts
+ *              as 1): a captured graph takes new ones at every replay.
+ *  beta1, beta2 in [0, 1);  eps >= 0, finite.
+ *  grad_scale  [1] fp32 on the device, or NULL for 1.  One that is NaN or infinite (an
+ *              overflowed norm) skips the step: nothing is written.
+ */
+luq_status luq_adamw_step(const void* plan, size_t plan_bytes, int64_t count, const float* lr, const int64_t* step,
+                          double beta1, double beta2, float eps, const float* grad_scale, uint64_t seed, void* stream);
 
 #ifdef __cplusplus
 }

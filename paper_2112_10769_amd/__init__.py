@@ -22,6 +22,7 @@ LUQ_ERR_WORKSPACE = 5
 LUQ_ERR_NONFINITE = 8
 LUQ_F32, LUQ_BF16 = 0, 1
 LUQ_I32, LUQ_I64 = 0, 1
+LUQ_SOFTMAX, LUQ_SIGMOID = 0, 1
 ALPHA_PW2 = 0x100  # or-ed into R: power-of-two alpha
 SMP_SUM = 0x10     # or-ed into n_samples = 2: the two samples as int8 sums
 CARRIER_FP6 = 0x40  # or-ed into n_samples = 1 of the backward GEMMs: FP6 MFMA carrier
@@ -39,6 +40,8 @@ EXPORTS = (
 EXPORTS_LM = (
     "luq_group_ids", "luq_embedding_fwd", "luq_embedding_grad", "luq_layernorm_fwd", "luq_layernorm_bwd",
     "int4_gemm_fwd_grouped", "luq_gemm_dgrad_grouped", "luq_grouped_wgrad_workspace", "luq_gemm_wgrad_grouped",
+    "luq_route_fwd", "luq_route_bwd", "luq_cross_entropy_workspace", "luq_cross_entropy_fwd", "luq_cross_entropy_bwd",
+    "luq_adamw_plan_bytes", "luq_adamw_plan", "luq_adamw_step",
 )
 
 
@@ -103,6 +106,23 @@ def _load():
     lib.luq_grouped_wgrad_workspace.argtypes = [i64, i64, i64, i64]
     lib.luq_gemm_wgrad_grouped.restype = i32
     lib.luq_gemm_wgrad_grouped.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i64, i64, i64, vp, vp, sz, vp]
+    lib.luq_route_fwd.restype = i32
+    lib.luq_route_fwd.argtypes = [vp, i32, i64, i64, i64, i32, vp, i64, i64, i32, i32, f32, vp, vp, vp]
+    lib.luq_route_bwd.restype = i32
+    lib.luq_route_bwd.argtypes = [vp, vp, i32, vp, i64, i64, i64, i32, i32, f32, vp, vp]
+    lib.luq_cross_entropy_workspace.restype = sz
+    lib.luq_cross_entropy_workspace.argtypes = [i64, i64, i64, i32, i32, i32]
+    lib.luq_cross_entropy_fwd.restype = i32
+    lib.luq_cross_entropy_fwd.argtypes = [vp, i32, vp, i32, vp, i32, i64, i64, i64, f32, f32, vp, vp, vp, sz, vp]
+    lib.luq_cross_entropy_bwd.restype = i32
+    lib.luq_cross_entropy_bwd.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, i64, i64, i64, f32, f32, i32, vp, vp, i32, vp, sz,
+                                          vp]
+    lib.luq_adamw_plan_bytes.restype = sz
+    lib.luq_adamw_plan_bytes.argtypes = [vp, i64]
+    lib.luq_adamw_plan.restype = i32
+    lib.luq_adamw_plan.argtypes = [vp, i64, vp, sz]
+    lib.luq_adamw_step.restype = i32
+    lib.luq_adamw_step.argtypes = [vp, sz, i64, vp, vp, ctypes.c_double, ctypes.c_double, f32, vp, u64, vp]
     return lib
 
 
@@ -591,3 +611,207 @@ def luq_gemm_wgrad_grouped(g_codes_t, alpha, a_codes_t, a_scale, a_signed, offse
                                     _workspace(ws, gpu), ws.numel(), _stream(dev))
     _check(st, "luq_gemm_wgrad_grouped")
     return dw
+
+
+# ---- choice of experts, loss, weights' update -------------------------------------------------
+
+_SCORES = {"softmax": LUQ_SOFTMAX, "sigmoid": LUQ_SIGMOID}
+
+
+def _score(name):
+    if name in _SCORES:
+        return _SCORES[name]
+    raise ValueError(f"score must be softmax or sigmoid, not {name!r}")
+
+
+def luq_route_fwd(logits, top_k, score="softmax", bias=None, groups=1, top_groups=1, group_best=1, renorm=True, scale=1.0,
+                  experts=None, weights=None):
+    """The top_k experts of every row of logits [..., experts] and their weights: (experts int32, weights float32) of
+    [..., top_k], the largest first.  bias (float32 [experts]) moves the choice alone; of `groups` runs of experts the
+    top_groups whose group_best best experts rank highest remain; renorm divides by the sum of the chosen scores.
+    Places without an expert (logits of -inf) hold -1 and 0."""
+    dev, gpu, E = logits.device, logits.get_device(), logits.shape[-1]
+    T = logits.numel() // max(E, 1)
+    dt, sc = _dtype(logits), _score(score)
+    bias = _input(bias, E, torch.float32, gpu, "bias")
+    if experts is None:
+        experts = torch.empty((*logits.shape[:-1], top_k), dtype=torch.int32, device=dev)
+    if weights is None:
+        weights = torch.empty((*logits.shape[:-1], top_k), dtype=torch.float32, device=dev)
+    if not logits.is_contiguous():
+        logits = logits.contiguous()
+    st = LIB.luq_route_fwd(logits.data_ptr(), dt, T, E, top_k, sc, _ptr(bias), groups, top_groups, group_best,
+                           1 if renorm else 0, scale, _buffer(experts, T * top_k, torch.int32, gpu, "experts"),
+                           _buffer(weights, T * top_k, torch.float32, gpu, "weights"), _stream(dev))
+    _check(st, "luq_route_fwd")
+    return experts, weights
+
+
+def luq_route_bwd(dweights, logits, experts, score="softmax", renorm=True, scale=1.0, dlogits=None):
+    """Gradient of luq_route_fwd's logits, in their dtype, from that of the weights (float32) and the experts it chose;
+    dlogits may be logits."""
+    dev, gpu, E, K = logits.device, logits.get_device(), logits.shape[-1], experts.shape[-1]
+    T = logits.numel() // max(E, 1)
+    dt, sc = _dtype(logits), _score(score)
+    dweights = _input(dweights, T * K, torch.float32, gpu, "dweights")
+    experts = _input(experts, T * K, torch.int32, gpu, "experts")
+    if dlogits is None:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    if not logits.is_contiguous():
+        logits = logits.contiguous()
+    st = LIB.luq_route_bwd(dweights.data_ptr(), logits.data_ptr(), dt, experts.data_ptr(), T, E, K, sc, 1 if renorm else 0, scale,
+                           _buffer(dlogits, T * E, logits.dtype, gpu, "dlogits"), _stream(dev))
+    _check(st, "luq_route_bwd")
+    return dlogits
+
+
+def _code_of(dtype):
+    if dtype is torch.float32:
+        return LUQ_F32
+    if dtype is torch.bfloat16:
+        return LUQ_BF16
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def luq_cross_entropy_workspace(T, V, D, x_dtype, table_dtype, grad_dtype=None):
+    """Bytes of the workspace of luq_cross_entropy_fwd, or with the dtype of dtable of luq_cross_entropy_bwd."""
+    return int(LIB.luq_cross_entropy_workspace(T, V, D, _code_of(x_dtype), _code_of(table_dtype),
+                                               -1 if grad_dtype is None else _code_of(grad_dtype)))
+
+
+def _aligned(t):
+    """t contiguous, on a 16-byte address."""
+    if not t.is_contiguous():
+        t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
+def _loss_operands(x, table, targets):
+    """Sizes and types of a loss, its operands checked."""
+    gpu = x.get_device()
+    if table.dim() != 2 or table.get_device() != gpu or x.shape[-1] != table.shape[1]:
+        raise ValueError("table must be [V, x.shape[-1]] on x's device")
+    V, D = table.shape
+    T = x.numel() // max(D, 1)
+    if targets.numel() != T or targets.get_device() != gpu:
+        raise ValueError("targets must be one id for each row of x, on its device")
+    return gpu, T, V, D, _dtype(x), _dtype(table), _index(targets)
+
+
+def luq_cross_entropy_fwd(x, table, targets, scale=1.0, smoothing=0.0, loss=None, lse=None, ws=None):
+    """Softmax cross entropy of the logits scale * x table^T, which are not kept: (loss, lse), float32 of targets'
+    shape.  Targets below 0 are padding (0), those at or above the table's rows give NaN."""
+    gpu, T, V, D, xt, tt, it = _loss_operands(x, table, targets)
+    dev = x.device
+    if loss is None:
+        loss = torch.empty(targets.shape, dtype=torch.float32, device=dev)
+    if lse is None:
+        lse = torch.empty(targets.shape, dtype=torch.float32, device=dev)
+    if ws is None:
+        ws = _bytes(LIB.luq_cross_entropy_workspace(T, V, D, xt, tt, -1), dev)
+    x, table, targets = _aligned(x), _aligned(table), targets.contiguous()
+    st = LIB.luq_cross_entropy_fwd(x.data_ptr(), xt, table.data_ptr(), tt, targets.data_ptr(), it, T, V, D, scale, smoothing,
+                                   _buffer(loss, T, torch.float32, gpu, "loss"), _buffer(lse, T, torch.float32, gpu, "lse"),
+                                   _workspace(ws, gpu), ws.numel(), _stream(dev))
+    _check(st, "luq_cross_entropy_fwd")
+    return loss, lse
+
+
+def luq_cross_entropy_bwd(dloss, x, table, targets, lse, scale=1.0, smoothing=0.0, accumulate=False, dx=None, dtable=None,
+                          ws=None):
+    """Gradients (dx in x's dtype, dtable in float32, or of the dtable passed in: bfloat16 where the table is) of
+    luq_cross_entropy_fwd, from those of the losses.  accumulate adds to the dtable passed in."""
+    gpu, T, V, D, xt, tt, it = _loss_operands(x, table, targets)
+    dev = x.device
+    dloss = _input(dloss, T, torch.float32, gpu, "dloss")
+    lse = _input(lse, T, torch.float32, gpu, "lse")
+    if dx is None:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate adds to a dtable that is passed in")
+        dtable = torch.empty(V, D, dtype=torch.float32, device=dev)
+    gt = _dtype(dtable)
+    if ws is None:
+        ws = _bytes(LIB.luq_cross_entropy_workspace(T, V, D, xt, tt, gt), dev)
+    x, table, targets = _aligned(x), _aligned(table), targets.contiguous()
+    st = LIB.luq_cross_entropy_bwd(dloss.data_ptr(), x.data_ptr(), xt, table.data_ptr(), tt, targets.data_ptr(), it,
+                                   lse.data_ptr(), T, V, D, scale, smoothing, 1 if accumulate else 0,
+                                   _buffer(dx, T * D, x.dtype, gpu, "dx"), _buffer(dtable, V * D, dtable.dtype, gpu, "dtable"), gt,
+                                   _workspace(ws, gpu), ws.numel(), _stream(dev))
+    _check(st, "luq_cross_entropy_bwd")
+    return dx, dtable
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("weight_decay", ctypes.c_float), ("lr_scale", ctypes.c_float), ("gt", ctypes.c_int),
+                ("state_bits", ctypes.c_int)]
+
+
+class AdamwPlan:
+    """The work of luq_adamw_step on the device, and the tensors it names, which it keeps alive."""
+    __slots__ = ("plan", "bytes", "count", "gpu", "tensors")
+
+    def __init__(self, plan, nbytes, count, gpu, tensors):
+        self.plan, self.bytes, self.count, self.gpu, self.tensors = plan, nbytes, count, gpu, tensors
+
+
+def luq_adamw_plan_bytes(sizes):
+    """Bytes of the plan for tensors of these numbers of elements."""
+    return int(LIB.luq_adamw_plan_bytes((ctypes.c_int64 * max(len(sizes), 1))(*sizes), len(sizes)))
+
+
+def _each(value, count, name):
+    """One value for every tensor."""
+    if value is None or isinstance(value, (int, float)):
+        return [value] * count
+    if len(value) != count:
+        raise ValueError(f"{name} must be one for each tensor")
+    return list(value)
+
+
+def luq_adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copy=None, weight_decay=0.0, lr_scale=1.0):
+    """The plan of a step over params (float32), whose gradients (float32 or bfloat16) and states keep their places.
+    m and v of a tensor are float32, or uint8 codes with m_scale and v_scale (uint8, one for 32 elements); they begin as
+    zeros.  copy: bfloat16 tensors that get the new weights too.  weight_decay and lr_scale: one for all, or a list;
+    the other lists may hold None where a tensor has none."""
+    count = len(params)
+    gpu = params[0].get_device() if count else -1
+    lists = [_each(t, count, name) for t, name in ((grads, "grads"), (m, "m"), (v, "v"), (m_scale, "m_scale"),
+                                                   (v_scale, "v_scale"), (copy, "copy"), (weight_decay, "weight_decay"),
+                                                   (lr_scale, "lr_scale"))]
+    entries = (_AdamwTensor * max(count, 1))()
+    for e, p, g, mi, vi, ms, vs, c, decay, rate in zip(entries, params, *lists):
+        n = p.numel()
+        bits = 32 if mi.dtype is torch.float32 else 8
+        state = torch.float32 if bits == 32 else torch.uint8
+        e.p = _buffer(p, n, torch.float32, gpu, "params")
+        e.g, e.gt = _buffer(g, n, g.dtype, gpu, "grads"), _dtype(g)
+        e.m, e.v = _buffer(mi, n, state, gpu, "m"), _buffer(vi, n, state, gpu, "v")
+        if bits == 8:
+            if ms is None or vs is None:
+                raise ValueError("states in 8 bits have m_scale and v_scale")
+            e.m_scale = _buffer(ms, -(-n // 32), torch.uint8, gpu, "m_scale")
+            e.v_scale = _buffer(vs, -(-n // 32), torch.uint8, gpu, "v_scale")
+        e.copy = None if c is None else _buffer(c, n, torch.bfloat16, gpu, "copy")
+        e.n, e.weight_decay, e.lr_scale, e.state_bits = n, decay, rate, bits
+    nbytes = luq_adamw_plan_bytes([p.numel() for p in params])
+    host = torch.empty(max(nbytes, 1), dtype=torch.uint8)
+    st = LIB.luq_adamw_plan(ctypes.addressof(entries), count, host.data_ptr(), nbytes)
+    _check(st, "luq_adamw_plan")
+    plan = host.to(params[0].device) if count else host
+    return AdamwPlan(plan, nbytes, count, gpu, (list(params), *lists[:6]))
+
+
+def luq_adamw_step(plan, lr, step, betas=(0.9, 0.999), eps=1e-8, seed=0, grad_scale=None):
+    """One AdamW step of the plan's tensors.  lr (float32), step (int64, from 1) and grad_scale (float32, or None for 1)
+    hold one element on the device; a grad_scale that is not finite skips the step."""
+    gpu = plan.gpu
+    if step.dtype is not torch.int64 or step.numel() != 1 or step.get_device() != gpu:
+        raise ValueError("step must be one int64 on the plan's device")
+    st = LIB.luq_adamw_step(plan.plan.data_ptr(), plan.bytes, plan.count, _scalar(lr, gpu, "lr"), step.data_ptr(), betas[0],
+                            betas[1], eps, None if grad_scale is None else _scalar(grad_scale, gpu, "grad_scale"),
+                            seed & (2**64 - 1), _stream(lr.device))
+    _check(st, "luq_adamw_step")

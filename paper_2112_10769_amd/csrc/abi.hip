@@ -641,4 +641,202 @@ luq_status luq_gemm_wgrad_grouped(const uint8_t* g_codes_t, const float* alpha, 
                                               experts, T, Nout, Kin, dw, ws, static_cast<hipStream_t>(stream)));
 }
 
+// ---- choice of experts
+
+static luq_status route_checks(const char* fn, luq_dtype dt, int64_t T, int64_t experts, int64_t top_k, luq_score score,
+                               int renorm, float scale) {
+  const luq_status st = check_types(fn, dt, dt);
+  if (st != LUQ_OK) return st;
+  if (T < 0 || T > kMaxIds || experts < 1 || experts > kMaxExperts)
+    return fail(LUQ_ERR_SHAPE, "%s: T in [0, 2^28], experts in [1, 4096]", fn);
+  if (top_k < 1 || top_k > 64 || top_k > experts) return fail(LUQ_ERR_SHAPE, "%s: top_k in [1, 64], at most experts", fn);
+  if (score != LUQ_SOFTMAX && score != LUQ_SIGMOID) return fail(LUQ_ERR_PARAM, "%s: score", fn);
+  if (renorm != 0 && renorm != 1) return fail(LUQ_ERR_PARAM, "%s: renorm must be 0 or 1", fn);
+  if (!(scale > -__builtin_inff() && scale < __builtin_inff())) return fail(LUQ_ERR_PARAM, "%s: scale must be finite", fn);
+  return LUQ_OK;
+}
+
+luq_status luq_route_fwd(const void* logits, luq_dtype dt, int64_t T, int64_t experts, int64_t top_k, luq_score score,
+                         const float* bias, int64_t groups, int64_t top_groups, int group_best, int renorm,
+                         float scale, int32_t* chosen, float* weights, void* stream) {
+  const char* fn = "luq_route_fwd";
+  g_last_error[0] = 0;
+  const luq_status st = route_checks(fn, dt, T, experts, top_k, score, renorm, scale);
+  if (st != LUQ_OK) return st;
+  if (groups < 1 || groups > 64 || experts % groups || top_groups < 1 || top_groups > groups ||
+      top_k > top_groups * (experts / groups))
+    return fail(LUQ_ERR_SHAPE, "%s: groups in [1, 64] divides experts, top_groups of them hold top_k experts", fn);
+  if (group_best != 1 && group_best != 2) return fail(LUQ_ERR_PARAM, "%s: group_best must be 1 or 2", fn);
+  if (T == 0) return LUQ_OK;
+  if (!logits || !chosen || !weights) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned_to(logits, elem_size(dt)) || !aligned4(bias) || !aligned4(chosen) || !aligned4(weights))
+    return fail(LUQ_ERR_ALIGN, "%s: a tensor is misaligned", fn);
+  const luq::RouteArgs a{logits, bias, T, (int)experts, (int)top_k, (int)groups, (int)top_groups, group_best, renorm,
+                         score == LUQ_SIGMOID, scale};
+  return hip_status(luq::launch_route_fwd(a, dt == LUQ_BF16, chosen, weights, static_cast<hipStream_t>(stream)));
+}
+
+luq_status luq_route_bwd(const float* dweights, const void* logits, luq_dtype dt, const int32_t* chosen, int64_t T,
+                         int64_t experts, int64_t top_k, luq_score score, int renorm, float scale, void* dlogits,
+                         void* stream) {
+  const char* fn = "luq_route_bwd";
+  g_last_error[0] = 0;
+  const luq_status st = route_checks(fn, dt, T, experts, top_k, score, renorm, scale);
+  if (st != LUQ_OK) return st;
+  if (T == 0) return LUQ_OK;
+  if (!dweights || !logits || !chosen || !dlogits) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned4(dweights) || !aligned_to(logits, elem_size(dt)) || !aligned4(chosen) || !aligned_to(dlogits, elem_size(dt)))
+    return fail(LUQ_ERR_ALIGN, "%s: a tensor is misaligned", fn);
+  const luq::RouteArgs a{logits, nullptr, T, (int)experts, (int)top_k, 1, 1, 1, renorm, score == LUQ_SIGMOID, scale};
+  return hip_status(luq::launch_route_bwd(a, dt == LUQ_BF16, dweights, chosen, dlogits, static_cast<hipStream_t>(stream)));
+}
+
+// ---- cross entropy
+
+static bool cross_entropy_sizes(int64_t T, int64_t V, int64_t D) {
+  const int64_t most = (int64_t)1 << 36;
+  return T >= 0 && T <= ((int64_t)1 << 21) && V >= 1 && V <= kMaxIds && D >= 1 && D <= ((int64_t)1 << 17) &&
+         T * V <= 2 * most && T * D <= most && V * D <= most;
+}
+
+size_t luq_cross_entropy_workspace(int64_t T, int64_t V, int64_t D, luq_dtype xt, luq_dtype tt, int gt) {
+  if (!cross_entropy_sizes(T, V, D) || (xt != LUQ_F32 && xt != LUQ_BF16) || (tt != LUQ_F32 && tt != LUQ_BF16) || T == 0) return 0;
+  if (gt < 0) return luq::cross_entropy_fwd_workspace_bytes(T, V, D, xt == LUQ_BF16, tt == LUQ_BF16);
+  if (gt != LUQ_F32 && (gt != LUQ_BF16 || tt != LUQ_BF16)) return 0;
+  return luq::cross_entropy_bwd_workspace_bytes(T, V, D, xt == LUQ_BF16, tt == LUQ_BF16, gt == LUQ_BF16);
+}
+
+static luq_status cross_entropy_checks(const char* fn, luq_dtype xt, luq_dtype tt, luq_index it, int64_t T, int64_t V,
+                                       int64_t D, float scale, float smoothing) {
+  luq_status st = check_types(fn, xt, tt);
+  if (st == LUQ_OK) st = check_index(fn, it);
+  if (st != LUQ_OK) return st;
+  if (!cross_entropy_sizes(T, V, D))
+    return fail(LUQ_ERR_SHAPE, "%s: T in [0, 2^21], V in [1, 2^28], D in [1, 2^17], T*V up to 2^37, T*D and V*D up to 2^36", fn);
+  if (!(scale > -__builtin_inff() && scale < __builtin_inff())) return fail(LUQ_ERR_PARAM, "%s: scale must be finite", fn);
+  if (!(smoothing >= 0.0f && smoothing <= 1.0f)) return fail(LUQ_ERR_PARAM, "%s: smoothing must be in [0, 1]", fn);
+  return LUQ_OK;
+}
+
+luq_status luq_cross_entropy_fwd(const void* x, luq_dtype xt, const void* table, luq_dtype tt, const void* targets,
+                                 luq_index it, int64_t T, int64_t V, int64_t D, float scale, float smoothing,
+                                 float* loss, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "luq_cross_entropy_fwd";
+  g_last_error[0] = 0;
+  luq_status st = cross_entropy_checks(fn, xt, tt, it, T, V, D, scale, smoothing);
+  if (st != LUQ_OK) return st;
+  if (T == 0) return LUQ_OK;
+  if (!x || !table || !targets || !loss || !lse) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned16(x) || !aligned16(table)) return fail(LUQ_ERR_ALIGN, "%s: x and table must be 16-byte aligned", fn);
+  if (!aligned_to(targets, it == LUQ_I64 ? 8 : 4) || !aligned4(loss) || !aligned4(lse))
+    return fail(LUQ_ERR_ALIGN, "%s: targets, loss or lse misaligned", fn);
+  st = check_workspace(fn, luq_cross_entropy_workspace(T, V, D, xt, tt, -1), ws, ws_bytes);
+  if (st != LUQ_OK) return st;
+  const luq::CrossEntropyArgs a{x, table, targets, xt == LUQ_BF16, tt == LUQ_BF16, it == LUQ_I64, T, V, D, scale, smoothing};
+  return hip_status(luq::launch_cross_entropy_fwd(a, loss, lse, ws, static_cast<hipStream_t>(stream)));
+}
+
+luq_status luq_cross_entropy_bwd(const float* dloss, const void* x, luq_dtype xt, const void* table, luq_dtype tt,
+                                 const void* targets, luq_index it, const float* lse, int64_t T, int64_t V, int64_t D,
+                                 float scale, float smoothing, int accumulate, void* dx, void* dtable, luq_dtype gt,
+                                 void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "luq_cross_entropy_bwd";
+  g_last_error[0] = 0;
+  luq_status st = cross_entropy_checks(fn, xt, tt, it, T, V, D, scale, smoothing);
+  if (st == LUQ_OK) st = check_types(fn, gt, gt);
+  if (st != LUQ_OK) return st;
+  if (gt == LUQ_BF16 && tt != LUQ_BF16) return fail(LUQ_ERR_DTYPE, "%s: an fp32 table has an fp32 gradient", fn);
+  if (accumulate != 0 && accumulate != 1) return fail(LUQ_ERR_PARAM, "%s: accumulate must be 0 or 1", fn);
+  if (!dtable || (T > 0 && (!dloss || !x || !table || !targets || !lse || !dx))) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned16(x) || !aligned16(table)) return fail(LUQ_ERR_ALIGN, "%s: x and table must be 16-byte aligned", fn);
+  if (!aligned_to(targets, it == LUQ_I64 ? 8 : 4) || !aligned4(dloss) || !aligned4(lse) || !aligned_to(dx, elem_size(xt)) ||
+      !aligned_to(dtable, T > 0 ? elem_size(gt) : 4))
+    return fail(LUQ_ERR_ALIGN, "%s: a tensor is misaligned", fn);
+  st = check_workspace(fn, luq_cross_entropy_workspace(T, V, D, xt, tt, gt), ws, ws_bytes);
+  if (st != LUQ_OK) return st;
+  const luq::CrossEntropyArgs a{x, table, targets, xt == LUQ_BF16, tt == LUQ_BF16, it == LUQ_I64, T, V, D, scale, smoothing};
+  return hip_status(luq::launch_cross_entropy_bwd(a, dloss, lse, accumulate, dx, dtable, gt == LUQ_BF16, ws,
+                                                  static_cast<hipStream_t>(stream)));
+}
+
+// ---- AdamW
+
+// Chunks of a plan's tensors; -1 if refused.
+static int64_t adamw_chunks(const int64_t* n, int64_t count, int64_t stride) {
+  if (!n || count < 0 || count > ((int64_t)1 << 20)) return -1;
+  const int64_t most = (int64_t)1 << 35;
+  int64_t total = 0, chunks = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    const int64_t k = *reinterpret_cast<const int64_t*>(reinterpret_cast<const char*>(n) + i * stride);
+    if (k < 0 || k > most) return -1;
+    total += k;
+    chunks += (k + luq::kAdamwChunk - 1) / luq::kAdamwChunk;
+    if (total > most) return -1;
+  }
+  return chunks;
+}
+
+static size_t adamw_bytes(int64_t count, int64_t chunks) {
+  return chunks > 0 ? (size_t)count * sizeof(luq::AdamwEntry) + (size_t)chunks * sizeof(luq::AdamwChunk) : 0;
+}
+
+size_t luq_adamw_plan_bytes(const int64_t* n, int64_t count) {
+  return adamw_bytes(count, adamw_chunks(n, count, sizeof(int64_t)));
+}
+
+luq_status luq_adamw_plan(const luq_adamw_tensor* tensors, int64_t count, void* plan, size_t plan_bytes) {
+  const char* fn = "luq_adamw_plan";
+  g_last_error[0] = 0;
+  if (!tensors && count > 0) return fail(LUQ_ERR_NULL, "%s: tensors is NULL", fn);
+  const int64_t chunks = count > 0 ? adamw_chunks(&tensors->n, count, sizeof(luq_adamw_tensor)) : (count == 0 ? 0 : -1);
+  if (chunks < 0) return fail(LUQ_ERR_SHAPE, "%s: at most 2^20 tensors, of 2^35 elements together", fn);
+  for (int64_t i = 0; i < count; ++i) {
+    const luq_adamw_tensor& t = tensors[i];
+    if (t.gt != LUQ_F32 && t.gt != LUQ_BF16) return fail(LUQ_ERR_DTYPE, "%s: gradient's type", fn);
+    if (t.state_bits != 32 && t.state_bits != 8) return fail(LUQ_ERR_PARAM, "%s: state_bits must be 32 or 8", fn);
+    const float inf = __builtin_inff();
+    if (!(t.weight_decay > -inf && t.weight_decay < inf && t.lr_scale > -inf && t.lr_scale < inf))
+      return fail(LUQ_ERR_PARAM, "%s: weight_decay and lr_scale must be finite", fn);
+    const bool codes = t.state_bits == 8;
+    if (t.n > 0 && (!t.p || !t.g || !t.m || !t.v || (codes && (!t.m_scale || !t.v_scale))))
+      return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+    if (!aligned4(t.p) || !aligned_to(t.g, t.gt == LUQ_F32 ? 4 : 2) || !aligned_to(t.copy, 2) ||
+        (!codes && (!aligned4(t.m) || !aligned4(t.v))))
+      return fail(LUQ_ERR_ALIGN, "%s: a tensor is misaligned", fn);
+  }
+  if (plan_bytes != adamw_bytes(count, chunks)) return fail(LUQ_ERR_WORKSPACE, "%s: plan_bytes is not luq_adamw_plan_bytes", fn);
+  if (chunks == 0) return LUQ_OK;
+  if (!plan) return fail(LUQ_ERR_NULL, "%s: plan is NULL", fn);
+  if (!aligned_to(plan, 8)) return fail(LUQ_ERR_ALIGN, "%s: plan must be 8-byte aligned", fn);
+  luq::AdamwEntry* const entries = static_cast<luq::AdamwEntry*>(plan);
+  luq::AdamwChunk* chunk = reinterpret_cast<luq::AdamwChunk*>(entries + count);
+  for (int64_t i = 0; i < count; ++i) {
+    const luq_adamw_tensor& t = tensors[i];
+    entries[i] = {t.p, t.g, t.m, t.v, t.m_scale, t.v_scale, static_cast<uint16_t*>(t.copy), t.n, t.weight_decay, t.lr_scale,
+                  t.gt == LUQ_BF16, t.state_bits};
+    for (int64_t c = 0; c * luq::kAdamwChunk < t.n; ++c) *chunk++ = {(uint32_t)i, (uint32_t)c};
+  }
+  return LUQ_OK;
+}
+
+luq_status luq_adamw_step(const void* plan, size_t plan_bytes, int64_t count, const float* lr, const int64_t* step,
+                          double beta1, double beta2, float eps, const float* grad_scale, uint64_t seed, void* stream) {
+  const char* fn = "luq_adamw_step";
+  g_last_error[0] = 0;
+  if (count < 0 || count > ((int64_t)1 << 20)) return fail(LUQ_ERR_SHAPE, "%s: count in [0, 2^20]", fn);
+  if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return fail(LUQ_ERR_PARAM, "%s: betas must be in [0, 1)", fn);
+  if (!(eps >= 0.0f && eps < __builtin_inff())) return fail(LUQ_ERR_PARAM, "%s: eps must be finite and >= 0", fn);
+  if (plan_bytes == 0) return LUQ_OK;
+  const size_t entries = (size_t)count * sizeof(luq::AdamwEntry);
+  if (plan_bytes <= entries || (plan_bytes - entries) % sizeof(luq::AdamwChunk))
+    return fail(LUQ_ERR_WORKSPACE, "%s: plan_bytes is not luq_adamw_plan_bytes", fn);
+  const int64_t chunks = (int64_t)((plan_bytes - entries) / sizeof(luq::AdamwChunk));
+  if (chunks > ((int64_t)1 << 23) + count) return fail(LUQ_ERR_SHAPE, "%s: the plan has too many elements", fn);
+  if (!plan || !lr || !step) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
+  if (!aligned16(plan) || !aligned4(lr) || !aligned_to(step, 8) || !aligned4(grad_scale))
+    return fail(LUQ_ERR_ALIGN, "%s: plan must be 16-byte aligned, the scalars to their types", fn);
+  return hip_status(luq::launch_adamw(plan, count, chunks, lr, step, beta1, beta2, eps, grad_scale, seed,
+                                      static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

@@ -1,0 +1,708 @@
+// Softmax cross entropy of the last layer, the logits not kept, and its gradients.
+//
+//   z_tv = scale x_t . W_v,  lse_t = log sum_v exp z_tv
+//   loss_t = lse_t - (1 - eps) z_t,target - eps / V sum_v z_tv
+//   g_tv = dloss_t scale (exp(z_tv - lse_t) - (1 - eps) [v = target] - eps / V),  dx = g W,  dW = g^T x
+//
+// Forward: a tile of products leaves each row's maximum, sum of exponentials and sum of logits over
+// its columns; a second launch joins them.  Backward: a piece of the vocabulary at a time, the
+// products again, their gradient g in bf16 (in both orders), and the two products with it.  All four
+// products are the K-major tile of bf16_tile.hpp; operands that lie otherwise are laid out first.
+//
+// g in bf16 is what a bf16 product takes; its rounding is of the size of a bf16 output's own.  An
+// fp32 output takes two bf16 terms of g with bf16 activations, three with fp32 ones.
+#include <type_traits>
+
+#include "bf16_tile.hpp"
+#include "luq_launch.hpp"
+
+namespace luq {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+
+__device__ __forceinline__ int64_t target_of(const void* targets, int i64, int64_t t) {
+  return i64 ? static_cast<const int64_t*>(targets)[t] : static_cast<const int32_t*>(targets)[t];
+}
+
+// Terms of v: bf16 numbers whose sum it is to 8 bits a term.  What is not finite has one term.
+template <int N>
+__device__ __forceinline__ void terms(float v, uint16_t (&h)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint16_t b = from_f32<uint16_t>(v);
+    if ((b & 0x7FFF) == 0x7F80 && fabsf(v) < __builtin_inff()) b -= 1;   // not rounded up to infinity
+    h[i] = b;
+    const float rest = v - to_f32(b);
+    v = fabsf(v) < __builtin_inff() ? rest : 0.0f;
+  }
+}
+
+typedef uint32_t v4w __attribute__((ext_vector_type(4)));
+
+// N terms of eight elements, 16 bytes a term.
+template <int N>
+__device__ __forceinline__ void terms8(const float (&v)[8], v4w (&w)[N]) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) {
+    uint16_t a[N], b[N];
+    terms<N>(v[k], a);
+    terms<N>(v[k + 1], b);
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i][k / 2] = (uint32_t)a[i] | (uint32_t)b[i] << 16;
+  }
+}
+
+// ---- operands laid out: terms of a matrix, its rows a multiple of eight long, or its transpose
+
+struct PackArgs {
+  const void* src;      // [rows][cols]
+  int64_t rows, cols;
+  const void* targets;  // rows whose target is not in [0, vocab) become 0, or NULL
+  int i64;
+  int64_t vocab;
+  uint16_t* out;
+  int64_t ld, plane;
+  __device__ __forceinline__ bool kept(int64_t row) const {
+    if (!targets) return true;
+    const int64_t y = target_of(targets, i64, row);
+    return y >= 0 && y < vocab;
+  }
+};
+
+template <typename T, int N>
+__global__ __launch_bounds__(256) void pack_rows_kernel(PackArgs a) {
+  const int64_t pieces = a.ld / 8;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < a.rows * pieces; at += (int64_t)gridDim.x * 256) {
+    const int64_t row = at / pieces, c = (at - row * pieces) * 8;
+    float v[8];
+    if (a.kept(row)) load_row<8>(static_cast<const T*>(a.src) + row * a.cols + c, a.cols - c, v);
+    else
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+    v4w w[N];
+    terms8<N>(v, w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<v4w*>(a.out + i * a.plane + row * a.ld + c) = w[i];
+  }
+}
+
+// [cols][ld], ld at least rows: 64 x 64 elements a workgroup.
+template <typename T, int N>
+__global__ __launch_bounds__(256) void pack_cols_kernel(PackArgs a) {
+  __shared__ float tile[64][65];
+  const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int at = threadIdx.x + u * 256, row = at / 8, c = (at & 7) * 8;
+    float v[8];
+    const bool in = r0 + row < a.rows && c0 + c < a.cols;
+    if (in && a.kept(r0 + row)) load_row<8>(static_cast<const T*>(a.src) + (r0 + row) * a.cols + c0 + c, a.cols - c0 - c, v);
+    else
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tile[row][c + k] = v[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int at = threadIdx.x + u * 256, c = at / 8, row = (at & 7) * 8;
+    if (c0 + c >= a.cols || r0 + row >= a.ld) continue;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = tile[row + k][c];
+    v4w w[N];
+    terms8<N>(v, w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<v4w*>(a.out + i * a.plane + (c0 + c) * a.ld + r0 + row) = w[i];
+  }
+}
+
+// ---- the products
+
+using Tile = Bf16Tile<2, 2, 2, 2, 64, 2>;
+
+// Where a lane's sums lie: row `row(i)` of the matrix, columns col(j, q) .. + 3 in registers 4q .. 4q + 3.
+struct Lane {
+  int64_t row0, col0;
+  __device__ __forceinline__ Lane(int64_t m0, int64_t n0) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    row0 = m0 + (wave / Tile::WN) * Tile::TM * 32 + (lane & 31);
+    col0 = n0 + (wave % Tile::WN) * Tile::TN * 32 + 4 * (lane >> 5);
+  }
+  __device__ __forceinline__ int64_t row(int i) const { return row0 + i * 32; }
+  __device__ __forceinline__ int64_t col(int j, int q) const { return col0 + j * 32 + 8 * q; }
+};
+
+struct LossArgs {
+  const void* targets;
+  int i64;
+  int64_t T, V;
+  float scale;
+  float* part;     // [column parts][3][T]: maximum (times log2 e), sum of exponentials, sum of logits
+  float* at_target;
+};
+
+__global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g, LossArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Tile::kLds];
+  int tm, tn;
+  bf16_tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * Tile::BM, n0 = (int64_t)tn * Tile::BN;
+  Tile tile;
+  tile.run(g, m0, n0, 0, g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK), lds);
+  const Lane at(m0, n0);
+  const float log2_scale = a.scale * kLog2e;
+  const bool whole = n0 + Tile::BN <= a.V;
+  const int64_t part = (int64_t)tn * Tile::WN + (threadIdx.x >> 6) % Tile::WN;
+#pragma unroll
+  for (int i = 0; i < Tile::TM; ++i) {
+    const int64_t row = at.row(i);
+    const int64_t y = row < a.T ? target_of(a.targets, a.i64, row) : -1;
+    float top = -3.0e38f, sum = 0.0f, all = 0.0f;
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const bool in = whole || at.col(j, e / 4) + e % 4 < a.V;
+        const float z = tile.acc[i][j][e];
+        if (at.col(j, e / 4) + e % 4 == y) a.at_target[row] = z * a.scale;
+        all += in ? z : 0.0f;
+        tile.acc[i][j][e] = in ? z * log2_scale : -__builtin_inff();
+        top = fmaxf(top, tile.acc[i][j][e]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(tile.acc[i][j][e] - top);
+    sum += __shfl_xor(sum, 32, kWave);
+    all += __shfl_xor(all, 32, kWave);
+    if ((threadIdx.x & 32) == 0 && row < a.T) {
+      float* const out = a.part + part * 3 * a.T + row;
+      out[0] = top;
+      out[a.T] = sum;
+      out[2 * a.T] = all * a.scale;
+    }
+  }
+}
+
+// The rows' parts joined: 64 rows a workgroup, its 16 waves every 16th part.
+__global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t parts, float smoothing, float* __restrict__ loss,
+                                                         float* __restrict__ lse) {
+  __shared__ float red[3][16][kWave];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * kWave + lane;
+  float top = -3.0e38f, sum = 0.0f, all = 0.0f;
+  if (row < a.T) {
+    constexpr int U = 4;
+    for (int64_t p = wave; p < parts; p += 16 * U) {
+      float m[U], s[U], z[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t q = p + 16 * u;
+        const float* const src = a.part + (q < parts ? q : p) * 3 * a.T + row;
+        m[u] = q < parts ? src[0] : -3.0e38f;
+        s[u] = q < parts ? src[a.T] : 0.0f;
+        z[u] = q < parts ? src[2 * a.T] : 0.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float next = fmaxf(top, m[u]);
+        sum = sum * __builtin_amdgcn_exp2f(top - next) + s[u] * __builtin_amdgcn_exp2f(m[u] - next);
+        top = next;
+        all += z[u];
+      }
+    }
+  }
+  red[0][wave][lane] = top;
+  red[1][wave][lane] = sum;
+  red[2][wave][lane] = all;
+  __syncthreads();
+  if (wave != 0 || row >= a.T) return;
+  float most = top;
+  for (int w = 1; w < 16; ++w) most = fmaxf(most, red[0][w][lane]);
+  sum = all = 0.0f;
+  for (int w = 0; w < 16; ++w) {
+    sum += red[1][w][lane] * __builtin_amdgcn_exp2f(red[0][w][lane] - most);
+    all += red[2][w][lane];
+  }
+  const int64_t y = target_of(a.targets, a.i64, row);
+  const bool kept = y >= 0 && y < a.V;
+  const float l = most * kLn2 + logf(sum);
+  lse[row] = kept ? l : 0.0f;
+  loss[row] = y < 0     ? 0.0f
+              : !kept   ? __builtin_nanf("")
+              : smoothing > 0.0f ? l - (1.0f - smoothing) * a.at_target[row] - smoothing / (float)a.V * all
+                                 : l - a.at_target[row];
+}
+
+// ---- backward
+
+// A slab of a wave's sums in LDS: 32 rows of its columns in fp32, from which both orders are read
+// in pieces of eight.
+constexpr int kSlabCols = Tile::TN * 32, kSlabPitch = kSlabCols + 4;
+static_assert((size_t)Tile::WM * Tile::WN * 32 * kSlabPitch * 4 <= (size_t)Tile::kLds, "slabs fit in the stages' place");
+
+struct Slab {
+  float* e;
+  __device__ __forceinline__ explicit Slab(uint8_t* lds) {
+    e = reinterpret_cast<float*>(lds) + (threadIdx.x >> 6) * 32 * kSlabPitch;
+  }
+  __device__ __forceinline__ void put(int j, int q, const float (&v)[4]) {
+    const int lane = threadIdx.x & 63;
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<f4*>(e + (lane & 31) * kSlabPitch + j * 32 + 8 * q + 4 * (lane >> 5)) = f4{v[0], v[1], v[2], v[3]};
+  }
+  __device__ __forceinline__ void row8(int row, int c, float (&v)[8]) const { load_pack(e + row * kSlabPitch + c, v); }
+  __device__ __forceinline__ void col8(int row, int c, float (&v)[8]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = e[(row + k) * kSlabPitch + c];
+  }
+};
+
+struct GradArgs {
+  const void* targets;
+  int i64;
+  int64_t T, V;        // V: of the whole table
+  int64_t v0, cols;    // the piece: its first row of the table, and how many
+  float scale, smoothing;
+  const float* dloss;
+  const float* lse;
+  uint16_t* g;         // [row_terms][T][ld_g]: columns up to the next multiple of eight are written
+  int64_t ld_g, plane_g;
+  uint16_t* gt;        // [col_terms][cols][ld_t]: ld_t is T's next multiple of eight
+  int64_t ld_t, plane_t;
+  int row_terms, col_terms;
+};
+
+template <int N>
+__device__ __forceinline__ void store_terms(const float (&v)[8], uint16_t* p, int64_t plane) {
+  v4w w[N];
+  terms8<N>(v, w);
+#pragma unroll
+  for (int i = 0; i < N; ++i) *reinterpret_cast<v4w*>(p + i * plane) = w[i];
+}
+__device__ __forceinline__ void store_terms(int n, const float (&v)[8], uint16_t* p, int64_t plane) {
+  if (n == 1) store_terms<1>(v, p, plane);
+  else if (n == 2) store_terms<2>(v, p, plane);
+  else store_terms<3>(v, p, plane);
+}
+
+__global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g, GradArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Tile::kLds];
+  int tm, tn;
+  bf16_tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * Tile::BM, n0 = (int64_t)tn * Tile::BN;
+  Tile tile;
+  tile.run(g, m0, n0, 0, g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK), lds);
+  const Lane at(m0, n0);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t rows0 = m0 + (wave / Tile::WN) * Tile::TM * 32, cols0 = n0 + (wave % Tile::WN) * kSlabCols;
+  const float each = a.smoothing / (float)a.V;
+  Slab slab(lds);
+#pragma unroll
+  for (int i = 0; i < Tile::TM; ++i) {
+    const int64_t row = at.row(i);
+    const int64_t y = row < a.T ? target_of(a.targets, a.i64, row) : -1;
+    const bool kept = y >= 0 && y < a.V;
+    const float up = kept ? a.dloss[row] * a.scale : 0.0f, base = kept ? a.lse[row] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t c = at.col(j, q) + k;
+          // the difference first: near the maximum it is exact
+          float p = __builtin_amdgcn_exp2f(fmaf(tile.acc[i][j][4 * q + k], a.scale, -base) * kLog2e) - each;
+          if (a.v0 + c == y) p -= 1.0f - a.smoothing;
+          v[k] = kept && c < a.cols ? p * up : 0.0f;
+        }
+        slab.put(j, q, v);
+      }
+    // in the order of the rows, and transposed
+#pragma unroll
+    for (int u = 0; u < 32 * kSlabCols / 8 / 64; ++u) {
+      const int item = lane + u * 64, r = item / (kSlabCols / 8), c = item % (kSlabCols / 8) * 8;
+      const int64_t gr = rows0 + i * 32 + r, gc = cols0 + c;
+      if (gr < a.T && gc < a.cols) {
+        float v[8];
+        slab.row8(r, c, v);
+        store_terms(a.row_terms, v, a.g + gr * a.ld_g + gc, a.plane_g);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 32 * kSlabCols / 8 / 64; ++u) {
+      const int item = lane + u * 64, c = item / 4, r = item % 4 * 8;
+      const int64_t gr = rows0 + i * 32 + r, gc = cols0 + c;
+      if (gr < a.T && gc < a.cols) {
+        float v[8];
+        slab.col8(r, c, v);
+        store_terms(a.col_terms, v, a.gt + gc * a.ld_t + gr, a.plane_t);
+      }
+    }
+  }
+}
+
+// Where a product's sums go: partial sums (fp32, one matrix a split, added to when `add`), or an
+// output of type fp32 or bf16, added to when `add`; `before` (fp32) is added too.
+struct OutArgs {
+  int64_t M, N;
+  float* part;
+  void* out;
+  int bf16, add;
+  const void* targets;   // rows whose target is not in [0, vocab) become 0, or NULL
+  int i64;
+  int64_t vocab;
+  int chunk;             // stages of a split
+  __device__ __forceinline__ bool kept(int64_t row) const {
+    if (!targets) return true;
+    const int64_t y = target_of(targets, i64, row);
+    return y >= 0 && y < vocab;
+  }
+  template <typename T>
+  __device__ __forceinline__ void put(int64_t row, int64_t col, float (&v)[8]) const {
+    T* const p = static_cast<T*>(out) + row * N + col;
+    if (add) {
+      float old[8];
+      load_row<8>(p, N - col, old);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += old[k];
+    }
+    if (!kept(row))
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+    store_row<8>(p, N - col, v);
+  }
+};
+
+__global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g, OutArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Tile::kLds];
+  int tm, tn;
+  bf16_tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * Tile::BM, n0 = (int64_t)tn * Tile::BN;
+  const int stages = g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK);
+  const int beg = blockIdx.y * a.chunk, end = min(beg + a.chunk, stages);
+  Tile tile;
+  tile.run(g, m0, n0, beg, end, lds);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t rows0 = m0 + (wave / Tile::WN) * Tile::TM * 32, cols0 = n0 + (wave % Tile::WN) * kSlabCols;
+  Slab slab(lds);
+#pragma unroll
+  for (int i = 0; i < Tile::TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < Tile::TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float v[4] = {tile.acc[i][j][4 * q], tile.acc[i][j][4 * q + 1], tile.acc[i][j][4 * q + 2], tile.acc[i][j][4 * q + 3]};
+        slab.put(j, q, v);
+      }
+#pragma unroll
+    for (int u = 0; u < 32 * kSlabCols / 8 / 64; ++u) {
+      const int item = lane + u * 64, r = item / (kSlabCols / 8), c = item % (kSlabCols / 8) * 8;
+      const int64_t row = rows0 + i * 32 + r, col = cols0 + c;
+      if (row >= a.M || col >= a.N) continue;
+      float v[8];
+      slab.row8(r, c, v);
+      if (a.part) {
+        float* const p = a.part + ((int64_t)blockIdx.y * a.M + row) * a.N + col;
+        if (a.add) {
+          float old[8];
+          load_row<8>(p, a.N - col, old);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] += old[k];
+        }
+        store_row<8>(p, a.N - col, v);
+      } else if (a.bf16) {
+        a.put<uint16_t>(row, col, v);
+      } else {
+        a.put<float>(row, col, v);
+      }
+    }
+  }
+}
+
+// The splits' sums, in order, to the output.
+__global__ __launch_bounds__(256) void out_join_kernel(OutArgs a, const float* __restrict__ part, int splits) {
+  const int64_t pieces = (a.N + 7) / 8;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < a.M * pieces; at += (int64_t)gridDim.x * 256) {
+    const int64_t row = at / pieces, col = (at - row * pieces) * 8;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int s = 0; s < splits; ++s) {
+      float w[8];
+      load_row<8>(part + ((int64_t)s * a.M + row) * a.N + col, a.N - col, w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += w[k];
+    }
+    if (a.bf16) a.put<uint16_t>(row, col, v);
+    else a.put<float>(row, col, v);
+  }
+}
+
+// ---- host side
+
+int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// All pairs of na and nb terms whose product is not below 2^-24 of the largest; the smallest
+// first, while the sums are small (1000 tokens of 510 columns in fp32: 2.4e-6 off with the
+// largest first).
+PlanePairs pairs_of(int na, int nb) {
+  PlanePairs p{0, 0, 0};
+  for (int sum = 2; sum >= 0; --sum)
+    for (int i = 0; i < na; ++i) {
+      const int j = sum - i;
+      if (j < 0 || j >= nb) continue;
+      p.a |= (uint32_t)i << (4 * p.count);
+      p.b |= (uint32_t)j << (4 * p.count);
+      ++p.count;
+    }
+  return p;
+}
+
+// Splits of a reduction of `stages` stages over `tiles` tiles: enough for two workgroups a CU, of
+// four stages at least.
+int splits_of(int64_t tiles, int64_t stages) {
+  if (tiles >= 256) return 1;
+  int64_t s = ceil_div(512, tiles);
+  if (s > stages / 4) s = stages / 4;
+  if (s > 64) s = 64;
+  return s < 1 ? 1 : (int)s;
+}
+
+struct Carver {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t p = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return p;
+  }
+};
+
+// How a call is laid out; the same for its workspace query and its launches.
+struct Layout {
+  int64_t T, V, D, T8, D8;
+  int xn, tn;                 // terms of x and the table
+  bool pack_x, pack_t;        // laid out in rows: fp32, or rows that are no whole 16-byte pieces
+  size_t x_rows, t_rows;      // offsets in the workspace
+  // forward
+  int64_t parts;
+  size_t part, at_target;
+  // backward
+  int64_t piece, pieces;
+  int g_rows, g_cols;         // terms of g in the product for dx, and in that for dtable
+  int tx, xt;                 // terms of the table and of x in these products
+  int splits_x, splits_w;
+  size_t x_cols, t_cols, g, gt, sum_x, sum_w;
+  bool sums_x;
+  size_t bytes;
+  Layout(int64_t T_, int64_t V_, int64_t D_, int x_bf16, int t_bf16) : T(T_), V(V_), D(D_), T8(up8(T_)), D8(up8(D_)) {
+    xn = x_bf16 ? 1 : 3;
+    tn = t_bf16 ? 1 : 3;
+    pack_x = !x_bf16 || (D & 7);
+    pack_t = !t_bf16 || (D & 7);
+    x_rows = c.take(pack_x ? (size_t)xn * T * D8 * 2 : 0);
+    t_rows = c.take(pack_t ? (size_t)tn * V * D8 * 2 : 0);
+  }
+  void forward() {
+    parts = ceil_div(V, Tile::BN) * Tile::WN;
+    part = c.take((size_t)parts * 3 * T * sizeof(float));
+    at_target = c.take((size_t)T * sizeof(float));
+    bytes = c.at;
+  }
+  // The piece: g of 2^27 elements (256 MiB in each order and term), a thousand columns at least.
+  void backward(int x_bf16, int g_bf16) {
+    int64_t most = ((int64_t)1 << 27) / (T > 0 ? T : 1) & ~(int64_t)127;
+    if (most < 1024) most = 1024;
+    if (most > (int64_t)1 << 21) most = (int64_t)1 << 21;   // a tile's rows lie within 32-bit offsets
+    const int64_t all = ceil_div(V, 128) * 128;
+    if (most > all) most = all;
+    pieces = ceil_div(V, most);
+    piece = ceil_div(ceil_div(V, pieces), 128) * 128;
+    pieces = ceil_div(V, piece);
+    g_rows = x_bf16 ? 1 : 3;
+    tx = x_bf16 && tn > 2 ? 2 : tn;
+    g_cols = g_bf16 ? 1 : x_bf16 ? 2 : 3;
+    xt = g_bf16 && xn > 2 ? 2 : xn;
+    splits_x = splits_of(ceil_div(T, Tile::BM) * ceil_div(D, Tile::BN),
+                         pairs_of(g_rows, tx).count * ceil_div(piece, Tile::BK));
+    splits_w = splits_of(ceil_div(piece < V ? piece : V, Tile::BM) * ceil_div(D, Tile::BN),
+                         pairs_of(g_cols, xt).count * ceil_div(T8, Tile::BK));
+    x_cols = c.take((size_t)xt * D * T8 * 2);
+    t_cols = c.take((size_t)tx * D * piece * 2);
+    g = c.take((size_t)g_rows * T * piece * 2);
+    gt = c.take((size_t)g_cols * piece * T8 * 2);
+    sums_x = splits_x > 1 || pieces > 1;
+    sum_x = c.take(sums_x ? (size_t)splits_x * T * D * sizeof(float) : 0);
+    sum_w = c.take(splits_w > 1 ? (size_t)splits_w * piece * D * sizeof(float) : 0);
+    bytes = c.at;
+  }
+
+ private:
+  Carver c;
+};
+
+template <typename F>
+void with_terms(int bf16, int n, F f) {
+  if (bf16) f(uint16_t{}, std::integral_constant<int, 1>{});
+  else if (n == 2) f(float{}, std::integral_constant<int, 2>{});
+  else f(float{}, std::integral_constant<int, 3>{});
+}
+
+void pack_rows(const PackArgs& a, int bf16, int n, hipStream_t st) {
+  const int64_t need = ceil_div(a.rows * (a.ld / 8), 256);
+  with_terms(bf16, n, [&](auto elem, auto count) {
+    hipLaunchKernelGGL((pack_rows_kernel<decltype(elem), decltype(count)::value>), dim3((unsigned)(need < 16384 ? need : 16384)),
+                       dim3(256), 0, st, a);
+  });
+}
+
+// The grid's second dimension has 65535 blocks: D is at most 2^17.
+void pack_cols(const PackArgs& a, int bf16, int n, hipStream_t st) {
+  with_terms(bf16, n, [&](auto elem, auto count) {
+    hipLaunchKernelGGL((pack_cols_kernel<decltype(elem), decltype(count)::value>),
+                       dim3((unsigned)ceil_div(a.ld, 64), (unsigned)ceil_div(a.cols, 64)), dim3(256), 0, st, a);
+  });
+}
+
+// The operands of the logits' product, laid out if need be.
+Bf16Product logits_product(const CrossEntropyArgs& a, const Layout& l, uint8_t* ws, hipStream_t st) {
+  Bf16Product g;
+  g.A = {static_cast<const uint16_t*>(a.x), a.T, a.D, 0};
+  g.B = {static_cast<const uint16_t*>(a.table), a.V, a.D, 0};
+  if (l.pack_x) {
+    uint16_t* const out = reinterpret_cast<uint16_t*>(ws + l.x_rows);
+    pack_rows({a.x, a.T, a.D, nullptr, 0, 0, out, l.D8, a.T * l.D8}, a.x_bf16, l.xn, st);
+    g.A = {out, a.T, l.D8, a.T * l.D8};
+  }
+  if (l.pack_t) {
+    uint16_t* const out = reinterpret_cast<uint16_t*>(ws + l.t_rows);
+    pack_rows({a.table, a.V, a.D, nullptr, 0, 0, out, l.D8, a.V * l.D8}, a.t_bf16, l.tn, st);
+    g.B = {out, a.V, l.D8, a.V * l.D8};
+  }
+  g.pairs = pairs_of(l.xn, l.tn);
+  g.K = l.pack_x || l.pack_t ? l.D8 : a.D;
+  g.splits = 1;
+  return g;
+}
+
+void place(Bf16Product& g, int64_t M, int64_t N) {
+  g.tiles_m = (int)ceil_div(M, Tile::BM);
+  g.tiles_n = (int)ceil_div(N, Tile::BN);
+}
+
+void out_product(const Bf16Product& g, OutArgs o, int splits, hipStream_t st) {
+  const int stages = g.pairs.count * (int)ceil_div(g.K, Tile::BK);
+  o.chunk = (int)ceil_div(stages, splits);
+  hipLaunchKernelGGL(out_tile_kernel, dim3((unsigned)g.tiles_m * g.tiles_n, splits), dim3(Tile::kThreads), 0, st, g, o);
+}
+
+void out_join(const OutArgs& o, const float* part, int splits, hipStream_t st) {
+  const int64_t need = ceil_div(o.M * ceil_div(o.N, 8), 256);
+  hipLaunchKernelGGL(out_join_kernel, dim3((unsigned)(need < 16384 ? need : 16384)), dim3(256), 0, st, o, part, splits);
+}
+
+__global__ void zero_kernel(uint32_t* p, int64_t words) {
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < words; i += (int64_t)gridDim.x * blockDim.x) p[i] = 0;
+}
+__global__ void zero_half_kernel(uint16_t* p) { *p = 0; }
+
+}  // namespace
+
+size_t cross_entropy_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int x_bf16, int t_bf16) {
+  Layout l(T, V, D, x_bf16, t_bf16);
+  l.forward();
+  return l.bytes;
+}
+
+size_t cross_entropy_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int x_bf16, int t_bf16, int g_bf16) {
+  Layout l(T, V, D, x_bf16, t_bf16);
+  l.backward(x_bf16, g_bf16);
+  return l.bytes;
+}
+
+hipError_t launch_cross_entropy_fwd(const CrossEntropyArgs& a, float* loss, float* lse, void* ws, hipStream_t st) {
+  if (a.T == 0) return hipSuccess;
+  Layout l(a.T, a.V, a.D, a.x_bf16, a.t_bf16);
+  l.forward();
+  uint8_t* const w = static_cast<uint8_t*>(ws);
+  Bf16Product g = logits_product(a, l, w, st);
+  place(g, a.T, a.V);
+  const LossArgs la{a.targets, a.i64, a.T, a.V, a.scale, reinterpret_cast<float*>(w + l.part),
+                    reinterpret_cast<float*>(w + l.at_target)};
+  hipLaunchKernelGGL(loss_tile_kernel, dim3((unsigned)g.tiles_m * g.tiles_n), dim3(Tile::kThreads), 0, st, g, la);
+  hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)ceil_div(a.T, 64)), dim3(1024), 0, st, la, l.parts, a.smoothing, loss, lse);
+  return hipGetLastError();
+}
+
+hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dloss, const float* lse, int accumulate,
+                                    void* dx, void* dtable, int g_bf16, void* ws, hipStream_t st) {
+  if (a.T == 0) {
+    if (accumulate) return hipSuccess;
+    const int64_t bytes = a.V * a.D * (g_bf16 ? 2 : 4), words = bytes / 4;
+    if (words) {
+      const int64_t need = ceil_div(words, 256);
+      hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(need < 16384 ? need : 16384)), dim3(256), 0, st, static_cast<uint32_t*>(dtable), words);
+    }
+    if (bytes & 3) hipLaunchKernelGGL(zero_half_kernel, dim3(1), dim3(1), 0, st, static_cast<uint16_t*>(dtable) + words * 2);
+    return hipGetLastError();
+  }
+  Layout l(a.T, a.V, a.D, a.x_bf16, a.t_bf16);
+  l.backward(a.x_bf16, g_bf16);
+  uint8_t* const w = static_cast<uint8_t*>(ws);
+  auto half = [&](size_t at) { return reinterpret_cast<uint16_t*>(w + at); };
+  Bf16Product z = logits_product(a, l, w, st);
+  // the transpose of x; a row that is padding is zeros: 0 times what it holds need not be 0
+  pack_cols({a.x, a.T, a.D, a.targets, a.i64, a.V, half(l.x_cols), l.T8, a.D * l.T8}, a.x_bf16, l.xt, st);
+  const Bf16Planes logits_b = z.B;
+  for (int64_t p = 0; p < l.pieces; ++p) {
+    const int64_t v0 = p * l.piece, cols = a.V - v0 < l.piece ? a.V - v0 : l.piece;
+    // g of the piece
+    z.B = {logits_b.p + v0 * logits_b.ld, cols, logits_b.ld, logits_b.plane};
+    place(z, a.T, cols);
+    const GradArgs ga{a.targets, a.i64, a.T, a.V, v0, cols, a.scale, a.smoothing, dloss, lse,
+                      half(l.g), l.piece, a.T * l.piece, half(l.gt), l.T8, l.piece * l.T8, l.g_rows, l.g_cols};
+    hipLaunchKernelGGL(grad_tile_kernel, dim3((unsigned)z.tiles_m * z.tiles_n), dim3(Tile::kThreads), 0, st, z, ga);
+    // dx += g W
+    const size_t elem = a.t_bf16 ? 2 : 4;
+    pack_cols({static_cast<const uint8_t*>(a.table) + (size_t)v0 * a.D * elem, cols, a.D, nullptr, 0, 0, half(l.t_cols), up8(cols),
+               a.D * up8(cols)},
+              a.t_bf16, l.tx, st);
+    Bf16Product x;
+    x.A = {half(l.g), a.T, l.piece, a.T * l.piece};
+    x.B = {half(l.t_cols), a.D, up8(cols), a.D * up8(cols)};
+    x.pairs = pairs_of(l.g_rows, l.tx);
+    x.K = up8(cols);
+    place(x, a.T, a.D);
+    OutArgs ox{a.T, a.D, l.sums_x ? reinterpret_cast<float*>(w + l.sum_x) : nullptr, dx, a.x_bf16, p > 0, a.targets, a.i64, a.V, 0};
+    out_product(x, ox, l.splits_x, st);
+    // dW = g^T x
+    Bf16Product t;
+    t.A = {half(l.gt), cols, l.T8, l.piece * l.T8};
+    t.B = {half(l.x_cols), a.D, l.T8, a.D * l.T8};
+    t.pairs = pairs_of(l.g_cols, l.xt);
+    t.K = l.T8;
+    place(t, cols, a.D);
+    uint8_t* const rows = static_cast<uint8_t*>(dtable) + (size_t)v0 * a.D * (g_bf16 ? 2 : 4);
+    OutArgs ow{cols, a.D, nullptr, rows, g_bf16, accumulate, nullptr, 0, 0, 0};
+    if (l.splits_w > 1) {
+      OutArgs sums = ow;
+      sums.part = reinterpret_cast<float*>(w + l.sum_w);
+      sums.add = 0;
+      out_product(t, sums, l.splits_w, st);
+      out_join(ow, sums.part, l.splits_w, st);
+    } else {
+      out_product(t, ow, 1, st);
+    }
+  }
+  if (l.sums_x) {
+    const OutArgs ox{a.T, a.D, nullptr, dx, a.x_bf16, 0, a.targets, a.i64, a.V, 0};
+    out_join(ox, reinterpret_cast<const float*>(w + l.sum_x), l.splits_x, st);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace luq

@@ -122,6 +122,54 @@ hipError_t launch_grouped_depth(GroupedA kind, const uint8_t* A, const float* al
                                 const float* bscale, int b_signed, const int32_t* offsets, int64_t experts, int64_t T,
                                 int64_t M, int64_t N, float* C, void* ws, hipStream_t st);
 
+// Choice of experts.
+struct RouteArgs {
+  const void* logits;
+  const float* bias;
+  int64_t T;
+  int E, K, groups, top_groups, best, renorm, sigmoid;
+  float scale;
+};
+hipError_t launch_route_fwd(const RouteArgs& a, int bf16, int32_t* chosen, float* weights, hipStream_t st);
+hipError_t launch_route_bwd(const RouteArgs& a, int bf16, const float* dweights, const int32_t* chosen, void* dlogits,
+                            hipStream_t st);
+
+// Cross entropy of the last layer.
+struct CrossEntropyArgs {
+  const void* x;
+  const void* table;
+  const void* targets;
+  int x_bf16, t_bf16, i64;
+  int64_t T, V, D;
+  float scale, smoothing;
+};
+// Bytes of the workspace; backward: with a gradient of the table in bf16 (g_bf16) or fp32.
+size_t cross_entropy_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int x_bf16, int t_bf16);
+size_t cross_entropy_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int x_bf16, int t_bf16, int g_bf16);
+hipError_t launch_cross_entropy_fwd(const CrossEntropyArgs& a, float* loss, float* lse, void* ws, hipStream_t st);
+hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dloss, const float* lse, int accumulate,
+                                    void* dx, void* dtable, int g_bf16, void* ws, hipStream_t st);
+
+// A plan of AdamW: an entry for each tensor, then its chunks of elements.
+constexpr int kAdamwChunk = 4096;
+struct AdamwEntry {
+  float* p;
+  const void* g;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  uint16_t* copy;
+  int64_t n;
+  float weight_decay, lr_scale;
+  int g_bf16, state_bits;
+};
+struct AdamwChunk {
+  uint32_t tensor, index;
+};
+hipError_t launch_adamw(const void* plan, int64_t count, int64_t chunks, const float* lr, const int64_t* step,
+                        double beta1, double beta2, float eps, const float* grad_scale, uint64_t seed, hipStream_t st);
+
 hipError_t launch_im2col3x3_t(const uint8_t* act, int64_t B, int64_t H, int64_t W, int64_t C,
                               uint8_t* col_t, hipStream_t st);
 
