@@ -205,7 +205,7 @@ typedef enum { LUQ_SOFTMAX = 0, LUQ_SIGMOID = 1 } luq_score;
  *
  *  logits   [T][experts], type dt.  bias  [experts] fp32, or NULL.
  *  chosen   out: [T][top_k] int32;  weights  out: [T][top_k] fp32.
- *  T in [0, 2^28], experts in [1, 4096], top_k in [1, 64]; groups in [1, 64] divides
+ *  T in [0, 2^25], experts in [1, 4096], top_k in [1, 64]; groups in [1, 64] divides
  *  experts; top_groups in [1, groups]; top_k is at most the experts of top_groups groups.
  *  scale is finite.  No workspace.
  */

@@ -647,8 +647,8 @@ static luq_status route_checks(const char* fn, luq_dtype dt, int64_t T, int64_t 
                                int renorm, float scale) {
   const luq_status st = check_types(fn, dt, dt);
   if (st != LUQ_OK) return st;
-  if (T < 0 || T > kMaxIds || experts < 1 || experts > kMaxExperts)
-    return fail(LUQ_ERR_SHAPE, "%s: T in [0, 2^28], experts in [1, 4096]", fn);
+  if (T < 0 || T > ((int64_t)1 << 25) || experts < 1 || experts > kMaxExperts)
+    return fail(LUQ_ERR_SHAPE, "%s: T in [0, 2^25], experts in [1, 4096]", fn);
   if (top_k < 1 || top_k > 64 || top_k > experts) return fail(LUQ_ERR_SHAPE, "%s: top_k in [1, 64], at most experts", fn);
   if (score != LUQ_SOFTMAX && score != LUQ_SIGMOID) return fail(LUQ_ERR_PARAM, "%s: score", fn);
   if (renorm != 0 && renorm != 1) return fail(LUQ_ERR_PARAM, "%s: renorm must be 0 or 1", fn);

@@ -2,10 +2,22 @@
 //
 //   s = softmax(l) or sigmoid(l),  c = s + bias,  w_k = scale s_k (/ sum of the chosen s)
 //
-// A wave a row.  The choice is k times the largest key of the row: a key is c as an unsigned
-// number of the same order.  Without a bias, and with groups ranked by their largest expert,
-// the order of c is that of the logits, whose keys need no exponential; otherwise c is
-// formed in 64 bits, so that two implementations that round differently choose alike.
+// 8 to 64 lanes a row, each with NE neighbouring experts.  The choice is k times the largest
+// key of the row (a key is a value as an unsigned number of the same order): of the lanes that
+// hold it the first has the lowest index.  Without a bias, and with groups ranked by their
+// largest expert, the order of c is that of the logits, whose keys need no exponential.
+//
+// Otherwise c is a sum, and which of two nearly equal ones is larger must not hang on a rounding:
+// the row is chosen in fp32 first, and again in 64 bits where two values that the choice
+// compared are nearer to each other than fp32's errors (3 of 1000 rows of 256 experts).
+//
+// Where a key's lowest bits are free (a bf16 logit's, or those of a sum, whose neighbours are looked
+// at again anyway) they hold the expert's place, in the row or in the lane: taking an expert out is
+// then a comparison for each key, without a branch.
+//
+// Bound by instructions, not by memory (16384 rows of 256 experts in 8 groups, top 8: 23 us, their
+// 16.8 MB would take 3.4; a wave a row with the choice in 64 bits took 57, in fp32 with the place
+// beside the key 27 to 32): many rows take as few lanes as 16 experts a lane allow, few rows as many.
 #include <type_traits>
 
 #include "luq_launch.hpp"
@@ -15,16 +27,68 @@ namespace luq {
 
 namespace {
 
-constexpr int kRouteWaves = 4, kMaxPer = 64;
+constexpr int kRouteWaves = 4, kMaxPer = 64, kMaxTop = 64;
 
 // Keys: unsigned numbers in the order of the values; 0 is no value's (-inf is barred).
-__device__ __forceinline__ uint64_t key_of(float v) {
+__device__ __forceinline__ uint32_t key_of(float v) {
   const uint32_t b = __float_as_uint(v + 0.0f);   // -0 is 0
-  return (uint64_t)(b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) << 32 | 0xFFFFFFFFu;
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t k) {
+  return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k);
 }
 __device__ __forceinline__ uint64_t key_of(double v) {
   const uint64_t b = __double_as_longlong(v + 0.0);
   return b ^ ((uint64_t)((int64_t)b >> 63) | 0x8000000000000000ull);
+}
+__device__ __forceinline__ double value_of(uint64_t k) {
+  return __longlong_as_double(k >> 63 ? k ^ 0x8000000000000000ull : ~k);
+}
+
+// A reduction over the LPR lanes of a row, in registers; every lane gets the result.
+template <int LPR, typename V, typename F>
+__device__ __forceinline__ V row_reduce(V v, F f) {
+  static_assert(sizeof(V) == 4, "a word");
+  auto step = [&](uint32_t other) { v = f(v, __builtin_bit_cast(V, other)); };
+  auto bits = [&]() { return __builtin_bit_cast(uint32_t, v); };
+  step(__builtin_amdgcn_update_dpp(0, bits(), 0xB1, 0xF, 0xF, true));                     // lanes 1 0 3 2
+  step(__builtin_amdgcn_update_dpp(0, bits(), 0x4E, 0xF, 0xF, true));                     // lanes 2 3 0 1
+  if constexpr (LPR >= 8) step(__builtin_amdgcn_update_dpp(0, bits(), 0x141, 0xF, 0xF, true));    // eight reversed
+  if constexpr (LPR >= 16) step(__builtin_amdgcn_update_dpp(0, bits(), 0x140, 0xF, 0xF, true));   // sixteen reversed
+  if constexpr (LPR >= 32) {
+    const auto s = __builtin_amdgcn_permlane16_swap(bits(), bits(), false, false);
+    const uint32_t x = s[0], y = s[1];   // (a bit cast of a vector's element takes the first)
+    v = f(__builtin_bit_cast(V, x), __builtin_bit_cast(V, y));
+  }
+  if constexpr (LPR >= 64) {
+    const auto s = __builtin_amdgcn_permlane32_swap(bits(), bits(), false, false);
+    const uint32_t x = s[0], y = s[1];   // (a bit cast of a vector's element takes the first)
+    v = f(__builtin_bit_cast(V, x), __builtin_bit_cast(V, y));
+  }
+  return v;
+}
+template <int LPR>
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  return row_reduce<LPR>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+template <int LPR>
+__device__ __forceinline__ float row_max(float v) {
+  return row_reduce<LPR>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LPR>
+__device__ __forceinline__ float row_min(float v) {
+  return row_reduce<LPR>(v, [](float a, float b) { return fminf(a, b); });
+}
+template <int LPR>
+__device__ __forceinline__ float row_total(float v) {
+  return row_reduce<LPR>(v, [](float a, float b) { return a + b; });
+}
+// The lanes of this lane's row that say yes, the row's first lane in bit 0.
+template <int LPR>
+__device__ __forceinline__ uint64_t row_ballot(bool yes) {
+  const uint64_t all = __ballot(yes);
+  if constexpr (LPR == kWave) return all;
+  return all >> (threadIdx.x & (kWave - 1) & ~(LPR - 1)) & ((1ull << LPR) - 1);
 }
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -32,186 +96,387 @@ __device__ __forceinline__ double wave_sum64(double v) {
   for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, kWave);
   return v;
 }
-__device__ __forceinline__ float wave_max32(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, kWave));
-  return v;
-}
 
-// The largest key of a wave and the lowest index that has it (a lane's own are the largest of
-// its keys and that one's index).
-__device__ __forceinline__ void wave_best(uint64_t& key, int& index) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) {
-    const uint64_t k = __shfl_xor((unsigned long long)key, d, kWave);
-    const int i = __shfl_xor(index, d, kWave);
-    if (k > key || (k == key && i < index)) {
-      key = k;
-      index = i;
-    }
+// The first of the lanes that hold a wave's largest key, or -1 if all are 0.
+__device__ __forceinline__ int wave_first(uint64_t key) {
+  const uint32_t high = (uint32_t)(key >> 32), most = row_max<kWave>(high);
+  if (most == 0) return -1;   // (no value's key has a high word of 0)
+  uint64_t who = __ballot(high == most);
+  if (who & (who - 1)) {
+    const uint32_t low = high == most ? (uint32_t)key : 0, most_low = row_max<kWave>(low);
+    who = __ballot(high == most && low == most_low);
   }
+  return __builtin_ctzll(who);
 }
 
 // A number that is neither NaN nor +inf.
 __device__ __forceinline__ bool sound(float v) { return v < __builtin_inff(); }
-__device__ __forceinline__ bool sound(double v) { return v < __builtin_inf(); }
 
-// NE experts a lane: expert i of lane t is i * 64 + t.  WIDE: c in 64 bits.
-template <typename T, int NE, bool WIDE>
-__global__ __launch_bounds__(kRouteWaves * kWave) void route_fwd_kernel(RouteArgs a, int32_t* __restrict__ chosen,
-                                                                        float* __restrict__ weights) {
-  extern __shared__ uint64_t lds_keys[];   // [waves][E], with groups
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int64_t row = (int64_t)blockIdx.x * (blockDim.x / kWave) + wave;
-  if (row >= a.T) return;
-  const T* const src = static_cast<const T*>(a.logits) + row * a.E;
-  float l[NE];
-  bool good = true;
+// Adds a pair (the first of it the larger) to the two largest keys.
+template <typename K>
+__device__ __forceinline__ void put_key(K& first, K& second, K k1, K k2) {
+  second = max(max(min(first, k1), second), k2);
+  first = max(first, k1);
+}
+
+// The choice of a row in 64 bits, by a wave; lane t has experts t * NE .. t * NE + NE - 1.
+// keys: [E] in LDS; list: the choices, in LDS.  The row holds no NaN and no +inf.
+template <typename T, int NE>
+__device__ void route_exact(const RouteArgs& a, int64_t row, uint64_t* keys, int* list) {
+  const int lane = threadIdx.x & (kWave - 1), e0 = lane * NE, left = a.E - e0;
+  const T* const src = static_cast<const T*>(a.logits) + row * a.E + e0;
+  float l[NE], top = -__builtin_inff();
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
-    const int e = i * kWave + lane;
-    l[i] = e < a.E ? to_f32(src[e]) : -__builtin_inff();
-    good &= sound(l[i]);
+    l[i] = i < left ? to_f32(src[i]) : -__builtin_inff();
+    top = fmaxf(top, l[i]);
   }
-  float top = l[0];
-#pragma unroll
-  for (int i = 1; i < NE; ++i) top = fmaxf(top, l[i]);
-  top = wave_max32(top);
+  top = row_max<kWave>(top);
   uint64_t key[NE];
-  if constexpr (WIDE) {
-    double s[NE], total = 0.0;
+  double s[NE], total = 0.0;
 #pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      if (a.sigmoid) {
-        s[i] = 1.0 / (1.0 + exp(-(double)l[i]));
-      } else {
-        s[i] = l[i] > -__builtin_inff() ? exp((double)l[i] - (double)top) : 0.0;
-        total += s[i];
-      }
+  for (int i = 0; i < NE; ++i) {
+    if (a.sigmoid) {
+      s[i] = 1.0 / (1.0 + exp(-(double)l[i]));
+    } else {
+      s[i] = l[i] > -__builtin_inff() ? exp((double)l[i] - (double)top) : 0.0;
+      total += s[i];
     }
-    if (!a.sigmoid) {
-      total = wave_sum64(total);
-#pragma unroll
-      for (int i = 0; i < NE; ++i) s[i] = s[i] / total;
-    }
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      const int e = i * kWave + lane;
-      const double c = a.bias && e < a.E ? s[i] + (double)a.bias[e] : s[i];
-      const bool barred = !(l[i] > -__builtin_inff()) || c == -__builtin_inf();
-      good &= barred || sound(c);
-      key[i] = barred ? 0 : key_of(c);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < NE; ++i) key[i] = l[i] > -__builtin_inff() ? key_of(l[i]) : 0;
   }
-  if (__ballot(good) != ~0ull) {
-    if (lane < a.K) {
-      chosen[row * a.K + lane] = -1;
-      weights[row * a.K + lane] = __builtin_nanf("");
-    }
-    return;
+  if (!a.sigmoid) total = wave_sum64(total);
+#pragma unroll
+  for (int i = 0; i < NE; ++i) {
+    if (!a.sigmoid) s[i] = s[i] / total;
+    const double c = a.bias && i < left ? s[i] + (double)a.bias[e0 + i] : s[i];
+    key[i] = l[i] > -__builtin_inff() && c > -__builtin_inf() ? key_of(c) : 0;
   }
   if (a.groups > 1) {
-    // lane g ranks group g
-    uint64_t* const mine = lds_keys + wave * a.E;
+    const int size = a.E / a.groups, lanes = size / NE;
+    const bool whole = size % NE == 0 && (lanes & (lanes - 1)) == 0;
+    uint64_t first = 0, second = 0;
+    if (whole) {   // groups of a power of two of lanes
 #pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      const int e = i * kWave + lane;
-      if (e < a.E) mine[e] = key[i];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int size = a.E / a.groups;
-    uint64_t rank = 0;
-    if (lane < a.groups) {
-      uint64_t first = 0, second = 0;
-      for (int j = 0; j < size; ++j) {
-        const uint64_t k = mine[lane * size + j];
-        if (k > first) {
-          second = first;
-          first = k;
-        } else if (k > second) {
-          second = k;
-        }
-      }
-      rank = first;
-      if constexpr (WIDE) {
-        if (a.best == 2 && second) {
-          auto value = [](uint64_t k) {
-            return __longlong_as_double(k >> 63 ? k ^ 0x8000000000000000ull : ~k);
-          };
-          rank = key_of(value(first) + value(second));
-        }
-      }
-    }
-    uint64_t kept = 0;   // a bit for each group
-    for (int j = 0; j < a.top_groups; ++j) {
-      uint64_t k = rank;
-      int g = lane;
-      wave_best(k, g);
-      if (k == 0) break;
-      kept |= 1ull << g;
-      if (lane == g) rank = 0;
-    }
+      for (int i = 0; i < NE; ++i) put_key<uint64_t>(first, second, key[i], 0);
+      for (int d = 1; d < lanes; d *= 2)
+        put_key<uint64_t>(first, second, __shfl_xor((unsigned long long)first, d, kWave),
+                          __shfl_xor((unsigned long long)second, d, kWave));
+    } else {       // lane g reads group g
 #pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      const int e = i * kWave + lane;
-      if (e < a.E && !(kept >> (e / size) & 1)) key[i] = 0;
+      for (int i = 0; i < NE; ++i)
+        if (i < left) keys[e0 + i] = key[i];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (lane < a.groups)
+        for (int i = 0; i < size; ++i) put_key<uint64_t>(first, second, keys[lane * size + i], 0);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    const uint64_t rank = a.best == 2 && second ? key_of(value_of(first) + value_of(second)) : first;
+    // groups before this lane's, by rank and then by place
+    const int step = whole ? lanes : 1, mine = lane / step;
+    int before = 0;
+    for (int g = 0; g < a.groups; ++g) {
+      const uint64_t r = __shfl((unsigned long long)rank, g * step, kWave);
+      before += r > rank || (r == rank && g < mine);
+    }
+    const uint64_t kept = __ballot(before < a.top_groups && mine < a.groups);
+#pragma unroll
+    for (int i = 0; i < NE; ++i)
+      if (i < left && !(kept >> ((e0 + i) / size * step) & 1)) key[i] = 0;
   }
-  // lane k keeps the k-th choice
-  int my_expert = -1;
-  float my_logit = -__builtin_inff();
-  for (int k = 0; k < a.K; ++k) {
-    uint64_t best = key[0];
-    int index = lane;
+  uint64_t best = 0;
+  int at = 0;
+  auto local = [&]() {
+    best = key[0];
+    at = 0;
 #pragma unroll
     for (int i = 1; i < NE; ++i)
       if (key[i] > best) {
         best = key[i];
-        index = i * kWave + lane;
+        at = i;
       }
-    wave_best(best, index);
-    if (best == 0) break;
-    float v = 0.0f;
+  };
+  local();
+  for (int k = 0; k < a.K; ++k) {
+    const int who = wave_first(best);
+    if (lane == max(who, 0)) {
+      list[k] = who >= 0 ? e0 + at : -1;
 #pragma unroll
-    for (int i = 0; i < NE; ++i)
-      if (index == i * kWave + lane) {
-        key[i] = 0;
-        v = l[i];
-      }
-    v = __shfl(v, index & (kWave - 1), kWave);
-    if (lane == k) {
-      my_expert = index;
-      my_logit = v;
+      for (int i = 0; i < NE; ++i)
+        if (i == at) key[i] = 0;
+      local();
     }
   }
-  const bool have = my_expert >= 0;
-  float w = 0.0f;
-  if (a.renorm) {
-    // of shares only ratios count: scores over the largest of them, or over e^top where all are small
-    const float most = wave_max32(my_logit);
-    if (a.sigmoid) {
-      const float ref = fminf(most, 0.0f);
-      w = !have ? 0.0f : my_logit > 0.0f ? 1.0f / (1.0f + expf(-my_logit)) : expf(my_logit - ref) / (1.0f + expf(my_logit));
-    } else {
-      w = have ? expf(my_logit - most) : 0.0f;
-    }
-    const float total = wave_sum(w);
-    w = total > 0.0f ? w / total : 0.0f;
-  } else if (a.sigmoid) {
-    w = have ? 1.0f / (1.0f + expf(-my_logit)) : 0.0f;
+}
+
+// How much two values of c in fp32 may be off, together.  A sigmoid is off by 5 u (its exponential
+// by (2 |l| + 2) u of itself, of which s (1 - s) remains, a sum and a reciprocal by 3 u), a softmax by
+// 60 u of itself (an exponential of d by (3 |d| + 2) u of itself, the sum's terms as much on average,
+// the additions and the division), and the addition of the bias by u |c|.  Sums of two: twice that.
+__device__ __forceinline__ float near_of(bool sigmoid, float most_score, float most_c) {
+  return (sigmoid ? 0x1p-20f : 0x1p-17f * most_score) + 0x1p-22f * most_c;
+}
+
+// LPR lanes a row, NE experts a lane: lane j has experts j * NE .. j * NE + NE - 1.  SUM: c is a sum.
+// dynamic LDS, with groups: a region a wave for the keys of its rows, or of a row in 64 bits.
+template <int LPR>
+__host__ __device__ constexpr int route_wave_bytes(int E) {
+  return (kWave / LPR > 2 ? kWave / LPR * 4 : 8) * E;
+}
+template <typename T, int LPR, int NE, bool SUM>
+__global__ __launch_bounds__(kRouteWaves * kWave) void route_fwd_kernel(RouteArgs a, int32_t* __restrict__ chosen,
+                                                                        float* __restrict__ weights) {
+  constexpr int kRows = kWave / LPR, kList = LPR * NE < kMaxTop ? LPR * NE : kMaxTop, kMine = (kList + LPR - 1) / LPR;
+  // the place that a key holds: of sixteen free bits the one in the row (equal keys are then in the
+  // order of their places), else the one in the lane
+  constexpr bool kPacked = SUM || sizeof(T) == 2, kInRow = !SUM && sizeof(T) == 2;
+  constexpr uint32_t kPlace = kInRow ? LPR * NE - 1 : kPacked ? NE - 1 : 0;
+  static_assert((NE & (NE - 1)) == 0 && LPR * NE <= 65536, "a place in the lowest bits");
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds_keys[];
+  __shared__ int lists[SUM ? kRouteWaves : 1][kMaxTop];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & (LPR - 1);
+  const int64_t row0 = ((int64_t)blockIdx.x * (blockDim.x / kWave) + wave) * kRows, row = row0 + lane / LPR;
+  if (row0 >= a.T) return;
+  const bool in = row < a.T;
+  const int e0 = j * NE, left = in ? a.E - e0 : 0;
+  uint8_t* const region = lds_keys + wave * route_wave_bytes<LPR>(a.E);
+  const T* const src = static_cast<const T*>(a.logits) + row * a.E;
+  float l[NE];
+  if (left >= NE) {
+    RowPack<T, NE> pack;
+    pack.load(src + e0);
+#pragma unroll
+    for (int i = 0; i < NE; ++i) l[i] = pack.get(i);
   } else {
-    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) l[i] = i < left ? to_f32(src[e0 + i]) : -__builtin_inff();
+  }
+  bool good = true, near = false;
+  float top = l[0];
+#pragma unroll
+  for (int i = 0; i < NE; ++i) {
+    good &= sound(l[i]);
+    top = fmaxf(top, l[i]);
+  }
+  top = row_max<LPR>(top);
+  constexpr float kLog2e = 1.44269504088896341f;
+  uint32_t key[NE];
+  float tolerance = 0.0f;
+  auto pack_place = [&](uint32_t k, int i) { return kPacked ? (k & ~kPlace) | (kPlace - (kInRow ? e0 + i : i)) : k; };
+  if constexpr (SUM) {
+    float s[NE], total = 0.0f, big = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      if (a.sigmoid) {
+        s[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l[i] * kLog2e));
+      } else {
+        s[i] = l[i] > -__builtin_inff() ? __builtin_amdgcn_exp2f((l[i] - top) * kLog2e) : 0.0f;
+        total += s[i];
+      }
+    }
+    float share = 1.0f;
+    if (!a.sigmoid) share = 1.0f / row_total<LPR>(total);
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      const float c = fmaf(s[i], share, a.bias && i < left ? a.bias[e0 + i] : 0.0f);
+      const bool barred = !(l[i] > -__builtin_inff()) || c == -__builtin_inff();
+      good &= barred || sound(c);
+      key[i] = barred ? 0 : pack_place(key_of(c), i);
+      if (!barred) big = fmaxf(big, fabsf(c));
+    }
+    tolerance = near_of(a.sigmoid, share, row_max<LPR>(big));
+  } else {
+#pragma unroll
+    for (int i = 0; i < NE; ++i) key[i] = l[i] > -__builtin_inff() ? pack_place(key_of(l[i]), i) : 0;
+  }
+  const bool bad = row_ballot<LPR>(!good) != 0;
+  // of a key with a place, the least and the largest value that it may stand for
+  auto least = [&](uint32_t k) { return value_of(k & ~kPlace); };
+  auto largest = [&](uint32_t k) { return value_of(k | kPlace); };
+  if (a.groups > 1) {
+    // the rank of this lane's group: of whole lanes, a power of two of them, in registers; else
+    // lane g of the row reads group g.  Ranks are values without places.
+    const int size = a.E / a.groups, lanes = size / NE;
+    auto rank_of = [&](uint32_t first, uint32_t second) {
+      if constexpr (SUM) {
+        if (a.best == 2 && second) return key_of(least(first) + least(second));
+      }
+      return first & ~kPlace;
+    };
+    // how far a rank in fp32 may be off: both places, and both sums
+    const float rank_tolerance = SUM ? 2.0f * tolerance : 0.0f;
+    if (size % NE == 0 && (lanes & (lanes - 1)) == 0) {
+      uint32_t first = 0, second = 0;
+#pragma unroll
+      for (int i = 0; i < NE; ++i) put_key<uint32_t>(first, second, key[i], 0);
+#pragma unroll
+      for (int d = 1; d < LPR; d *= 2)
+        if (d < lanes) put_key<uint32_t>(first, second, __shfl_xor(first, d, kWave), __shfl_xor(second, d, kWave));
+      uint32_t rank = rank_of(first, second);
+      if (e0 >= a.E) rank = 0;
+      // groups before ours, by rank and then by place
+      const int mine = j / lanes;
+      int before = 0;
+      for (int g = 0; g < a.groups; ++g) {
+        const uint32_t r = __shfl(rank, (lane & ~(LPR - 1)) + g * lanes, kWave);
+        before += r > rank || (r == rank && g < mine);
+      }
+      const bool kept = before < a.top_groups;
+      if constexpr (SUM) {
+        const float low = row_min<LPR>(kept && rank ? value_of(rank) : __builtin_inff());
+        float high = !kept && rank ? largest(first) + (a.best == 2 && second ? largest(second) : 0.0f) : -__builtin_inff();
+        high = row_max<LPR>(high);
+        near |= high > -__builtin_inff() && low - high <= rank_tolerance;
+      }
+      if (!kept)
+#pragma unroll
+        for (int i = 0; i < NE; ++i) key[i] = 0;
+    } else {
+      uint32_t* const mine = reinterpret_cast<uint32_t*>(region) + lane / LPR * a.E;
+#pragma unroll
+      for (int i = 0; i < NE; ++i)
+        if (i < left) mine[e0 + i] = key[i];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      // groups beyond the row's lanes: a lane takes every LPR-th
+      constexpr int kPerLane = kMaxTop / LPR;
+      uint32_t ranks[kPerLane];
+      float highs[kPerLane];
+#pragma unroll
+      for (int q = 0; q < kPerLane; ++q) {
+        const int g = j + q * LPR;
+        uint32_t first = 0, second = 0;
+        if (in && g < a.groups)
+          for (int i = 0; i < size; ++i) put_key<uint32_t>(first, second, mine[g * size + i], 0);
+        ranks[q] = rank_of(first, second);
+        highs[q] = ranks[q] ? largest(first) + (a.best == 2 && second ? largest(second) : 0.0f) : -__builtin_inff();
+      }
+      uint64_t kept = 0;
+      float low = __builtin_inff();
+      for (int n = 0; n < a.top_groups; ++n) {
+        uint32_t best = 0;
+        int at = 0;
+#pragma unroll
+        for (int q = 0; q < kPerLane; ++q)
+          if (ranks[q] > best) {
+            best = ranks[q];
+            at = q;
+          }
+        const uint32_t most = row_max<LPR>(best);
+        // the lowest group of those: by q first, then by lane
+        const uint64_t who = row_ballot<LPR>(best == most);
+        int g = 1 << 20;
+        for (uint64_t w = most ? who : 0; w; w &= w - 1) {
+          const int t = __builtin_ctzll(w);
+          g = min(g, t + LPR * __shfl(at, (lane & ~(LPR - 1)) + t, kWave));
+        }
+        if (most == 0) continue;
+        low = value_of(most);
+        kept |= 1ull << g;
+#pragma unroll
+        for (int q = 0; q < kPerLane; ++q)
+          if (g == j + q * LPR) {
+            ranks[q] = 0;
+            highs[q] = -__builtin_inff();
+          }
+      }
+      if constexpr (SUM) {
+        float high = highs[0];
+#pragma unroll
+        for (int q = 1; q < kPerLane; ++q) high = fmaxf(high, highs[q]);
+        high = row_max<LPR>(high);
+        near |= high > -__builtin_inff() && low - high <= rank_tolerance;
+      }
+#pragma unroll
+      for (int i = 0; i < NE; ++i)
+        if (i < left && !(kept >> ((e0 + i) / size) & 1)) key[i] = 0;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  }
+  // the choices, the k-th in lane k mod LPR; with SUM one more, for its distance
+  int expert[kMine];
+#pragma unroll
+  for (int q = 0; q < kMine; ++q) expert[q] = -1;
+  uint32_t last = 0;
+  for (int k = 0; k < a.K + SUM; ++k) {
+    uint32_t best = key[0];
+    int at = 0;
+#pragma unroll
+    for (int i = 1; i < NE; ++i) {
+      if constexpr (!kPacked) at = key[i] > best ? i : at;
+      best = max(best, key[i]);
+    }
+    const uint32_t most = row_max<LPR>(best);
+    if constexpr (SUM) {
+      near |= k > 0 && most && least(last) - largest(most) <= tolerance;
+      last = most;
+      if (k == a.K) break;
+    }
+    int first = 0, index;
+    if constexpr (!kInRow) {
+      const uint64_t who = row_ballot<LPR>(best == most);
+      first = LPR <= 32 ? __builtin_ctz((uint32_t)who) : __builtin_ctzll(who);
+    }
+    if constexpr (kPacked) {
+      index = (int)(kPlace - (most & kPlace)) + first * NE;
+      const uint32_t out = kInRow || j == first ? most : 0;
+#pragma unroll
+      for (int i = 0; i < NE; ++i) key[i] = key[i] == out ? 0 : key[i];
+    } else {
+      index = __shfl(at, (lane & ~(LPR - 1)) + first, kWave) + first * NE;
+#pragma unroll
+      for (int i = 0; i < NE; ++i) key[i] = j == first && i == at ? 0 : key[i];
+    }
+#pragma unroll
+    for (int q = 0; q < kMine; ++q)
+      if (k == j + q * LPR && most) expert[q] = index;
+  }
+  if constexpr (SUM) {
+    // rows where two values are too near to tell, one after the other by the whole wave
+    uint64_t again = __ballot(in && !bad && near && j == 0);
+    while (again) {
+      const int r = __builtin_ctzll(again) / LPR;
+      again &= again - 1;
+      route_exact<T, (LPR * NE + kWave - 1) / kWave>(a, row0 + r, reinterpret_cast<uint64_t*>(region), lists[wave]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int q = 0; q < kMine; ++q)
+        if (lane / LPR == r && j + q * LPR < a.K) expert[q] = lists[wave][j + q * LPR];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  }
+  if (!in) return;
+  float logit[kMine], w[kMine], most = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+  for (int q = 0; q < kMine; ++q) {
+    if (bad) expert[q] = -1;
+    logit[q] = expert[q] < 0 ? -__builtin_inff() : to_f32(src[expert[q]]);
+    most = fmaxf(most, logit[q]);
+  }
+  // of shares only ratios count: scores over the largest of them, or over e^top where all are small
+  const float ref = a.renorm ? (a.sigmoid ? fminf(row_max<LPR>(most), 0.0f) : row_max<LPR>(most)) : a.sigmoid ? 0.0f : top;
+#pragma unroll
+  for (int q = 0; q < kMine; ++q) {
+    const float v = logit[q];
+    w[q] = expert[q] < 0 ? 0.0f
+           : !a.sigmoid  ? expf(v - ref)
+           : v > 0.0f    ? 1.0f / (1.0f + expf(-v))
+                         : expf(v - ref) / (1.0f + expf(v));
+    total += w[q];
+  }
+  if (a.renorm) {
+    total = row_total<LPR>(total);
+  } else if (a.sigmoid) {
+    total = 1.0f;
+  } else {
+    total = 0.0f;
 #pragma unroll
     for (int i = 0; i < NE; ++i) total += l[i] > -__builtin_inff() ? expf(l[i] - top) : 0.0f;
-    total = wave_sum(total);
-    w = have ? expf(my_logit - top) / total : 0.0f;
+    total = row_total<LPR>(total);
   }
-  if (lane < a.K) {
-    chosen[row * a.K + lane] = my_expert;
-    weights[row * a.K + lane] = w * a.scale;
+#pragma unroll
+  for (int q = 0; q < kMine; ++q) {
+    const int k = j + q * LPR;
+    if (k >= a.K) break;
+    chosen[row * a.K + k] = expert[q];
+    weights[row * a.K + k] = bad ? __builtin_nanf("") : expert[q] < 0 ? 0.0f : w[q] / total * a.scale;
   }
 }
 
@@ -251,10 +516,10 @@ __global__ __launch_bounds__(kRouteWaves * kWave) void route_bwd_kernel(RouteArg
     float top = l[0];
 #pragma unroll
     for (int i = 1; i < NE; ++i) top = fmaxf(top, l[i]);
-    top = wave_max32(top);
+    top = row_max<kWave>(top);
     float grad = d;      // of the choice's score; with renorm and softmax times the score
     if (a.renorm) {
-      const float most = wave_max32(mine), ref = a.sigmoid ? fminf(most, 0.0f) : most;
+      const float most = row_max<kWave>(mine), ref = a.sigmoid ? fminf(most, 0.0f) : most;
       float s = 0.0f, rest = 1.0f;   // score over e^ref; 1 - score
       if (have) {
         const float low = expf(-fabsf(mine));
@@ -332,19 +597,38 @@ void with_per_lane(int E, F f) {
 
 }  // namespace
 
+// Rows that fill the machine with 16 experts a lane (256 experts, 16384 rows: 23 us, 32 with 4 a lane;
+// 4 rows: 12.4 and 6.4 us a call).
+constexpr int64_t kManyRows = 4096;
+
 hipError_t launch_route_fwd(const RouteArgs& a, int bf16, int32_t* chosen, float* weights, hipStream_t st) {
   // without a bias and without sums the logits' order is the scores'
-  const bool wide = a.bias || (a.groups > 1 && a.best == 2);
+  const bool sum = a.bias || (a.groups > 1 && a.best == 2);
   const int waves = a.groups > 1 && a.E > 512 ? 1 : kRouteWaves;
-  const size_t lds = a.groups > 1 ? (size_t)waves * a.E * sizeof(uint64_t) : 0;
-  with_per_lane(a.E, [&](auto ne) {
-    constexpr int NE = decltype(ne)::value;
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)((a.T + waves - 1) / waves)), dim3(waves * kWave), lds, st, a, chosen, weights);
+  auto go = [&](auto lpr, auto ne) {
+    constexpr int LPR = decltype(lpr)::value, NE = decltype(ne)::value;
+    const int rows = waves * (kWave / LPR);
+    const size_t lds = a.groups > 1 ? (size_t)waves * route_wave_bytes<LPR>(a.E) : 0;
+    auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((a.T + rows - 1) / rows)), dim3(waves * kWave), lds, st, a, chosen, weights);
     };
-    if (bf16) wide ? go(route_fwd_kernel<uint16_t, NE, true>) : go(route_fwd_kernel<uint16_t, NE, false>);
-    else wide ? go(route_fwd_kernel<float, NE, true>) : go(route_fwd_kernel<float, NE, false>);
-  });
+    if (bf16) sum ? launch(route_fwd_kernel<uint16_t, LPR, NE, true>) : launch(route_fwd_kernel<uint16_t, LPR, NE, false>);
+    else sum ? launch(route_fwd_kernel<float, LPR, NE, true>) : launch(route_fwd_kernel<float, LPR, NE, false>);
+  };
+  using std::integral_constant;
+  const bool many = a.T >= kManyRows;
+  if (a.E <= 8) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+  else if (a.E <= 16) go(integral_constant<int, 8>{}, integral_constant<int, 2>{});
+  else if (a.E <= 32) go(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+  else if (a.E <= 64) go(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+  else if (a.E <= 128 && many) go(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+  else if (a.E <= 128) go(integral_constant<int, 32>{}, integral_constant<int, 4>{});
+  else if (a.E <= 256 && many) go(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+  else if (a.E <= 256) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else if (a.E <= 512 && many) go(integral_constant<int, 32>{}, integral_constant<int, 16>{});
+  else if (a.E <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else if (a.E <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+  else go(integral_constant<int, 64>{}, integral_constant<int, kMaxPer>{});
   return hipGetLastError();
 }
 

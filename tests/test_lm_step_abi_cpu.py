@@ -25,7 +25,7 @@ def _call(fn, defaults, kw):
 
 ROUTE = dict(logits=P, dt=0, T=4, E=64, K=8, score=0, bias=NUL, groups=8, top_groups=4, best=2, renorm=1, scale=1.0, chosen=P2,
              weights=P3, stream=NUL)
-ROUTE_BAD = [(dict(dt=2), DTYPE), (dict(T=-1), SHAPE), (dict(T=(1 << 28) + 1), SHAPE), (dict(E=0), SHAPE), (dict(E=4097), SHAPE),
+ROUTE_BAD = [(dict(dt=2), DTYPE), (dict(T=-1), SHAPE), (dict(T=(1 << 25) + 1), SHAPE), (dict(E=0), SHAPE), (dict(E=4097), SHAPE),
              (dict(K=0), SHAPE), (dict(K=65), SHAPE), (dict(score=2), PARAM), (dict(renorm=2), PARAM), (dict(scale=INF), PARAM),
              (dict(scale=NAN), PARAM), (dict(logits=NUL), NULL), (dict(logits=HALF), ALIGN), (dict(logits=ODD, dt=1), ALIGN),
              (dict(chosen=NUL), NULL), (dict(chosen=HALF), ALIGN)]
