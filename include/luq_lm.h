@@ -239,7 +239,7 @@ luq_status luq_route_bwd(const float* dweights, const void* logits, luq_dtype dt
  *  targets  [T]; one below 0 is padding: loss 0, no gradient, whatever its row of x holds.
  *           One at or above V is a data error: loss NaN, no gradient.
  *  T in [0, 2^21], V in [1, 2^28], D in [1, 2^17]; T * V at most 2^37, T * D and V * D at most
- *  2^36; scale finite, smoothing in [0, 1].
+ *  2^36; scale finite and not 0, smoothing in [0, 1].
  *
  * Products are those of bf16 matrix instructions with fp32 sums.  An fp32 tensor is taken
  * as three bf16 terms (24 bits, fewer below 2^-110: a term is a multiple of 2^-133), of

@@ -713,7 +713,8 @@ static luq_status cross_entropy_checks(const char* fn, luq_dtype xt, luq_dtype t
   if (st != LUQ_OK) return st;
   if (!cross_entropy_sizes(T, V, D))
     return fail(LUQ_ERR_SHAPE, "%s: T in [0, 2^21], V in [1, 2^28], D in [1, 2^17], T*V up to 2^37, T*D and V*D up to 2^36", fn);
-  if (!(scale > -__builtin_inff() && scale < __builtin_inff())) return fail(LUQ_ERR_PARAM, "%s: scale must be finite", fn);
+  if (!(scale > -__builtin_inff() && scale < __builtin_inff()) || scale == 0.0f)
+    return fail(LUQ_ERR_PARAM, "%s: scale must be finite and not 0", fn);
   if (!(smoothing >= 0.0f && smoothing <= 1.0f)) return fail(LUQ_ERR_PARAM, "%s: smoothing must be in [0, 1]", fn);
   return LUQ_OK;
 }

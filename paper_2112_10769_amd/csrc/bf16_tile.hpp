@@ -119,7 +119,6 @@ struct Bf16Tile {
       __builtin_amdgcn_s_waitcnt(kWaitLds);
       __builtin_amdgcn_s_waitcnt(kWaitLoads);
       asm volatile("s_barrier" ::: "memory");
-      issue(buf == 0 ? NBUF - 1 : buf - 1);
       const uint8_t* const As = lds + buf * kStage + (wm * TM * 32 + r) * kRowBytes;
       const uint8_t* const Bs = lds + buf * kStage + (BM + wn * TN * 32 + r) * kRowBytes;
       const int swz = (r * kPieces / 8) & (kPieces - 1);
@@ -131,6 +130,8 @@ struct Bf16Tile {
         for (int i = 0; i < TM; ++i) a[i] = *reinterpret_cast<const v8bf*>(As + i * 32 * kRowBytes + at);
 #pragma unroll
         for (int j = 0; j < TN; ++j) b[j] = *reinterpret_cast<const v8bf*>(Bs + j * 32 * kRowBytes + at);
+        // after the first fragments' reads, which the products wait for
+        if (kk == 0) issue(buf == 0 ? NBUF - 1 : buf - 1);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll

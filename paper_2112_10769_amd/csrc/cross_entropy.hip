@@ -122,9 +122,13 @@ __global__ __launch_bounds__(256) void pack_cols_kernel(PackArgs a) {
 
 // ---- the products
 
-using Tile = Bf16Tile<2, 2, 2, 2, 64, 2>;
+// Eight waves on 256 x 256 (1300 TFLOP/s alone, 128 KB of LDS: one workgroup a CU), or four on
+// 128 x 128 (1100; two a CU) where there are few tiles.
+using BigTile = Bf16Tile<2, 4, 4, 2, 64, 2>;
+using SmallTile = Bf16Tile<2, 2, 2, 2, 64, 2>;
 
 // Where a lane's sums lie: row `row(i)` of the matrix, columns col(j, q) .. + 3 in registers 4q .. 4q + 3.
+template <typename Tile>
 struct Lane {
   int64_t row0, col0;
   __device__ __forceinline__ Lane(int64_t m0, int64_t n0) {
@@ -141,10 +145,12 @@ struct LossArgs {
   int i64;
   int64_t T, V;
   float scale;
+  int smoothed;    // whether the sum of logits is asked for
   float* part;     // [column parts][3][T]: maximum (times log2 e), sum of exponentials, sum of logits
   float* at_target;
 };
 
+template <typename Tile>
 __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g, LossArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[Tile::kLds];
   int tm, tn;
@@ -152,34 +158,63 @@ __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g
   const int64_t m0 = (int64_t)tm * Tile::BM, n0 = (int64_t)tn * Tile::BN;
   Tile tile;
   tile.run(g, m0, n0, 0, g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK), lds);
-  const Lane at(m0, n0);
-  const float log2_scale = a.scale * kLog2e;
-  const bool whole = n0 + Tile::BN <= a.V;
+  const Lane<Tile> at(m0, n0);
+  const float c = a.scale * kLog2e;
+  const int half = (threadIdx.x & 63) >> 5;
+  const int64_t cols0 = at.col0 - 4 * half;   // of the wave
+  if (n0 + Tile::BN > a.V) {
+    // columns beyond the table: nothing, whatever the sign of the scale
+    const float none = c < 0.0f ? __builtin_inff() : -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < Tile::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (at.col(j, e / 4) + e % 4 >= a.V) tile.acc[i][j][e] = none;
+  }
   const int64_t part = (int64_t)tn * Tile::WN + (threadIdx.x >> 6) % Tile::WN;
 #pragma unroll
   for (int i = 0; i < Tile::TM; ++i) {
     const int64_t row = at.row(i);
     const int64_t y = row < a.T ? target_of(a.targets, a.i64, row) : -1;
-    float top = -3.0e38f, sum = 0.0f, all = 0.0f;
+    float all = 0.0f;
+    if (a.smoothed) {
 #pragma unroll
-    for (int j = 0; j < Tile::TN; ++j)
+      for (int j = 0; j < Tile::TN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const bool in = whole || at.col(j, e / 4) + e % 4 < a.V;
-        const float z = tile.acc[i][j][e];
-        if (at.col(j, e / 4) + e % 4 == y) a.at_target[row] = z * a.scale;
-        all += in ? z : 0.0f;
-        tile.acc[i][j][e] = in ? z * log2_scale : -__builtin_inff();
-        top = fmaxf(top, tile.acc[i][j][e]);
-      }
+        for (int e = 0; e < 16; ++e) all += at.col(j, e / 4) + e % 4 < a.V ? tile.acc[i][j][e] : 0.0f;
+      all += __shfl_xor(all, 32, kWave);
+    }
+    const int mine = y >= cols0 && y < cols0 + Tile::TN * 32 ? (int)(y - cols0) - 4 * half : -8;
+    if (__ballot(mine != -8)) {   // a target among the wave's columns
+#pragma unroll
+      for (int j = 0; j < Tile::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (mine == j * 32 + 8 * (e / 4) + e % 4) a.at_target[row] = tile.acc[i][j][e] * a.scale;
+    }
+    float top = tile.acc[i][0][0];
+    if (c < 0.0f) {
+#pragma unroll
+      for (int j = 0; j < Tile::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fminf(top, tile.acc[i][j][e]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < Tile::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, tile.acc[i][j][e]);
+    }
+    top = fmaxf(top * c, -3.0e38f);
     top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(tile.acc[i][j][e] - top);
+      for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(tile.acc[i][j][e], c, -top));
     sum += __shfl_xor(sum, 32, kWave);
-    all += __shfl_xor(all, 32, kWave);
-    if ((threadIdx.x & 32) == 0 && row < a.T) {
+    if (half == 0 && row < a.T) {
       float* const out = a.part + part * 3 * a.T + row;
       out[0] = top;
       out[a.T] = sum;
@@ -187,6 +222,10 @@ __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g
     }
   }
 }
+
+// (hipcc leaves the host's side of the tiles' kernels out unless asked for)
+template __global__ void loss_tile_kernel<BigTile>(Bf16Product, LossArgs);
+template __global__ void loss_tile_kernel<SmallTile>(Bf16Product, LossArgs);
 
 // The rows' parts joined: 64 rows a workgroup, its 16 waves every 16th part.
 __global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t parts, float smoothing, float* __restrict__ loss,
@@ -242,23 +281,23 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t par
 
 // A slab of a wave's sums in LDS: 32 rows of its columns in fp32, from which both orders are read
 // in pieces of eight.
-constexpr int kSlabCols = Tile::TN * 32, kSlabPitch = kSlabCols + 4;
-static_assert((size_t)Tile::WM * Tile::WN * 32 * kSlabPitch * 4 <= (size_t)Tile::kLds, "slabs fit in the stages' place");
-
+template <typename Tile>
 struct Slab {
+  static constexpr int kCols = Tile::TN * 32, kPitch = kCols + 4, kItems = 32 * kCols / 8 / 64;
+  static_assert((size_t)Tile::WM * Tile::WN * 32 * kPitch * 4 <= (size_t)Tile::kLds, "slabs fit in the stages' place");
   float* e;
   __device__ __forceinline__ explicit Slab(uint8_t* lds) {
-    e = reinterpret_cast<float*>(lds) + (threadIdx.x >> 6) * 32 * kSlabPitch;
+    e = reinterpret_cast<float*>(lds) + (threadIdx.x >> 6) * 32 * kPitch;
   }
   __device__ __forceinline__ void put(int j, int q, const float (&v)[4]) {
     const int lane = threadIdx.x & 63;
     typedef float f4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<f4*>(e + (lane & 31) * kSlabPitch + j * 32 + 8 * q + 4 * (lane >> 5)) = f4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f4*>(e + (lane & 31) * kPitch + j * 32 + 8 * q + 4 * (lane >> 5)) = f4{v[0], v[1], v[2], v[3]};
   }
-  __device__ __forceinline__ void row8(int row, int c, float (&v)[8]) const { load_pack(e + row * kSlabPitch + c, v); }
+  __device__ __forceinline__ void row8(int row, int c, float (&v)[8]) const { load_pack(e + row * kPitch + c, v); }
   __device__ __forceinline__ void col8(int row, int c, float (&v)[8]) const {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = e[(row + k) * kSlabPitch + c];
+    for (int k = 0; k < 8; ++k) v[k] = e[(row + k) * kPitch + c];
   }
 };
 
@@ -277,19 +316,31 @@ struct GradArgs {
   int row_terms, col_terms;
 };
 
+// N terms of eight gradients (far from the largest number: nothing is rounded up to infinity).
 template <int N>
-__device__ __forceinline__ void store_terms(const float (&v)[8], uint16_t* p, int64_t plane) {
-  v4w w[N];
-  terms8<N>(v, w);
+__device__ __forceinline__ void store_terms(float (&v)[8], uint16_t* p, int64_t plane) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) *reinterpret_cast<v4w*>(p + i * plane) = w[i];
+  for (int i = 0; i < N; ++i) {
+    v4w w;
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+      const uint16_t lo = from_f32<uint16_t>(v[k]), hi = from_f32<uint16_t>(v[k + 1]);
+      w[k / 2] = (uint32_t)lo | (uint32_t)hi << 16;
+      if (i + 1 < N) {
+        v[k] -= to_f32(lo);
+        v[k + 1] -= to_f32(hi);
+      }
+    }
+    *reinterpret_cast<v4w*>(p + i * plane) = w;
+  }
 }
-__device__ __forceinline__ void store_terms(int n, const float (&v)[8], uint16_t* p, int64_t plane) {
+__device__ __forceinline__ void store_terms(int n, float (&v)[8], uint16_t* p, int64_t plane) {
   if (n == 1) store_terms<1>(v, p, plane);
   else if (n == 2) store_terms<2>(v, p, plane);
   else store_terms<3>(v, p, plane);
 }
 
+template <typename Tile>
 __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g, GradArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[Tile::kLds];
   int tm, tn;
@@ -297,36 +348,45 @@ __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g
   const int64_t m0 = (int64_t)tm * Tile::BM, n0 = (int64_t)tn * Tile::BN;
   Tile tile;
   tile.run(g, m0, n0, 0, g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK), lds);
-  const Lane at(m0, n0);
+  const Lane<Tile> at(m0, n0);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t rows0 = m0 + (wave / Tile::WN) * Tile::TM * 32, cols0 = n0 + (wave % Tile::WN) * kSlabCols;
+  const int64_t rows0 = m0 + (wave / Tile::WN) * Tile::TM * 32, cols0 = n0 + (wave % Tile::WN) * Slab<Tile>::kCols;
   const float each = a.smoothing / (float)a.V;
-  Slab slab(lds);
+  const bool whole = n0 + Tile::BN <= a.cols;
+  Slab<Tile> slab(lds);
 #pragma unroll
   for (int i = 0; i < Tile::TM; ++i) {
     const int64_t row = at.row(i);
     const int64_t y = row < a.T ? target_of(a.targets, a.i64, row) : -1;
     const bool kept = y >= 0 && y < a.V;
     const float up = kept ? a.dloss[row] * a.scale : 0.0f, base = kept ? a.lse[row] : 0.0f;
+    const bool any_out = !whole || __ballot(!kept);
+    const int64_t rel = y - a.v0 - cols0;
+    const int mine = kept && rel >= 0 && rel < Slab<Tile>::kCols ? (int)rel - 4 * (lane >> 5) : -8;
+    const bool any_target = __ballot(mine != -8);
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int64_t c = at.col(j, q) + k;
-          // the difference first: near the maximum it is exact
-          float p = __builtin_amdgcn_exp2f(fmaf(tile.acc[i][j][4 * q + k], a.scale, -base) * kLog2e) - each;
-          if (a.v0 + c == y) p -= 1.0f - a.smoothing;
-          v[k] = kept && c < a.cols ? p * up : 0.0f;
-        }
+        for (int k = 0; k < 4; ++k)   // the difference first: near the maximum it is exact
+          v[k] = __builtin_amdgcn_exp2f(fmaf(tile.acc[i][j][4 * q + k], a.scale, -base) * kLog2e) - each;
+        if (any_target)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (mine == j * 32 + 8 * q + k) v[k] -= 1.0f - a.smoothing;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] *= up;
+        if (any_out)   // whatever the row holds
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = kept && at.col(j, q) + k < a.cols ? v[k] : 0.0f;
         slab.put(j, q, v);
       }
     // in the order of the rows, and transposed
 #pragma unroll
-    for (int u = 0; u < 32 * kSlabCols / 8 / 64; ++u) {
-      const int item = lane + u * 64, r = item / (kSlabCols / 8), c = item % (kSlabCols / 8) * 8;
+    for (int u = 0; u < Slab<Tile>::kItems; ++u) {
+      const int item = lane + u * 64, r = item / (Slab<Tile>::kCols / 8), c = item % (Slab<Tile>::kCols / 8) * 8;
       const int64_t gr = rows0 + i * 32 + r, gc = cols0 + c;
       if (gr < a.T && gc < a.cols) {
         float v[8];
@@ -335,7 +395,7 @@ __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g
       }
     }
 #pragma unroll
-    for (int u = 0; u < 32 * kSlabCols / 8 / 64; ++u) {
+    for (int u = 0; u < Slab<Tile>::kItems; ++u) {
       const int item = lane + u * 64, c = item / 4, r = item % 4 * 8;
       const int64_t gr = rows0 + i * 32 + r, gc = cols0 + c;
       if (gr < a.T && gc < a.cols) {
@@ -346,6 +406,9 @@ __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g
     }
   }
 }
+
+template __global__ void grad_tile_kernel<BigTile>(Bf16Product, GradArgs);
+template __global__ void grad_tile_kernel<SmallTile>(Bf16Product, GradArgs);
 
 // Where a product's sums go: partial sums (fp32, one matrix a split, added to when `add`), or an
 // output of type fp32 or bf16, added to when `add`; `before` (fp32) is added too.
@@ -379,6 +442,7 @@ struct OutArgs {
   }
 };
 
+template <typename Tile>
 __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g, OutArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[Tile::kLds];
   int tm, tn;
@@ -389,8 +453,8 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
   Tile tile;
   tile.run(g, m0, n0, beg, end, lds);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t rows0 = m0 + (wave / Tile::WN) * Tile::TM * 32, cols0 = n0 + (wave % Tile::WN) * kSlabCols;
-  Slab slab(lds);
+  const int64_t rows0 = m0 + (wave / Tile::WN) * Tile::TM * 32, cols0 = n0 + (wave % Tile::WN) * Slab<Tile>::kCols;
+  Slab<Tile> slab(lds);
 #pragma unroll
   for (int i = 0; i < Tile::TM; ++i) {
 #pragma unroll
@@ -401,8 +465,8 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
         slab.put(j, q, v);
       }
 #pragma unroll
-    for (int u = 0; u < 32 * kSlabCols / 8 / 64; ++u) {
-      const int item = lane + u * 64, r = item / (kSlabCols / 8), c = item % (kSlabCols / 8) * 8;
+    for (int u = 0; u < Slab<Tile>::kItems; ++u) {
+      const int item = lane + u * 64, r = item / (Slab<Tile>::kCols / 8), c = item % (Slab<Tile>::kCols / 8) * 8;
       const int64_t row = rows0 + i * 32 + r, col = cols0 + c;
       if (row >= a.M || col >= a.N) continue;
       float v[8];
@@ -424,6 +488,9 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
     }
   }
 }
+
+template __global__ void out_tile_kernel<BigTile>(Bf16Product, OutArgs);
+template __global__ void out_tile_kernel<SmallTile>(Bf16Product, OutArgs);
 
 // The splits' sums, in order, to the output.
 __global__ __launch_bounds__(256) void out_join_kernel(OutArgs a, const float* __restrict__ part, int splits) {
@@ -463,15 +530,35 @@ PlanePairs pairs_of(int na, int nb) {
   return p;
 }
 
-// Splits of a reduction of `stages` stages over `tiles` tiles: enough for two workgroups a CU, of
-// four stages at least.
-int splits_of(int64_t tiles, int64_t stages) {
-  if (tiles >= 256) return 1;
-  int64_t s = ceil_div(512, tiles);
-  if (s > stages / 4) s = stages / 4;
-  if (s > 64) s = 64;
-  return s < 1 ? 1 : (int)s;
+// A product's tile and the splits of its reduction, by predicted time: a CU's one large tile takes
+// 1.65 us a stage of 64 k, its two small ones 1.0 (0.6 alone), and beginning and end 4 us; the splits'
+// sums are written and read again.
+struct Choice {
+  bool big;
+  int splits;
+};
+Choice choose(int64_t M, int64_t N, int64_t stages, int most_splits) {
+  Choice best{false, 1};
+  double least = 1e300;
+  for (int big = 0; big < 2; ++big) {
+    const int64_t edge = big ? 256 : 128, tiles = ceil_div(M, edge) * ceil_div(N, edge);
+    for (int s = 1; s <= most_splits && (s == 1 || stages / s >= 2); ++s) {
+      const int64_t groups = tiles * s, slots = big ? 256 : 512;
+      const double stage = big ? 1.65 : groups <= 256 ? 0.6 : 1.0;
+      double t = (double)ceil_div(groups, slots) * ((double)ceil_div(stages, s) * stage + 4.0);
+      if (s > 1) t += 3.0 + (double)s * M * N * 8.0 / 4.5e6;
+      if (t < least) {
+        least = t;
+        best = {big != 0, s};
+      }
+    }
+  }
+  return best;
 }
+
+int64_t edge_of(bool big) { return big ? BigTile::BM : SmallTile::BM; }
+static_assert(BigTile::BM == BigTile::BN && SmallTile::BM == SmallTile::BN && BigTile::BK == SmallTile::BK, "square tiles");
+constexpr int kStage = BigTile::BK;
 
 struct Carver {
   size_t at = 0;
@@ -489,13 +576,14 @@ struct Layout {
   bool pack_x, pack_t;        // laid out in rows: fp32, or rows that are no whole 16-byte pieces
   size_t x_rows, t_rows;      // offsets in the workspace
   // forward
+  Choice z;                   // the logits' tile
   int64_t parts;
   size_t part, at_target;
   // backward
   int64_t piece, pieces;
   int g_rows, g_cols;         // terms of g in the product for dx, and in that for dtable
   int tx, xt;                 // terms of the table and of x in these products
-  int splits_x, splits_w;
+  Choice by_x, by_w;          // the tiles of the products for dx and dtable
   size_t x_cols, t_cols, g, gt, sum_x, sum_w;
   bool sums_x;
   size_t bytes;
@@ -508,7 +596,8 @@ struct Layout {
     t_rows = c.take(pack_t ? (size_t)tn * V * D8 * 2 : 0);
   }
   void forward() {
-    parts = ceil_div(V, Tile::BN) * Tile::WN;
+    z = choose(T, V, logits_stages(), 1);
+    parts = ceil_div(V, edge_of(z.big)) * (z.big ? BigTile::WN : SmallTile::WN);
     part = c.take((size_t)parts * 3 * T * sizeof(float));
     at_target = c.take((size_t)T * sizeof(float));
     bytes = c.at;
@@ -527,19 +616,21 @@ struct Layout {
     tx = x_bf16 && tn > 2 ? 2 : tn;
     g_cols = g_bf16 ? 1 : x_bf16 ? 2 : 3;
     xt = g_bf16 && xn > 2 ? 2 : xn;
-    splits_x = splits_of(ceil_div(T, Tile::BM) * ceil_div(D, Tile::BN),
-                         pairs_of(g_rows, tx).count * ceil_div(piece, Tile::BK));
-    splits_w = splits_of(ceil_div(piece < V ? piece : V, Tile::BM) * ceil_div(D, Tile::BN),
-                         pairs_of(g_cols, xt).count * ceil_div(T8, Tile::BK));
+    const int64_t rows = piece < V ? piece : V;
+    z = choose(T, rows, logits_stages(), 1);
+    by_x = choose(T, D, pairs_of(g_rows, tx).count * ceil_div(up8(rows), kStage), 64);
+    by_w = choose(rows, D, pairs_of(g_cols, xt).count * ceil_div(T8, kStage), 64);
     x_cols = c.take((size_t)xt * D * T8 * 2);
     t_cols = c.take((size_t)tx * D * piece * 2);
     g = c.take((size_t)g_rows * T * piece * 2);
     gt = c.take((size_t)g_cols * piece * T8 * 2);
-    sums_x = splits_x > 1 || pieces > 1;
-    sum_x = c.take(sums_x ? (size_t)splits_x * T * D * sizeof(float) : 0);
-    sum_w = c.take(splits_w > 1 ? (size_t)splits_w * piece * D * sizeof(float) : 0);
+    sums_x = by_x.splits > 1 || pieces > 1;
+    sum_x = c.take(sums_x ? (size_t)by_x.splits * T * D * sizeof(float) : 0);
+    sum_w = c.take(by_w.splits > 1 ? (size_t)by_w.splits * piece * D * sizeof(float) : 0);
     bytes = c.at;
   }
+
+  int64_t logits_stages() const { return pairs_of(xn, tn).count * ceil_div(D8, kStage); }
 
  private:
   Carver c;
@@ -589,15 +680,30 @@ Bf16Product logits_product(const CrossEntropyArgs& a, const Layout& l, uint8_t* 
   return g;
 }
 
-void place(Bf16Product& g, int64_t M, int64_t N) {
-  g.tiles_m = (int)ceil_div(M, Tile::BM);
-  g.tiles_n = (int)ceil_div(N, Tile::BN);
+void place(Bf16Product& g, int64_t M, int64_t N, bool big) {
+  g.tiles_m = (int)ceil_div(M, edge_of(big));
+  g.tiles_n = (int)ceil_div(N, edge_of(big));
 }
 
-void out_product(const Bf16Product& g, OutArgs o, int splits, hipStream_t st) {
-  const int stages = g.pairs.count * (int)ceil_div(g.K, Tile::BK);
-  o.chunk = (int)ceil_div(stages, splits);
-  hipLaunchKernelGGL(out_tile_kernel, dim3((unsigned)g.tiles_m * g.tiles_n, splits), dim3(Tile::kThreads), 0, st, g, o);
+template <typename Tile>
+void loss_tiles(const Bf16Product& g, const LossArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((loss_tile_kernel<Tile>), dim3((unsigned)g.tiles_m * g.tiles_n), dim3(Tile::kThreads), 0, st, g, a);
+}
+template <typename Tile>
+void grad_tiles(const Bf16Product& g, const GradArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((grad_tile_kernel<Tile>), dim3((unsigned)g.tiles_m * g.tiles_n), dim3(Tile::kThreads), 0, st, g, a);
+}
+template <typename Tile>
+void out_tiles(const Bf16Product& g, const OutArgs& a, int splits, hipStream_t st) {
+  hipLaunchKernelGGL((out_tile_kernel<Tile>), dim3((unsigned)g.tiles_m * g.tiles_n, splits), dim3(Tile::kThreads), 0, st, g, a);
+}
+
+void out_product(Bf16Product g, OutArgs o, Choice c, hipStream_t st) {
+  place(g, o.M, o.N, c.big);
+  const int stages = g.pairs.count * (int)ceil_div(g.K, kStage);
+  o.chunk = (int)ceil_div(stages, c.splits);
+  if (c.big) out_tiles<BigTile>(g, o, c.splits, st);
+  else out_tiles<SmallTile>(g, o, c.splits, st);
 }
 
 void out_join(const OutArgs& o, const float* part, int splits, hipStream_t st) {
@@ -630,10 +736,11 @@ hipError_t launch_cross_entropy_fwd(const CrossEntropyArgs& a, float* loss, floa
   l.forward();
   uint8_t* const w = static_cast<uint8_t*>(ws);
   Bf16Product g = logits_product(a, l, w, st);
-  place(g, a.T, a.V);
-  const LossArgs la{a.targets, a.i64, a.T, a.V, a.scale, reinterpret_cast<float*>(w + l.part),
+  place(g, a.T, a.V, l.z.big);
+  const LossArgs la{a.targets, a.i64, a.T, a.V, a.scale, a.smoothing > 0.0f, reinterpret_cast<float*>(w + l.part),
                     reinterpret_cast<float*>(w + l.at_target)};
-  hipLaunchKernelGGL(loss_tile_kernel, dim3((unsigned)g.tiles_m * g.tiles_n), dim3(Tile::kThreads), 0, st, g, la);
+  if (l.z.big) loss_tiles<BigTile>(g, la, st);
+  else loss_tiles<SmallTile>(g, la, st);
   hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)ceil_div(a.T, 64)), dim3(1024), 0, st, la, l.parts, a.smoothing, loss, lse);
   return hipGetLastError();
 }
@@ -662,10 +769,11 @@ hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dlos
     const int64_t v0 = p * l.piece, cols = a.V - v0 < l.piece ? a.V - v0 : l.piece;
     // g of the piece
     z.B = {logits_b.p + v0 * logits_b.ld, cols, logits_b.ld, logits_b.plane};
-    place(z, a.T, cols);
+    place(z, a.T, cols, l.z.big);
     const GradArgs ga{a.targets, a.i64, a.T, a.V, v0, cols, a.scale, a.smoothing, dloss, lse,
                       half(l.g), l.piece, a.T * l.piece, half(l.gt), l.T8, l.piece * l.T8, l.g_rows, l.g_cols};
-    hipLaunchKernelGGL(grad_tile_kernel, dim3((unsigned)z.tiles_m * z.tiles_n), dim3(Tile::kThreads), 0, st, z, ga);
+    if (l.z.big) grad_tiles<BigTile>(z, ga, st);
+    else grad_tiles<SmallTile>(z, ga, st);
     // dx += g W
     const size_t elem = a.t_bf16 ? 2 : 4;
     pack_cols({static_cast<const uint8_t*>(a.table) + (size_t)v0 * a.D * elem, cols, a.D, nullptr, 0, 0, half(l.t_cols), up8(cols),
@@ -676,31 +784,29 @@ hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dlos
     x.B = {half(l.t_cols), a.D, up8(cols), a.D * up8(cols)};
     x.pairs = pairs_of(l.g_rows, l.tx);
     x.K = up8(cols);
-    place(x, a.T, a.D);
     OutArgs ox{a.T, a.D, l.sums_x ? reinterpret_cast<float*>(w + l.sum_x) : nullptr, dx, a.x_bf16, p > 0, a.targets, a.i64, a.V, 0};
-    out_product(x, ox, l.splits_x, st);
+    out_product(x, ox, l.by_x, st);
     // dW = g^T x
     Bf16Product t;
     t.A = {half(l.gt), cols, l.T8, l.piece * l.T8};
     t.B = {half(l.x_cols), a.D, l.T8, a.D * l.T8};
     t.pairs = pairs_of(l.g_cols, l.xt);
     t.K = l.T8;
-    place(t, cols, a.D);
     uint8_t* const rows = static_cast<uint8_t*>(dtable) + (size_t)v0 * a.D * (g_bf16 ? 2 : 4);
     OutArgs ow{cols, a.D, nullptr, rows, g_bf16, accumulate, nullptr, 0, 0, 0};
-    if (l.splits_w > 1) {
+    if (l.by_w.splits > 1) {
       OutArgs sums = ow;
       sums.part = reinterpret_cast<float*>(w + l.sum_w);
       sums.add = 0;
-      out_product(t, sums, l.splits_w, st);
-      out_join(ow, sums.part, l.splits_w, st);
+      out_product(t, sums, l.by_w, st);
+      out_join(ow, sums.part, l.by_w.splits, st);
     } else {
-      out_product(t, ow, 1, st);
+      out_product(t, ow, l.by_w, st);
     }
   }
   if (l.sums_x) {
     const OutArgs ox{a.T, a.D, nullptr, dx, a.x_bf16, 0, a.targets, a.i64, a.V, 0};
-    out_join(ox, reinterpret_cast<const float*>(w + l.sum_x), l.splits_x, st);
+    out_join(ox, reinterpret_cast<const float*>(w + l.sum_x), l.by_x.splits, st);
   }
   return hipGetLastError();
 }

@@ -56,7 +56,7 @@ LOSS = dict(x=P, xt=1, table=P2, tt=1, targets=P3, it=0, T=5, V=100, D=64, scale
 LOSS_BAD = [(dict(xt=2), DTYPE), (dict(tt=-1), DTYPE), (dict(it=2), DTYPE), (dict(T=-1), SHAPE), (dict(T=(1 << 21) + 1), SHAPE),
             (dict(V=0), SHAPE), (dict(V=(1 << 28) + 1), SHAPE), (dict(D=0), SHAPE), (dict(D=(1 << 17) + 1), SHAPE),
             (dict(T=1 << 21, V=1 << 17), SHAPE), (dict(T=1 << 20, D=(1 << 16) + 1), SHAPE), (dict(V=1 << 20, D=(1 << 16) + 1), SHAPE),
-            (dict(scale=INF), PARAM), (dict(scale=NAN), PARAM), (dict(smoothing=-0.1), PARAM), (dict(smoothing=1.1), PARAM),
+            (dict(scale=INF), PARAM), (dict(scale=NAN), PARAM), (dict(scale=0.0), PARAM), (dict(smoothing=-0.1), PARAM), (dict(smoothing=1.1), PARAM),
             (dict(smoothing=NAN), PARAM), (dict(x=NUL), NULL), (dict(table=NUL), NULL), (dict(targets=NUL), NULL),
             (dict(lse=NUL), NULL), (dict(x=P8), ALIGN), (dict(table=P8), ALIGN), (dict(targets=HALF), ALIGN),
             (dict(targets=P4, it=1), ALIGN), (dict(lse=HALF), ALIGN), (dict(ws=NUL), WSP), (dict(ws_bytes=16), WSP), (dict(ws=P8), ALIGN)]
