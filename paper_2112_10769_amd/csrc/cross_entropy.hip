@@ -6,13 +6,12 @@
 //
 // Forward: a tile of products leaves each row's maximum, sum of exponentials and sum of logits over
 // its columns; a second launch joins them.  Backward: a piece of the vocabulary at a time, the
-// products again, their gradient g in bf16 (in both orders), and the two products with it.  All four
-// products are the K-major tile of bf16_tile.hpp; operands that lie otherwise are laid out first.
+// products again, their gradient g in bf16, and the two products with it, whose operands lie
+// across the reduction: they are transposed on the way out of LDS (written a second time, transposed,
+// g took 130 of 447 us for 4096 x 32000 of it, and the table's and x's transposes 50).
 //
 // g in bf16 is what a bf16 product takes; its rounding is of the size of a bf16 output's own.  An
 // fp32 output takes two bf16 terms of g with bf16 activations, three with fp32 ones.
-#include <type_traits>
-
 #include "bf16_tile.hpp"
 #include "luq_launch.hpp"
 
@@ -54,7 +53,7 @@ __device__ __forceinline__ void terms8(const float (&v)[8], v4w (&w)[N]) {
   }
 }
 
-// ---- operands laid out: terms of a matrix, its rows a multiple of eight long, or its transpose
+// ---- operands laid out: terms of a matrix, its rows a multiple of eight long
 
 struct PackArgs {
   const void* src;      // [rows][cols]
@@ -85,38 +84,6 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackArgs a) {
     terms8<N>(v, w);
 #pragma unroll
     for (int i = 0; i < N; ++i) *reinterpret_cast<v4w*>(a.out + i * a.plane + row * a.ld + c) = w[i];
-  }
-}
-
-// [cols][ld], ld at least rows: 64 x 64 elements a workgroup.
-template <typename T, int N>
-__global__ __launch_bounds__(256) void pack_cols_kernel(PackArgs a) {
-  __shared__ float tile[64][65];
-  const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int at = threadIdx.x + u * 256, row = at / 8, c = (at & 7) * 8;
-    float v[8];
-    const bool in = r0 + row < a.rows && c0 + c < a.cols;
-    if (in && a.kept(r0 + row)) load_row<8>(static_cast<const T*>(a.src) + (r0 + row) * a.cols + c0 + c, a.cols - c0 - c, v);
-    else
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) tile[row][c + k] = v[k];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int at = threadIdx.x + u * 256, c = at / 8, row = (at & 7) * 8;
-    if (c0 + c >= a.cols || r0 + row >= a.ld) continue;
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = tile[row + k][c];
-    v4w w[N];
-    terms8<N>(v, w);
-#pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<v4w*>(a.out + i * a.plane + (c0 + c) * a.ld + r0 + row) = w[i];
   }
 }
 
@@ -157,7 +124,7 @@ __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g
   bf16_tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
   const int64_t m0 = (int64_t)tm * Tile::BM, n0 = (int64_t)tn * Tile::BN;
   Tile tile;
-  tile.run(g, m0, n0, 0, g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK), lds);
+  tile.template run<false, false>(g, m0, n0, 0, g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK), lds);
   const Lane<Tile> at(m0, n0);
   const float c = a.scale * kLog2e;
   const int half = (threadIdx.x & 63) >> 5;
@@ -295,9 +262,36 @@ struct Slab {
     *reinterpret_cast<f4*>(e + (lane & 31) * kPitch + j * 32 + 8 * q + 4 * (lane >> 5)) = f4{v[0], v[1], v[2], v[3]};
   }
   __device__ __forceinline__ void row8(int row, int c, float (&v)[8]) const { load_pack(e + row * kPitch + c, v); }
-  __device__ __forceinline__ void col8(int row, int c, float (&v)[8]) const {
+};
+
+// The same in bf16.
+template <typename Tile>
+struct HalfSlab {
+  static constexpr int kCols = Tile::TN * 32, kPitch = kCols * 2 + 8, kItems = 32 * kCols / 8 / 64;
+  static_assert((size_t)Tile::WM * Tile::WN * 32 * kPitch <= (size_t)Tile::kLds, "slabs fit in the stages' place");
+  typedef uint32_t v2w __attribute__((ext_vector_type(2)));
+  uint8_t* e;
+  int lane;
+  __device__ __forceinline__ explicit HalfSlab(uint8_t* lds) : lane(threadIdx.x & 63) {
+    e = lds + (threadIdx.x >> 6) * 32 * kPitch;
+  }
+  // the lane's four columns of its row, and what rounding to bf16 leaves of them
+  __device__ __forceinline__ void put(int j, int q, float* v) const {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    v2w w;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = e[(row + k) * kPitch + c];
+    for (int k = 0; k < 2; ++k) {
+      w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[2 * k], v[2 * k + 1]}, bf2));
+      v[2 * k] -= __uint_as_float(w[k] << 16);
+      v[2 * k + 1] -= __uint_as_float(w[k] & 0xFFFF0000u);
+    }
+    *reinterpret_cast<v2w*>(e + (lane & 31) * kPitch + (j * 32 + 8 * q + 4 * (lane >> 5)) * 2) = w;
+  }
+  __device__ __forceinline__ v4w row8(int row, int c) const {
+    const v2w* const p = reinterpret_cast<const v2w*>(e + row * kPitch + c * 2);
+    const v2w a = p[0], b = p[1];
+    return v4w{a[0], a[1], b[0], b[1]};
   }
 };
 
@@ -309,36 +303,10 @@ struct GradArgs {
   float scale, smoothing;
   const float* dloss;
   const float* lse;
-  uint16_t* g;         // [row_terms][T][ld_g]: columns up to the next multiple of eight are written
-  int64_t ld_g, plane_g;
-  uint16_t* gt;        // [col_terms][cols][ld_t]: ld_t is T's next multiple of eight
-  int64_t ld_t, plane_t;
-  int row_terms, col_terms;
+  uint16_t* g;         // [terms][T][ld]: columns up to the next multiple of eight are written
+  int64_t ld, plane;
+  int terms;
 };
-
-// N terms of eight gradients (far from the largest number: nothing is rounded up to infinity).
-template <int N>
-__device__ __forceinline__ void store_terms(float (&v)[8], uint16_t* p, int64_t plane) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v4w w;
-#pragma unroll
-    for (int k = 0; k < 8; k += 2) {
-      const uint16_t lo = from_f32<uint16_t>(v[k]), hi = from_f32<uint16_t>(v[k + 1]);
-      w[k / 2] = (uint32_t)lo | (uint32_t)hi << 16;
-      if (i + 1 < N) {
-        v[k] -= to_f32(lo);
-        v[k + 1] -= to_f32(hi);
-      }
-    }
-    *reinterpret_cast<v4w*>(p + i * plane) = w;
-  }
-}
-__device__ __forceinline__ void store_terms(int n, float (&v)[8], uint16_t* p, int64_t plane) {
-  if (n == 1) store_terms<1>(v, p, plane);
-  else if (n == 2) store_terms<2>(v, p, plane);
-  else store_terms<3>(v, p, plane);
-}
 
 template <typename Tile>
 __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g, GradArgs a) {
@@ -347,13 +315,13 @@ __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g
   bf16_tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
   const int64_t m0 = (int64_t)tm * Tile::BM, n0 = (int64_t)tn * Tile::BN;
   Tile tile;
-  tile.run(g, m0, n0, 0, g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK), lds);
+  tile.template run<false, false>(g, m0, n0, 0, g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK), lds);
   const Lane<Tile> at(m0, n0);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t rows0 = m0 + (wave / Tile::WN) * Tile::TM * 32, cols0 = n0 + (wave % Tile::WN) * Slab<Tile>::kCols;
   const float each = a.smoothing / (float)a.V;
   const bool whole = n0 + Tile::BN <= a.cols;
-  Slab<Tile> slab(lds);
+  const HalfSlab<Tile> slab(lds);
 #pragma unroll
   for (int i = 0; i < Tile::TM; ++i) {
     const int64_t row = at.row(i);
@@ -362,47 +330,31 @@ __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g
     const float up = kept ? a.dloss[row] * a.scale : 0.0f, base = kept ? a.lse[row] : 0.0f;
     const bool any_out = !whole || __ballot(!kept);
     const int64_t rel = y - a.v0 - cols0;
-    const int mine = kept && rel >= 0 && rel < Slab<Tile>::kCols ? (int)rel - 4 * (lane >> 5) : -8;
+    const int mine = kept && rel >= 0 && rel < HalfSlab<Tile>::kCols ? (int)rel - 4 * (lane >> 5) : -8;
     const bool any_target = __ballot(mine != -8);
+    float v[Tile::TN][16];
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)   // the difference first: near the maximum it is exact
-          v[k] = __builtin_amdgcn_exp2f(fmaf(tile.acc[i][j][4 * q + k], a.scale, -base) * kLog2e) - each;
-        if (any_target)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (mine == j * 32 + 8 * q + k) v[k] -= 1.0f - a.smoothing;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] *= up;
-        if (any_out)   // whatever the row holds
-#pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = kept && at.col(j, q) + k < a.cols ? v[k] : 0.0f;
-        slab.put(j, q, v);
+      for (int e = 0; e < 16; ++e) {   // the difference first: near the maximum it is exact
+        v[j][e] = __builtin_amdgcn_exp2f(fmaf(tile.acc[i][j][e], a.scale, -base) * kLog2e) - each;
+        if (any_target && mine == j * 32 + 8 * (e / 4) + e % 4) v[j][e] -= 1.0f - a.smoothing;
+        v[j][e] *= up;
+        if (any_out) v[j][e] = kept && at.col(j, e / 4) + e % 4 < a.cols ? v[j][e] : 0.0f;   // whatever the row holds
       }
-    // in the order of the rows, and transposed
+    for (int n = 0; n < a.terms; ++n) {
 #pragma unroll
-    for (int u = 0; u < Slab<Tile>::kItems; ++u) {
-      const int item = lane + u * 64, r = item / (Slab<Tile>::kCols / 8), c = item % (Slab<Tile>::kCols / 8) * 8;
-      const int64_t gr = rows0 + i * 32 + r, gc = cols0 + c;
-      if (gr < a.T && gc < a.cols) {
-        float v[8];
-        slab.row8(r, c, v);
-        store_terms(a.row_terms, v, a.g + gr * a.ld_g + gc, a.plane_g);
-      }
-    }
+      for (int j = 0; j < Tile::TN; ++j)
 #pragma unroll
-    for (int u = 0; u < Slab<Tile>::kItems; ++u) {
-      const int item = lane + u * 64, c = item / 4, r = item % 4 * 8;
-      const int64_t gr = rows0 + i * 32 + r, gc = cols0 + c;
-      if (gr < a.T && gc < a.cols) {
-        float v[8];
-        slab.col8(r, c, v);
-        store_terms(a.col_terms, v, a.gt + gc * a.ld_t + gr, a.plane_t);
+        for (int q = 0; q < 4; ++q) slab.put(j, q, &v[j][4 * q]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int u = 0; u < HalfSlab<Tile>::kItems; ++u) {
+        const int item = lane + u * 64, r = item / (HalfSlab<Tile>::kCols / 8), c = item % (HalfSlab<Tile>::kCols / 8) * 8;
+        const int64_t gr = rows0 + i * 32 + r, gc = cols0 + c;
+        if (gr < a.T && gc < a.cols) *reinterpret_cast<v4w*>(a.g + n * a.plane + gr * a.ld + gc) = slab.row8(r, c);
       }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
   }
 }
@@ -442,7 +394,8 @@ struct OutArgs {
   }
 };
 
-template <typename Tile>
+// CA: A lies across the reduction (g^T); B does in both products.
+template <typename Tile, bool CA>
 __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g, OutArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[Tile::kLds];
   int tm, tn;
@@ -451,7 +404,7 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
   const int stages = g.pairs.count * (int)((g.K + Tile::BK - 1) / Tile::BK);
   const int beg = blockIdx.y * a.chunk, end = min(beg + a.chunk, stages);
   Tile tile;
-  tile.run(g, m0, n0, beg, end, lds);
+  tile.template run<CA, true>(g, m0, n0, beg, end, lds);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t rows0 = m0 + (wave / Tile::WN) * Tile::TM * 32, cols0 = n0 + (wave % Tile::WN) * Slab<Tile>::kCols;
   Slab<Tile> slab(lds);
@@ -489,8 +442,10 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
   }
 }
 
-template __global__ void out_tile_kernel<BigTile>(Bf16Product, OutArgs);
-template __global__ void out_tile_kernel<SmallTile>(Bf16Product, OutArgs);
+template __global__ void out_tile_kernel<BigTile, false>(Bf16Product, OutArgs);
+template __global__ void out_tile_kernel<SmallTile, false>(Bf16Product, OutArgs);
+template __global__ void out_tile_kernel<BigTile, true>(Bf16Product, OutArgs);
+template __global__ void out_tile_kernel<SmallTile, true>(Bf16Product, OutArgs);
 
 // The splits' sums, in order, to the output.
 __global__ __launch_bounds__(256) void out_join_kernel(OutArgs a, const float* __restrict__ part, int splits) {
@@ -571,7 +526,7 @@ struct Carver {
 
 // How a call is laid out; the same for its workspace query and its launches.
 struct Layout {
-  int64_t T, V, D, T8, D8;
+  int64_t T, V, D, D8;
   int xn, tn;                 // terms of x and the table
   bool pack_x, pack_t;        // laid out in rows: fp32, or rows that are no whole 16-byte pieces
   size_t x_rows, t_rows;      // offsets in the workspace
@@ -581,16 +536,18 @@ struct Layout {
   size_t part, at_target;
   // backward
   int64_t piece, pieces;
-  int g_rows, g_cols;         // terms of g in the product for dx, and in that for dtable
+  int g_x, g_w;               // terms of g in the product for dx, and in that for dtable
   int tx, xt;                 // terms of the table and of x in these products
   Choice by_x, by_w;          // the tiles of the products for dx and dtable
-  size_t x_cols, t_cols, g, gt, sum_x, sum_w;
+  size_t g, sum_x, sum_w;
   bool sums_x;
   size_t bytes;
-  Layout(int64_t T_, int64_t V_, int64_t D_, int x_bf16, int t_bf16) : T(T_), V(V_), D(D_), T8(up8(T_)), D8(up8(D_)) {
+  // x is laid out in the backward call too where it need not be: a row that is padding becomes
+  // zeros, since 0 times what it holds need not be 0.
+  Layout(int64_t T_, int64_t V_, int64_t D_, int x_bf16, int t_bf16, bool back) : T(T_), V(V_), D(D_), D8(up8(D_)) {
     xn = x_bf16 ? 1 : 3;
     tn = t_bf16 ? 1 : 3;
-    pack_x = !x_bf16 || (D & 7);
+    pack_x = back || !x_bf16 || (D & 7);
     pack_t = !t_bf16 || (D & 7);
     x_rows = c.take(pack_x ? (size_t)xn * T * D8 * 2 : 0);
     t_rows = c.take(pack_t ? (size_t)tn * V * D8 * 2 : 0);
@@ -612,66 +569,48 @@ struct Layout {
     pieces = ceil_div(V, most);
     piece = ceil_div(ceil_div(V, pieces), 128) * 128;
     pieces = ceil_div(V, piece);
-    g_rows = x_bf16 ? 1 : 3;
+    g_x = x_bf16 ? 1 : 3;
     tx = x_bf16 && tn > 2 ? 2 : tn;
-    g_cols = g_bf16 ? 1 : x_bf16 ? 2 : 3;
+    g_w = g_bf16 ? 1 : x_bf16 ? 2 : 3;
     xt = g_bf16 && xn > 2 ? 2 : xn;
     const int64_t rows = piece < V ? piece : V;
     z = choose(T, rows, logits_stages(), 1);
-    by_x = choose(T, D, pairs_of(g_rows, tx).count * ceil_div(up8(rows), kStage), 64);
-    by_w = choose(rows, D, pairs_of(g_cols, xt).count * ceil_div(T8, kStage), 64);
-    x_cols = c.take((size_t)xt * D * T8 * 2);
-    t_cols = c.take((size_t)tx * D * piece * 2);
-    g = c.take((size_t)g_rows * T * piece * 2);
-    gt = c.take((size_t)g_cols * piece * T8 * 2);
+    by_x = choose(T, D, pairs_of(g_x, tx).count * ceil_div(up8(rows), kStage), 64);
+    by_w = choose(rows, D, pairs_of(g_w, xt).count * ceil_div(T, kStage), 64);
+    g = c.take((size_t)g_terms() * T * piece * 2);
     sums_x = by_x.splits > 1 || pieces > 1;
     sum_x = c.take(sums_x ? (size_t)by_x.splits * T * D * sizeof(float) : 0);
     sum_w = c.take(by_w.splits > 1 ? (size_t)by_w.splits * piece * D * sizeof(float) : 0);
     bytes = c.at;
   }
 
+  int g_terms() const { return g_x > g_w ? g_x : g_w; }
   int64_t logits_stages() const { return pairs_of(xn, tn).count * ceil_div(D8, kStage); }
 
  private:
   Carver c;
 };
 
-template <typename F>
-void with_terms(int bf16, int n, F f) {
-  if (bf16) f(uint16_t{}, std::integral_constant<int, 1>{});
-  else if (n == 2) f(float{}, std::integral_constant<int, 2>{});
-  else f(float{}, std::integral_constant<int, 3>{});
-}
-
-void pack_rows(const PackArgs& a, int bf16, int n, hipStream_t st) {
+void pack_rows(const PackArgs& a, int bf16, hipStream_t st) {
   const int64_t need = ceil_div(a.rows * (a.ld / 8), 256);
-  with_terms(bf16, n, [&](auto elem, auto count) {
-    hipLaunchKernelGGL((pack_rows_kernel<decltype(elem), decltype(count)::value>), dim3((unsigned)(need < 16384 ? need : 16384)),
-                       dim3(256), 0, st, a);
-  });
-}
-
-// The grid's second dimension has 65535 blocks: D is at most 2^17.
-void pack_cols(const PackArgs& a, int bf16, int n, hipStream_t st) {
-  with_terms(bf16, n, [&](auto elem, auto count) {
-    hipLaunchKernelGGL((pack_cols_kernel<decltype(elem), decltype(count)::value>),
-                       dim3((unsigned)ceil_div(a.ld, 64), (unsigned)ceil_div(a.cols, 64)), dim3(256), 0, st, a);
-  });
+  const dim3 grid((unsigned)(need < 16384 ? need : 16384));
+  if (bf16) hipLaunchKernelGGL((pack_rows_kernel<uint16_t, 1>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(256), 0, st, a);
 }
 
 // The operands of the logits' product, laid out if need be.
-Bf16Product logits_product(const CrossEntropyArgs& a, const Layout& l, uint8_t* ws, hipStream_t st) {
+Bf16Product logits_product(const CrossEntropyArgs& a, const Layout& l, bool back, uint8_t* ws, hipStream_t st) {
   Bf16Product g;
   g.A = {static_cast<const uint16_t*>(a.x), a.T, a.D, 0};
   g.B = {static_cast<const uint16_t*>(a.table), a.V, a.D, 0};
   if (l.pack_x) {
     uint16_t* const out = reinterpret_cast<uint16_t*>(ws + l.x_rows);
-    pack_rows({a.x, a.T, a.D, nullptr, 0, 0, out, l.D8, a.T * l.D8}, a.x_bf16, l.xn, st);
+    pack_rows({a.x, a.T, a.D, back ? a.targets : nullptr, a.i64, a.V, out, l.D8, a.T * l.D8}, a.x_bf16, st);
     g.A = {out, a.T, l.D8, a.T * l.D8};
   }
   if (l.pack_t) {
     uint16_t* const out = reinterpret_cast<uint16_t*>(ws + l.t_rows);
-    pack_rows({a.table, a.V, a.D, nullptr, 0, 0, out, l.D8, a.V * l.D8}, a.t_bf16, l.tn, st);
+    pack_rows({a.table, a.V, a.D, nullptr, 0, 0, out, l.D8, a.V * l.D8}, a.t_bf16, st);
     g.B = {out, a.V, l.D8, a.V * l.D8};
   }
   g.pairs = pairs_of(l.xn, l.tn);
@@ -693,17 +632,18 @@ template <typename Tile>
 void grad_tiles(const Bf16Product& g, const GradArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((grad_tile_kernel<Tile>), dim3((unsigned)g.tiles_m * g.tiles_n), dim3(Tile::kThreads), 0, st, g, a);
 }
-template <typename Tile>
+template <typename Tile, bool CA>
 void out_tiles(const Bf16Product& g, const OutArgs& a, int splits, hipStream_t st) {
-  hipLaunchKernelGGL((out_tile_kernel<Tile>), dim3((unsigned)g.tiles_m * g.tiles_n, splits), dim3(Tile::kThreads), 0, st, g, a);
+  hipLaunchKernelGGL((out_tile_kernel<Tile, CA>), dim3((unsigned)g.tiles_m * g.tiles_n, splits), dim3(Tile::kThreads), 0, st, g, a);
 }
 
+template <bool CA>
 void out_product(Bf16Product g, OutArgs o, Choice c, hipStream_t st) {
   place(g, o.M, o.N, c.big);
   const int stages = g.pairs.count * (int)ceil_div(g.K, kStage);
   o.chunk = (int)ceil_div(stages, c.splits);
-  if (c.big) out_tiles<BigTile>(g, o, c.splits, st);
-  else out_tiles<SmallTile>(g, o, c.splits, st);
+  if (c.big) out_tiles<BigTile, CA>(g, o, c.splits, st);
+  else out_tiles<SmallTile, CA>(g, o, c.splits, st);
 }
 
 void out_join(const OutArgs& o, const float* part, int splits, hipStream_t st) {
@@ -719,23 +659,23 @@ __global__ void zero_half_kernel(uint16_t* p) { *p = 0; }
 }  // namespace
 
 size_t cross_entropy_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int x_bf16, int t_bf16) {
-  Layout l(T, V, D, x_bf16, t_bf16);
+  Layout l(T, V, D, x_bf16, t_bf16, false);
   l.forward();
   return l.bytes;
 }
 
 size_t cross_entropy_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int x_bf16, int t_bf16, int g_bf16) {
-  Layout l(T, V, D, x_bf16, t_bf16);
+  Layout l(T, V, D, x_bf16, t_bf16, true);
   l.backward(x_bf16, g_bf16);
   return l.bytes;
 }
 
 hipError_t launch_cross_entropy_fwd(const CrossEntropyArgs& a, float* loss, float* lse, void* ws, hipStream_t st) {
   if (a.T == 0) return hipSuccess;
-  Layout l(a.T, a.V, a.D, a.x_bf16, a.t_bf16);
+  Layout l(a.T, a.V, a.D, a.x_bf16, a.t_bf16, false);
   l.forward();
   uint8_t* const w = static_cast<uint8_t*>(ws);
-  Bf16Product g = logits_product(a, l, w, st);
+  Bf16Product g = logits_product(a, l, false, w, st);
   place(g, a.T, a.V, l.z.big);
   const LossArgs la{a.targets, a.i64, a.T, a.V, a.scale, a.smoothing > 0.0f, reinterpret_cast<float*>(w + l.part),
                     reinterpret_cast<float*>(w + l.at_target)};
@@ -757,51 +697,45 @@ hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dlos
     if (bytes & 3) hipLaunchKernelGGL(zero_half_kernel, dim3(1), dim3(1), 0, st, static_cast<uint16_t*>(dtable) + words * 2);
     return hipGetLastError();
   }
-  Layout l(a.T, a.V, a.D, a.x_bf16, a.t_bf16);
+  Layout l(a.T, a.V, a.D, a.x_bf16, a.t_bf16, true);
   l.backward(a.x_bf16, g_bf16);
   uint8_t* const w = static_cast<uint8_t*>(ws);
   auto half = [&](size_t at) { return reinterpret_cast<uint16_t*>(w + at); };
-  Bf16Product z = logits_product(a, l, w, st);
-  // the transpose of x; a row that is padding is zeros: 0 times what it holds need not be 0
-  pack_cols({a.x, a.T, a.D, a.targets, a.i64, a.V, half(l.x_cols), l.T8, a.D * l.T8}, a.x_bf16, l.xt, st);
-  const Bf16Planes logits_b = z.B;
+  Bf16Product z = logits_product(a, l, true, w, st);
+  const Bf16Planes table = z.B;
   for (int64_t p = 0; p < l.pieces; ++p) {
     const int64_t v0 = p * l.piece, cols = a.V - v0 < l.piece ? a.V - v0 : l.piece;
     // g of the piece
-    z.B = {logits_b.p + v0 * logits_b.ld, cols, logits_b.ld, logits_b.plane};
+    z.B = {table.p + v0 * table.ld, cols, table.ld, table.plane};
     place(z, a.T, cols, l.z.big);
-    const GradArgs ga{a.targets, a.i64, a.T, a.V, v0, cols, a.scale, a.smoothing, dloss, lse,
-                      half(l.g), l.piece, a.T * l.piece, half(l.gt), l.T8, l.piece * l.T8, l.g_rows, l.g_cols};
+    const GradArgs ga{a.targets, a.i64, a.T, a.V, v0, cols, a.scale, a.smoothing, dloss, lse, half(l.g), l.piece, a.T * l.piece, l.g_terms()};
     if (l.z.big) grad_tiles<BigTile>(z, ga, st);
     else grad_tiles<SmallTile>(z, ga, st);
+    const Bf16Planes grad{half(l.g), a.T, l.piece, a.T * l.piece};
     // dx += g W
-    const size_t elem = a.t_bf16 ? 2 : 4;
-    pack_cols({static_cast<const uint8_t*>(a.table) + (size_t)v0 * a.D * elem, cols, a.D, nullptr, 0, 0, half(l.t_cols), up8(cols),
-               a.D * up8(cols)},
-              a.t_bf16, l.tx, st);
     Bf16Product x;
-    x.A = {half(l.g), a.T, l.piece, a.T * l.piece};
-    x.B = {half(l.t_cols), a.D, up8(cols), a.D * up8(cols)};
-    x.pairs = pairs_of(l.g_rows, l.tx);
+    x.A = grad;
+    x.B = z.B;
+    x.pairs = pairs_of(l.g_x, l.tx);
     x.K = up8(cols);
     OutArgs ox{a.T, a.D, l.sums_x ? reinterpret_cast<float*>(w + l.sum_x) : nullptr, dx, a.x_bf16, p > 0, a.targets, a.i64, a.V, 0};
-    out_product(x, ox, l.by_x, st);
+    out_product<false>(x, ox, l.by_x, st);
     // dW = g^T x
     Bf16Product t;
-    t.A = {half(l.gt), cols, l.T8, l.piece * l.T8};
-    t.B = {half(l.x_cols), a.D, l.T8, a.D * l.T8};
-    t.pairs = pairs_of(l.g_cols, l.xt);
-    t.K = l.T8;
+    t.A = grad;
+    t.B = z.A;
+    t.pairs = pairs_of(l.g_w, l.xt);
+    t.K = a.T;
     uint8_t* const rows = static_cast<uint8_t*>(dtable) + (size_t)v0 * a.D * (g_bf16 ? 2 : 4);
     OutArgs ow{cols, a.D, nullptr, rows, g_bf16, accumulate, nullptr, 0, 0, 0};
     if (l.by_w.splits > 1) {
       OutArgs sums = ow;
       sums.part = reinterpret_cast<float*>(w + l.sum_w);
       sums.add = 0;
-      out_product(t, sums, l.by_w, st);
+      out_product<true>(t, sums, l.by_w, st);
       out_join(ow, sums.part, l.by_w.splits, st);
     } else {
-      out_product(t, ow, l.by_w, st);
+      out_product<true>(t, ow, l.by_w, st);
     }
   }
   if (l.sums_x) {
