@@ -172,7 +172,6 @@ struct Bf16Tile {
     for (int i = 0; i < T; ++i) f[i] = *reinterpret_cast<const v8bf*>(row + i * 32 * kRowBytes + at);
   }
   static __device__ __forceinline__ v8bf join(v4h a, v4h b) {
-    typedef short v8h __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(v8bf, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 

@@ -93,6 +93,8 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackArgs a) {
 // 128 x 128 (1100; two a CU) where there are few tiles.
 using BigTile = Bf16Tile<2, 4, 4, 2, 64, 2>;
 using SmallTile = Bf16Tile<2, 2, 2, 2, 64, 2>;
+// A few rows: bound by the read of the table, six stages of which are under way (two workgroups a CU).
+using ThinTile = Bf16Tile<1, 2, 1, 1, 64, 6>;
 
 // Where a lane's sums lie: row `row(i)` of the matrix, columns col(j, q) .. + 3 in registers 4q .. 4q + 3.
 template <typename Tile>
@@ -193,14 +195,42 @@ __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g
 // (hipcc leaves the host's side of the tiles' kernels out unless asked for)
 template __global__ void loss_tile_kernel<BigTile>(Bf16Product, LossArgs);
 template __global__ void loss_tile_kernel<SmallTile>(Bf16Product, LossArgs);
+template __global__ void loss_tile_kernel<ThinTile>(Bf16Product, LossArgs);
+
+// Parts of a row joined, one after the other.
+struct RowSum {
+  float top = -3.0e38f, sum = 0.0f, all = 0.0f;
+  __device__ __forceinline__ void add(float m, float s, float z) {
+    const float next = fmaxf(top, m);
+    sum = sum * __builtin_amdgcn_exp2f(top - next) + s * __builtin_amdgcn_exp2f(m - next);
+    top = next;
+    all += z;
+  }
+};
+
+// The outputs of a row from its sums.
+struct LossOut {
+  float smoothing;
+  float* loss;
+  float* lse;
+  __device__ __forceinline__ void put(const LossArgs& a, int64_t row, const RowSum& r) const {
+    const int64_t y = target_of(a.targets, a.i64, row);
+    const bool kept = y >= 0 && y < a.V;
+    const float l = r.top * kLn2 + logf(r.sum);
+    lse[row] = kept ? l : 0.0f;
+    loss[row] = y < 0              ? 0.0f
+                : !kept            ? __builtin_nanf("")
+                : smoothing > 0.0f ? l - (1.0f - smoothing) * a.at_target[row] - smoothing / (float)a.V * r.all
+                                   : l - a.at_target[row];
+  }
+};
 
 // The rows' parts joined: 64 rows a workgroup, its 16 waves every 16th part.
-__global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t parts, float smoothing, float* __restrict__ loss,
-                                                         float* __restrict__ lse) {
+__global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t parts, LossOut out) {
   __shared__ float red[3][16][kWave];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = (int64_t)blockIdx.x * kWave + lane;
-  float top = -3.0e38f, sum = 0.0f, all = 0.0f;
+  RowSum r;
   if (row < a.T) {
     constexpr int U = 4;
     for (int64_t p = wave; p < parts; p += 16 * U) {
@@ -214,35 +244,46 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t par
         z[u] = q < parts ? src[2 * a.T] : 0.0f;
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float next = fmaxf(top, m[u]);
-        sum = sum * __builtin_amdgcn_exp2f(top - next) + s[u] * __builtin_amdgcn_exp2f(m[u] - next);
-        top = next;
-        all += z[u];
-      }
+      for (int u = 0; u < U; ++u) r.add(m[u], s[u], z[u]);
     }
   }
-  red[0][wave][lane] = top;
-  red[1][wave][lane] = sum;
-  red[2][wave][lane] = all;
+  red[0][wave][lane] = r.top;
+  red[1][wave][lane] = r.sum;
+  red[2][wave][lane] = r.all;
   __syncthreads();
   if (wave != 0 || row >= a.T) return;
-  float most = top;
-  for (int w = 1; w < 16; ++w) most = fmaxf(most, red[0][w][lane]);
-  sum = all = 0.0f;
-  for (int w = 0; w < 16; ++w) {
-    sum += red[1][w][lane] * __builtin_amdgcn_exp2f(red[0][w][lane] - most);
-    all += red[2][w][lane];
-  }
-  const int64_t y = target_of(a.targets, a.i64, row);
-  const bool kept = y >= 0 && y < a.V;
-  const float l = most * kLn2 + logf(sum);
-  lse[row] = kept ? l : 0.0f;
-  loss[row] = y < 0     ? 0.0f
-              : !kept   ? __builtin_nanf("")
-              : smoothing > 0.0f ? l - (1.0f - smoothing) * a.at_target[row] - smoothing / (float)a.V * all
-                                 : l - a.at_target[row];
+  RowSum all;
+  for (int w = 0; w < 16; ++w) all.add(red[0][w][lane], red[1][w][lane], red[2][w][lane]);
+  out.put(a, row, all);
 }
+
+// The same for few rows: a workgroup a row (4 rows of 1000 parts: 3 us, 9 with 64 rows a workgroup).
+__global__ __launch_bounds__(1024) void loss_join_few_kernel(LossArgs a, int64_t parts, LossOut out) {
+  __shared__ float red[3][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = blockIdx.x;
+  RowSum r;
+  for (int64_t p = threadIdx.x; p < parts; p += 1024) {
+    const float* const src = a.part + p * 3 * a.T + row;
+    r.add(src[0], src[a.T], src[2 * a.T]);
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) {
+    const float m = __shfl_xor(r.top, d, kWave), s = __shfl_xor(r.sum, d, kWave), z = __shfl_xor(r.all, d, kWave);
+    r.add(m, s, z);
+  }
+  if (lane == 0) {
+    red[0][wave] = r.top;
+    red[1][wave] = r.sum;
+    red[2][wave] = r.all;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  RowSum all;
+  for (int w = 0; w < 16; ++w) all.add(red[0][w], red[1][w], red[2][w]);
+  out.put(a, row, all);
+}
+constexpr int64_t kFewRows = 128;
 
 // ---- backward
 
@@ -361,6 +402,7 @@ __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g
 
 template __global__ void grad_tile_kernel<BigTile>(Bf16Product, GradArgs);
 template __global__ void grad_tile_kernel<SmallTile>(Bf16Product, GradArgs);
+template __global__ void grad_tile_kernel<ThinTile>(Bf16Product, GradArgs);
 
 // Where a product's sums go: partial sums (fp32, one matrix a split, added to when `add`), or an
 // output of type fp32 or bf16, added to when `add`; `before` (fp32) is added too.
@@ -369,6 +411,7 @@ struct OutArgs {
   float* part;
   void* out;
   int bf16, add;
+  const float* before;   // what earlier pieces left, added to the sums, or NULL
   const void* targets;   // rows whose target is not in [0, vocab) become 0, or NULL
   int i64;
   int64_t vocab;
@@ -424,6 +467,12 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
       if (row >= a.M || col >= a.N) continue;
       float v[8];
       slab.row8(r, c, v);
+      if (a.before) {
+        float old[8];
+        load_row<8>(a.before + row * a.N + col, a.N - col, old);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += old[k];
+      }
       if (a.part) {
         float* const p = a.part + ((int64_t)blockIdx.y * a.M + row) * a.N + col;
         if (a.add) {
@@ -488,12 +537,13 @@ PlanePairs pairs_of(int na, int nb) {
 // A product's tile and the splits of its reduction, by predicted time: a CU's one large tile takes
 // 1.65 us a stage of 64 k, its two small ones 1.0 (0.6 alone), and beginning and end 4 us; the splits'
 // sums are written and read again.
+enum class Edge { kThin, kSmall, kBig };
 struct Choice {
-  bool big;
+  Edge edge;
   int splits;
 };
 Choice choose(int64_t M, int64_t N, int64_t stages, int most_splits) {
-  Choice best{false, 1};
+  Choice best{Edge::kSmall, 1};
   double least = 1e300;
   for (int big = 0; big < 2; ++big) {
     const int64_t edge = big ? 256 : 128, tiles = ceil_div(M, edge) * ceil_div(N, edge);
@@ -504,15 +554,26 @@ Choice choose(int64_t M, int64_t N, int64_t stages, int most_splits) {
       if (s > 1) t += 3.0 + (double)s * M * N * 8.0 / 4.5e6;
       if (t < least) {
         least = t;
-        best = {big != 0, s};
+        best = {big ? Edge::kBig : Edge::kSmall, s};
       }
     }
   }
   return best;
 }
 
-int64_t edge_of(bool big) { return big ? BigTile::BM : SmallTile::BM; }
-static_assert(BigTile::BM == BigTile::BN && SmallTile::BM == SmallTile::BN && BigTile::BK == SmallTile::BK, "square tiles");
+// The logits' tile: up to kThinRows rows are bound by the table's read (@@).
+constexpr int64_t kThinRows = 64;
+Choice choose_logits(int64_t T, int64_t V, int64_t stages) {
+  if (T <= kThinRows) return {Edge::kThin, 1};
+  return choose(T, V, stages, 1);
+}
+
+// Calls f with the tile.
+template <typename F>
+auto with_tile(Edge edge, F f) {
+  return edge == Edge::kBig ? f(BigTile{}) : edge == Edge::kSmall ? f(SmallTile{}) : f(ThinTile{});
+}
+static_assert(BigTile::BK == SmallTile::BK && BigTile::BK == ThinTile::BK, "one stage");
 constexpr int kStage = BigTile::BK;
 
 struct Carver {
@@ -553,8 +614,8 @@ struct Layout {
     t_rows = c.take(pack_t ? (size_t)tn * V * D8 * 2 : 0);
   }
   void forward() {
-    z = choose(T, V, logits_stages(), 1);
-    parts = ceil_div(V, edge_of(z.big)) * (z.big ? BigTile::WN : SmallTile::WN);
+    z = choose_logits(T, V, logits_stages());
+    parts = with_tile(z.edge, [&](auto tile) { return ceil_div(V, decltype(tile)::BN) * decltype(tile)::WN; });
     part = c.take((size_t)parts * 3 * T * sizeof(float));
     at_target = c.take((size_t)T * sizeof(float));
     bytes = c.at;
@@ -574,7 +635,7 @@ struct Layout {
     g_w = g_bf16 ? 1 : x_bf16 ? 2 : 3;
     xt = g_bf16 && xn > 2 ? 2 : xn;
     const int64_t rows = piece < V ? piece : V;
-    z = choose(T, rows, logits_stages(), 1);
+    z = choose_logits(T, rows, logits_stages());
     by_x = choose(T, D, pairs_of(g_x, tx).count * ceil_div(up8(rows), kStage), 64);
     by_w = choose(rows, D, pairs_of(g_w, xt).count * ceil_div(T, kStage), 64);
     g = c.take((size_t)g_terms() * T * piece * 2);
@@ -619,9 +680,11 @@ Bf16Product logits_product(const CrossEntropyArgs& a, const Layout& l, bool back
   return g;
 }
 
-void place(Bf16Product& g, int64_t M, int64_t N, bool big) {
-  g.tiles_m = (int)ceil_div(M, edge_of(big));
-  g.tiles_n = (int)ceil_div(N, edge_of(big));
+void place(Bf16Product& g, int64_t M, int64_t N, Edge edge) {
+  with_tile(edge, [&](auto tile) {
+    g.tiles_m = (int)ceil_div(M, decltype(tile)::BM);
+    g.tiles_n = (int)ceil_div(N, decltype(tile)::BN);
+  });
 }
 
 template <typename Tile>
@@ -639,10 +702,10 @@ void out_tiles(const Bf16Product& g, const OutArgs& a, int splits, hipStream_t s
 
 template <bool CA>
 void out_product(Bf16Product g, OutArgs o, Choice c, hipStream_t st) {
-  place(g, o.M, o.N, c.big);
+  place(g, o.M, o.N, c.edge);
   const int stages = g.pairs.count * (int)ceil_div(g.K, kStage);
   o.chunk = (int)ceil_div(stages, c.splits);
-  if (c.big) out_tiles<BigTile, CA>(g, o, c.splits, st);
+  if (c.edge == Edge::kBig) out_tiles<BigTile, CA>(g, o, c.splits, st);
   else out_tiles<SmallTile, CA>(g, o, c.splits, st);
 }
 
@@ -676,12 +739,15 @@ hipError_t launch_cross_entropy_fwd(const CrossEntropyArgs& a, float* loss, floa
   l.forward();
   uint8_t* const w = static_cast<uint8_t*>(ws);
   Bf16Product g = logits_product(a, l, false, w, st);
-  place(g, a.T, a.V, l.z.big);
+  place(g, a.T, a.V, l.z.edge);
   const LossArgs la{a.targets, a.i64, a.T, a.V, a.scale, a.smoothing > 0.0f, reinterpret_cast<float*>(w + l.part),
                     reinterpret_cast<float*>(w + l.at_target)};
-  if (l.z.big) loss_tiles<BigTile>(g, la, st);
-  else loss_tiles<SmallTile>(g, la, st);
-  hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)ceil_div(a.T, 64)), dim3(1024), 0, st, la, l.parts, a.smoothing, loss, lse);
+  if (l.z.edge == Edge::kBig) loss_tiles<BigTile>(g, la, st);
+  else if (l.z.edge == Edge::kSmall) loss_tiles<SmallTile>(g, la, st);
+  else loss_tiles<ThinTile>(g, la, st);
+  const LossOut out{a.smoothing, loss, lse};
+  if (a.T <= kFewRows) hipLaunchKernelGGL(loss_join_few_kernel, dim3((unsigned)a.T), dim3(1024), 0, st, la, l.parts, out);
+  else hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)ceil_div(a.T, 64)), dim3(1024), 0, st, la, l.parts, out);
   return hipGetLastError();
 }
 
@@ -707,10 +773,11 @@ hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dlos
     const int64_t v0 = p * l.piece, cols = a.V - v0 < l.piece ? a.V - v0 : l.piece;
     // g of the piece
     z.B = {table.p + v0 * table.ld, cols, table.ld, table.plane};
-    place(z, a.T, cols, l.z.big);
+    place(z, a.T, cols, l.z.edge);
     const GradArgs ga{a.targets, a.i64, a.T, a.V, v0, cols, a.scale, a.smoothing, dloss, lse, half(l.g), l.piece, a.T * l.piece, l.g_terms()};
-    if (l.z.big) grad_tiles<BigTile>(z, ga, st);
-    else grad_tiles<SmallTile>(z, ga, st);
+    if (l.z.edge == Edge::kBig) grad_tiles<BigTile>(z, ga, st);
+    else if (l.z.edge == Edge::kSmall) grad_tiles<SmallTile>(z, ga, st);
+    else grad_tiles<ThinTile>(z, ga, st);
     const Bf16Planes grad{half(l.g), a.T, l.piece, a.T * l.piece};
     // dx += g W
     Bf16Product x;
@@ -718,7 +785,9 @@ hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dlos
     x.B = z.B;
     x.pairs = pairs_of(l.g_x, l.tx);
     x.K = up8(cols);
-    OutArgs ox{a.T, a.D, l.sums_x ? reinterpret_cast<float*>(w + l.sum_x) : nullptr, dx, a.x_bf16, p > 0, a.targets, a.i64, a.V, 0};
+    float* const sums = l.sums_x ? reinterpret_cast<float*>(w + l.sum_x) : nullptr;
+    const bool last = p + 1 == l.pieces && l.by_x.splits == 1;   // writes dx itself
+    OutArgs ox{a.T, a.D, last ? nullptr : sums, dx, a.x_bf16, last ? 0 : p > 0, last ? sums : nullptr, a.targets, a.i64, a.V, 0};
     out_product<false>(x, ox, l.by_x, st);
     // dW = g^T x
     Bf16Product t;
@@ -727,19 +796,19 @@ hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dlos
     t.pairs = pairs_of(l.g_w, l.xt);
     t.K = a.T;
     uint8_t* const rows = static_cast<uint8_t*>(dtable) + (size_t)v0 * a.D * (g_bf16 ? 2 : 4);
-    OutArgs ow{cols, a.D, nullptr, rows, g_bf16, accumulate, nullptr, 0, 0, 0};
+    OutArgs ow{cols, a.D, nullptr, rows, g_bf16, accumulate, nullptr, nullptr, 0, 0, 0};
     if (l.by_w.splits > 1) {
-      OutArgs sums = ow;
-      sums.part = reinterpret_cast<float*>(w + l.sum_w);
-      sums.add = 0;
-      out_product<true>(t, sums, l.by_w, st);
-      out_join(ow, sums.part, l.by_w.splits, st);
+      OutArgs part = ow;
+      part.part = reinterpret_cast<float*>(w + l.sum_w);
+      part.add = 0;
+      out_product<true>(t, part, l.by_w, st);
+      out_join(ow, part.part, l.by_w.splits, st);
     } else {
       out_product<true>(t, ow, l.by_w, st);
     }
   }
-  if (l.sums_x) {
-    const OutArgs ox{a.T, a.D, nullptr, dx, a.x_bf16, 0, a.targets, a.i64, a.V, 0};
+  if (l.by_x.splits > 1) {
+    const OutArgs ox{a.T, a.D, nullptr, dx, a.x_bf16, 0, nullptr, a.targets, a.i64, a.V, 0};
     out_join(ox, reinterpret_cast<const float*>(w + l.sum_x), l.by_x.splits, st);
   }
   return hipGetLastError();
