@@ -207,12 +207,40 @@ __device__ void route_exact(const RouteArgs& a, int64_t row, uint64_t* keys, int
   }
 }
 
-// How much two values of c in fp32 may be off, together.  A sigmoid is off by 5 u (its exponential
+// How much two values of c in fp32 may be off, together: a sigmoid is off by 5 u (its exponential
 // by (2 |l| + 2) u of itself, of which s (1 - s) remains, a sum and a reciprocal by 3 u), a softmax by
 // 60 u of itself (an exponential of d by (3 |d| + 2) u of itself, the sum's terms as much on average,
-// the additions and the division), and the addition of the bias by u |c|.  Sums of two: twice that.
-__device__ __forceinline__ float near_of(bool sigmoid, float most_score, float most_c) {
-  return (sigmoid ? 0x1p-20f : 0x1p-17f * most_score) + 0x1p-22f * most_c;
+// the additions and the division).  The addition of the bias is off by u |c| more.
+__device__ __forceinline__ float near_of(bool sigmoid, float most_score) {
+  return sigmoid ? 0x1p-20f : 0x1p-17f * most_score;
+}
+constexpr float kNearSum = 0x1p-23f;   // 2 u
+
+// The comparisons of an odd-even merge sort of N keys.
+template <int N>
+struct SortNetwork {
+  int count = 0, first[N > 1 ? N * 4 : 1] = {}, second[N > 1 ? N * 4 : 1] = {};
+  constexpr SortNetwork() {
+    for (int p = 1; p < N; p *= 2)
+      for (int d = p; d >= 1; d /= 2)
+        for (int b = d % p; b + d < N; b += 2 * d)
+          for (int i = 0; i < d; ++i)
+            if (i + b + d < N && (i + b) / (2 * p) == (i + b + d) / (2 * p)) {
+              first[count] = i + b;
+              second[count++] = i + b + d;
+            }
+  }
+};
+// Descending.
+template <int N>
+__device__ __forceinline__ void sort_keys(uint32_t (&k)[N]) {
+  constexpr SortNetwork<N> net;
+#pragma unroll
+  for (int i = 0; i < net.count; ++i) {
+    const uint32_t x = k[net.first[i]], y = k[net.second[i]];
+    k[net.first[i]] = max(x, y);
+    k[net.second[i]] = min(x, y);
+  }
 }
 
 // LPR lanes a row, NE experts a lane: lane j has experts j * NE .. j * NE + NE - 1.  SUM: c is a sum.
@@ -221,15 +249,18 @@ template <int LPR>
 __host__ __device__ constexpr int route_wave_bytes(int E) {
   return (kWave / LPR > 2 ? kWave / LPR * 4 : 8) * E;
 }
-template <typename T, int LPR, int NE, bool SUM>
+// ONE: fewer choices than lanes.
+template <typename T, int LPR, int NE, bool SUM, bool ONE>
 __global__ __launch_bounds__(kRouteWaves * kWave) void route_fwd_kernel(RouteArgs a, int32_t* __restrict__ chosen,
                                                                         float* __restrict__ weights) {
-  constexpr int kRows = kWave / LPR, kList = LPR * NE < kMaxTop ? LPR * NE : kMaxTop, kMine = (kList + LPR - 1) / LPR;
+  constexpr int kRows = kWave / LPR, kList = LPR * NE < kMaxTop ? LPR * NE : kMaxTop, kMine = ONE ? 1 : (kList + LPR - 1) / LPR;
   // the place that a key holds: of sixteen free bits the one in the row (equal keys are then in the
   // order of their places), else the one in the lane
   constexpr bool kPacked = SUM || sizeof(T) == 2, kInRow = !SUM && sizeof(T) == 2;
   constexpr uint32_t kPlace = kInRow ? LPR * NE - 1 : kPacked ? NE - 1 : 0;
   static_assert((NE & (NE - 1)) == 0 && LPR * NE <= 65536, "a place in the lowest bits");
+  // a lane's keys in order, the largest first: taking one out moves the others up
+  constexpr bool kSorted = kPacked && NE <= 16;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds_keys[];
   __shared__ int lists[SUM ? kRouteWaves : 1][kMaxTop];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & (LPR - 1);
@@ -262,27 +293,36 @@ __global__ __launch_bounds__(kRouteWaves * kWave) void route_fwd_kernel(RouteArg
   float tolerance = 0.0f;
   auto pack_place = [&](uint32_t k, int i) { return kPacked ? (k & ~kPlace) | (kPlace - (kInRow ? e0 + i : i)) : k; };
   if constexpr (SUM) {
-    float s[NE], total = 0.0f, big = 0.0f;
+    float s[NE], b[NE], share = 1.0f;
+    if (a.sigmoid) {
 #pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      if (a.sigmoid) {
-        s[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l[i] * kLog2e));
-      } else {
+      for (int i = 0; i < NE; ++i) s[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l[i] * kLog2e));
+    } else {
+      float total = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
         s[i] = l[i] > -__builtin_inff() ? __builtin_amdgcn_exp2f((l[i] - top) * kLog2e) : 0.0f;
         total += s[i];
       }
+      share = 1.0f / row_total<LPR>(total);
     }
-    float share = 1.0f;
-    if (!a.sigmoid) share = 1.0f / row_total<LPR>(total);
+    if (a.bias && left >= NE) {
+      RowPack<float, NE> pack;
+      pack.load(a.bias + e0);
+#pragma unroll
+      for (int i = 0; i < NE; ++i) b[i] = pack.get(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NE; ++i) b[i] = a.bias && i < left ? a.bias[e0 + i] : 0.0f;
+    }
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
-      const float c = fmaf(s[i], share, a.bias && i < left ? a.bias[e0 + i] : 0.0f);
-      const bool barred = !(l[i] > -__builtin_inff()) || c == -__builtin_inff();
-      good &= barred || sound(c);
-      key[i] = barred ? 0 : pack_place(key_of(c), i);
-      if (!barred) big = fmaxf(big, fabsf(c));
+      const float sum = fmaf(s[i], share, b[i]);
+      const float c = l[i] > -__builtin_inff() ? sum : -__builtin_inff();
+      good &= sound(c);
+      key[i] = c > -__builtin_inff() ? pack_place(key_of(c), i) : 0;
     }
-    tolerance = near_of(a.sigmoid, share, row_max<LPR>(big));
+    tolerance = near_of(a.sigmoid, share);
   } else {
 #pragma unroll
     for (int i = 0; i < NE; ++i) key[i] = l[i] > -__builtin_inff() ? pack_place(key_of(l[i]), i) : 0;
@@ -291,122 +331,147 @@ __global__ __launch_bounds__(kRouteWaves * kWave) void route_fwd_kernel(RouteArg
   // of a key with a place, the least and the largest value that it may stand for
   auto least = [&](uint32_t k) { return value_of(k & ~kPlace); };
   auto largest = [&](uint32_t k) { return value_of(k | kPlace); };
-  if (a.groups > 1) {
-    // the rank of this lane's group: of whole lanes, a power of two of them, in registers; else
-    // lane g of the row reads group g.  Ranks are values without places.
-    const int size = a.E / a.groups, lanes = size / NE;
-    auto rank_of = [&](uint32_t first, uint32_t second) {
-      if constexpr (SUM) {
-        if (a.best == 2 && second) return key_of(least(first) + least(second));
-      }
-      return first & ~kPlace;
-    };
-    // how far a rank in fp32 may be off: both places, and both sums
-    const float rank_tolerance = SUM ? 2.0f * tolerance : 0.0f;
-    if (size % NE == 0 && (lanes & (lanes - 1)) == 0) {
+  // the rank of this lane's group: of whole lanes, a power of two of them, in registers; else lane g
+  // of the row reads group g.  Ranks are values without places; each has the error of its sums.
+  const int size = a.groups > 1 ? a.E / a.groups : 0, lanes = size / NE;
+  const bool grouped = a.groups > 1, whole = size % NE == 0 && (lanes & (lanes - 1)) == 0;
+  auto rank_of = [&](uint32_t first, uint32_t second) {
+    if constexpr (SUM) {
+      if (a.best == 2 && second) return key_of(least(first) + least(second));
+    }
+    return first & ~kPlace;
+  };
+  // the least that a rank may stand for, and the largest
+  auto rank_error = [&](uint32_t first, uint32_t second) {
+    return kNearSum * (fabsf(least(first)) + (a.best == 2 && second ? 2.0f * fabsf(least(second)) : 0.0f));
+  };
+  auto rank_least = [&](uint32_t rank, uint32_t first, uint32_t second) {
+    return rank ? value_of(rank) - rank_error(first, second) : __builtin_inff();
+  };
+  auto rank_largest = [&](uint32_t rank, uint32_t first, uint32_t second) {
+    return rank ? largest(first) + (a.best == 2 && second ? largest(second) : 0.0f) + rank_error(first, second) : -__builtin_inff();
+  };
+  if (grouped && !whole) {
+    uint32_t* const mine = reinterpret_cast<uint32_t*>(region) + lane / LPR * a.E;
+#pragma unroll
+    for (int i = 0; i < NE; ++i)
+      if (i < left) mine[e0 + i] = key[i];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // groups beyond the row's lanes: a lane takes every LPR-th
+    constexpr int kPerLane = kMaxTop / LPR;
+    uint32_t ranks[kPerLane];
+    float lows[kPerLane], highs[kPerLane];
+#pragma unroll
+    for (int q = 0; q < kPerLane; ++q) {
+      const int g = j + q * LPR;
       uint32_t first = 0, second = 0;
+      if (in && g < a.groups)
+        for (int i = 0; i < size; ++i) put_key<uint32_t>(first, second, mine[g * size + i], 0);
+      ranks[q] = rank_of(first, second);
+      lows[q] = rank_least(ranks[q], first, second);
+      highs[q] = rank_largest(ranks[q], first, second);
+    }
+    uint64_t kept = 0;
+    float low = __builtin_inff();
+    for (int n = 0; n < a.top_groups; ++n) {
+      uint32_t best = 0;
+      int at = 0;
+#pragma unroll
+      for (int q = 0; q < kPerLane; ++q)
+        if (ranks[q] > best) {
+          best = ranks[q];
+          at = q;
+        }
+      const uint32_t most = row_max<LPR>(best);
+      // the lowest group of those: by q first, then by lane
+      const uint64_t who = row_ballot<LPR>(best == most);
+      int g = 1 << 20;
+      for (uint64_t w = most ? who : 0; w; w &= w - 1) {
+        const int t = __builtin_ctzll(w);
+        g = min(g, t + LPR * __shfl(at, (lane & ~(LPR - 1)) + t, kWave));
+      }
+      if (most == 0) continue;
+      kept |= 1ull << g;
+#pragma unroll
+      for (int q = 0; q < kPerLane; ++q)
+        if (g == j + q * LPR) {
+          low = fminf(low, lows[q]);
+          ranks[q] = 0;
+          highs[q] = -__builtin_inff();
+        }
+    }
+    if constexpr (SUM) {
+      float high = highs[0];
+#pragma unroll
+      for (int q = 1; q < kPerLane; ++q) high = fmaxf(high, highs[q]);
+      high = row_max<LPR>(high);
+      near |= high > -__builtin_inff() && row_min<LPR>(low) - high <= 2.0f * tolerance;
+    }
+#pragma unroll
+    for (int i = 0; i < NE; ++i)
+      if (i < left && !(kept >> ((e0 + i) / size) & 1)) key[i] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  if constexpr (kSorted) sort_keys(key);
+  if (grouped && whole) {
+    uint32_t first = 0, second = 0;
+    if constexpr (kSorted) {
+      first = key[0];
+      second = NE > 1 ? key[NE > 1] : 0;
+    } else {
 #pragma unroll
       for (int i = 0; i < NE; ++i) put_key<uint32_t>(first, second, key[i], 0);
-#pragma unroll
-      for (int d = 1; d < LPR; d *= 2)
-        if (d < lanes) put_key<uint32_t>(first, second, __shfl_xor(first, d, kWave), __shfl_xor(second, d, kWave));
-      uint32_t rank = rank_of(first, second);
-      if (e0 >= a.E) rank = 0;
-      // groups before ours, by rank and then by place
-      const int mine = j / lanes;
-      int before = 0;
-      for (int g = 0; g < a.groups; ++g) {
-        const uint32_t r = __shfl(rank, (lane & ~(LPR - 1)) + g * lanes, kWave);
-        before += r > rank || (r == rank && g < mine);
-      }
-      const bool kept = before < a.top_groups;
-      if constexpr (SUM) {
-        const float low = row_min<LPR>(kept && rank ? value_of(rank) : __builtin_inff());
-        float high = !kept && rank ? largest(first) + (a.best == 2 && second ? largest(second) : 0.0f) : -__builtin_inff();
-        high = row_max<LPR>(high);
-        near |= high > -__builtin_inff() && low - high <= rank_tolerance;
-      }
-      if (!kept)
-#pragma unroll
-        for (int i = 0; i < NE; ++i) key[i] = 0;
-    } else {
-      uint32_t* const mine = reinterpret_cast<uint32_t*>(region) + lane / LPR * a.E;
-#pragma unroll
-      for (int i = 0; i < NE; ++i)
-        if (i < left) mine[e0 + i] = key[i];
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      // groups beyond the row's lanes: a lane takes every LPR-th
-      constexpr int kPerLane = kMaxTop / LPR;
-      uint32_t ranks[kPerLane];
-      float highs[kPerLane];
-#pragma unroll
-      for (int q = 0; q < kPerLane; ++q) {
-        const int g = j + q * LPR;
-        uint32_t first = 0, second = 0;
-        if (in && g < a.groups)
-          for (int i = 0; i < size; ++i) put_key<uint32_t>(first, second, mine[g * size + i], 0);
-        ranks[q] = rank_of(first, second);
-        highs[q] = ranks[q] ? largest(first) + (a.best == 2 && second ? largest(second) : 0.0f) : -__builtin_inff();
-      }
-      uint64_t kept = 0;
-      float low = __builtin_inff();
-      for (int n = 0; n < a.top_groups; ++n) {
-        uint32_t best = 0;
-        int at = 0;
-#pragma unroll
-        for (int q = 0; q < kPerLane; ++q)
-          if (ranks[q] > best) {
-            best = ranks[q];
-            at = q;
-          }
-        const uint32_t most = row_max<LPR>(best);
-        // the lowest group of those: by q first, then by lane
-        const uint64_t who = row_ballot<LPR>(best == most);
-        int g = 1 << 20;
-        for (uint64_t w = most ? who : 0; w; w &= w - 1) {
-          const int t = __builtin_ctzll(w);
-          g = min(g, t + LPR * __shfl(at, (lane & ~(LPR - 1)) + t, kWave));
-        }
-        if (most == 0) continue;
-        low = value_of(most);
-        kept |= 1ull << g;
-#pragma unroll
-        for (int q = 0; q < kPerLane; ++q)
-          if (g == j + q * LPR) {
-            ranks[q] = 0;
-            highs[q] = -__builtin_inff();
-          }
-      }
-      if constexpr (SUM) {
-        float high = highs[0];
-#pragma unroll
-        for (int q = 1; q < kPerLane; ++q) high = fmaxf(high, highs[q]);
-        high = row_max<LPR>(high);
-        near |= high > -__builtin_inff() && low - high <= rank_tolerance;
-      }
-#pragma unroll
-      for (int i = 0; i < NE; ++i)
-        if (i < left && !(kept >> ((e0 + i) / size) & 1)) key[i] = 0;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+#pragma unroll
+    for (int d = 1; d < LPR; d *= 2)
+      if (d < lanes) put_key<uint32_t>(first, second, __shfl_xor(first, d, kWave), __shfl_xor(second, d, kWave));
+    uint32_t rank = rank_of(first, second);
+    if (e0 >= a.E) rank = 0;
+    // groups before ours, by rank and then by place
+    const int mine = j / lanes;
+    int before = 0;
+    for (int g = 0; g < a.groups; ++g) {
+      const uint32_t r = __shfl(rank, (lane & ~(LPR - 1)) + g * lanes, kWave);
+      before += r > rank || (r == rank && g < mine);
+    }
+    const bool kept = before < a.top_groups;
+    if constexpr (SUM) {
+      const float low = row_min<LPR>(kept ? rank_least(rank, first, second) : __builtin_inff());
+      const float high = row_max<LPR>(kept ? -__builtin_inff() : rank_largest(rank, first, second));
+      near |= high > -__builtin_inff() && low - high <= 2.0f * tolerance;
+    }
+    if (!kept)
+#pragma unroll
+      for (int i = 0; i < NE; ++i) key[i] = 0;
   }
   // the choices, the k-th in lane k mod LPR; with SUM one more, for its distance
   int expert[kMine];
 #pragma unroll
   for (int q = 0; q < kMine; ++q) expert[q] = -1;
-  uint32_t last = 0;
+  // whether the values of two keys, one behind the other, cannot be told apart
+  auto too_near = [&](uint32_t k1, uint32_t k2) {
+    const float v = least(k1), w = largest(k2);
+    return v - w <= tolerance + kNearSum * (fabsf(v) + fabsf(w));
+  };
+  uint32_t last = 0, taken = 0;
   for (int k = 0; k < a.K + SUM; ++k) {
     uint32_t best = key[0];
     int at = 0;
+    if constexpr (!kSorted) {
 #pragma unroll
-    for (int i = 1; i < NE; ++i) {
-      if constexpr (!kPacked) at = key[i] > best ? i : at;
-      best = max(best, key[i]);
+      for (int i = 1; i < NE; ++i) {
+        if constexpr (!kPacked) at = key[i] > best ? i : at;
+        best = max(best, key[i]);
+      }
     }
     const uint32_t most = row_max<LPR>(best);
     if constexpr (SUM) {
-      near |= k > 0 && most && least(last) - largest(most) <= tolerance;
-      last = most;
+      if constexpr (ONE) {
+        taken = k == j ? most : taken;   // looked at afterwards, all at once
+      } else {
+        near |= k > 0 && most && too_near(last, most);
+        last = most;
+      }
       if (k == a.K) break;
     }
     int first = 0, index;
@@ -416,9 +481,17 @@ __global__ __launch_bounds__(kRouteWaves * kWave) void route_fwd_kernel(RouteArg
     }
     if constexpr (kPacked) {
       index = (int)(kPlace - (most & kPlace)) + first * NE;
-      const uint32_t out = kInRow || j == first ? most : 0;
+      const bool out = kInRow ? best == most : j == first;
+      if constexpr (kSorted) {
 #pragma unroll
-      for (int i = 0; i < NE; ++i) key[i] = key[i] == out ? 0 : key[i];
+        for (int i = 0; i < NE; ++i) {
+          const uint32_t up = i + 1 < NE ? key[i + 1 < NE ? i + 1 : i] : 0, here = key[i];   // (values: of places it makes an index)
+          key[i] = out ? up : here;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) key[i] = out && key[i] == most ? 0 : key[i];
+      }
     } else {
       index = __shfl(at, (lane & ~(LPR - 1)) + first, kWave) + first * NE;
 #pragma unroll
@@ -428,9 +501,14 @@ __global__ __launch_bounds__(kRouteWaves * kWave) void route_fwd_kernel(RouteArg
     for (int q = 0; q < kMine; ++q)
       if (k == j + q * LPR && most) expert[q] = index;
   }
+  if constexpr (SUM && ONE) {
+    const uint32_t behind = __shfl_down(taken, 1, kWave);
+    near |= j < a.K && behind && too_near(taken, behind);
+  }
   if constexpr (SUM) {
     // rows where two values are too near to tell, one after the other by the whole wave
-    uint64_t again = __ballot(in && !bad && near && j == 0);
+    const bool row_near = row_ballot<LPR>(near) != 0;
+    uint64_t again = __ballot(in && !bad && row_near && j == 0);
     while (again) {
       const int r = __builtin_ctzll(again) / LPR;
       again &= again - 1;
@@ -612,8 +690,14 @@ hipError_t launch_route_fwd(const RouteArgs& a, int bf16, int32_t* chosen, float
     auto launch = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)((a.T + rows - 1) / rows)), dim3(waves * kWave), lds, st, a, chosen, weights);
     };
-    if (bf16) sum ? launch(route_fwd_kernel<uint16_t, LPR, NE, true>) : launch(route_fwd_kernel<uint16_t, LPR, NE, false>);
-    else sum ? launch(route_fwd_kernel<float, LPR, NE, true>) : launch(route_fwd_kernel<float, LPR, NE, false>);
+    auto typed = [&](auto elem, auto one) {
+      using T = decltype(elem);
+      constexpr bool ONE = decltype(one)::value;
+      sum ? launch(route_fwd_kernel<T, LPR, NE, true, ONE>) : launch(route_fwd_kernel<T, LPR, NE, false, ONE>);
+    };
+    auto counted = [&](auto one) { bf16 ? typed(uint16_t{}, one) : typed(float{}, one); };
+    if (a.K < LPR) counted(std::true_type{});
+    else counted(std::false_type{});
   };
   using std::integral_constant;
   const bool many = a.T >= kManyRows;
