@@ -14,6 +14,8 @@
 // code is the top of a float whose smallest normal number is e4m3's, and roots and quotients are the
 // hardware's, off by one unit of the last place or two.  They are rounded stochastically: of a step to the next code of 2^-4 to 2^-3 a v with
 // b2 = 0.999 changes 10^-3 at most, which rounding to nearest would lose every time.
+#include <math.h>
+
 #include "luq_launch.hpp"
 #include "row_ops.hpp"
 
@@ -31,7 +33,7 @@ struct AdamwArgs {
   const int64_t* step;
   const float* grad_scale;
   int64_t count;
-  double beta1, beta2;
+  double beta1, beta2, log_beta1, log_beta2;   // the logarithms to base 2
   float eps;
   uint32_t seed_lo, seed_hi;
 };
@@ -283,9 +285,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwArgs a) {
   c.c1 = (float)(1.0 - a.beta1);
   c.b2 = (float)a.beta2;
   c.c2 = (float)(1.0 - a.beta2);
-  c.root = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)t)));
+  c.root = (float)(1.0 / sqrt(1.0 - exp2((double)t * a.log_beta2)));
   c.eps = a.eps;
-  const double bias = 1.0 - pow(a.beta1, (double)t);
+  const double bias = 1.0 - exp2((double)t * a.log_beta1);
   for (int64_t at = blockIdx.x;;) {
     const int64_t next = at + gridDim.x;
     AdamwChunk next_ch = ch;
@@ -309,7 +311,7 @@ hipError_t launch_adamw(const void* plan, int64_t count, int64_t chunks, const f
                         double beta1, double beta2, float eps, const float* grad_scale, uint64_t seed, hipStream_t st) {
   const AdamwEntry* const entries = static_cast<const AdamwEntry*>(plan);
   const AdamwArgs a{entries, reinterpret_cast<const AdamwChunk*>(entries + count), lr, step, grad_scale, chunks, beta1, beta2,
-                    eps, (uint32_t)seed, (uint32_t)(seed >> 32)};
+                    log2(beta1), log2(beta2), eps, (uint32_t)seed, (uint32_t)(seed >> 32)};
   // a workgroup takes several chunks of many: what they have in common (two powers in 64 bits) is a
   // third of the instructions of one
   const int64_t most = kGroupsPerCu * 256;
