@@ -211,3 +211,38 @@ def test_views_and_streams(L):
         back = L.luq_cross_entropy_bwd(dloss, x, w, y, got[1])
     side.synchronize()
     assert all(torch.equal(p, q) for p, q in zip((*got, *back), (*want, *grads)))
+
+
+@pytest.mark.parametrize("T,V,D,xt,tt,gt", [(1500, 9100, 72, "bf16", "bf16", "bf16"), (2100, 4300, 1032, "bf16", "bf16", "f32"),
+                                            (1111, 6007, 333, "f32", "f32", "f32"), (4100, 2050, 1033, "bf16", "f32", "f32")])
+def test_large_tiles(L, T, V, D, xt, tt, gt):
+    """Sizes that take the 256 x 256 tiles in every product, with edges in both directions (the references on the GPU, in
+    64 bits)."""
+    x, w, y, dloss = _inputs(T, V, D, xt, tt)
+    announce("cross entropy, large tiles", T, V, D, xt, tt)
+    loss, lse = L.luq_cross_entropy_fwd(x, w, y, 1.0, 0.1)
+    x64, w64, ok = x.double(), w.double(), y >= 0
+    z = x64 @ w64.t()
+    want = torch.logsumexp(z, 1)
+    row, at = torch.arange(T, device="cuda"), y.clamp(min=0)
+    ref = want - 0.9 * z[row, at] - 0.1 * z.mean(1)
+    # additions in a row of a logit, of like magnitude as its largest terms' sum
+    nx, nw = (1 if xt == "bf16" else 3), (1 if tt == "bf16" else 3)
+    ez = (x64.abs() @ w64.abs().t()).amax(1) * (S._chain(S._pairs(nx, nw), D) * 2 + 8) * 2.0 ** -24
+    e = 3 * ez + (200 + V / 128) * 2.0 ** -24 * (1 + want.abs())
+    assert ((lse - want).abs()[ok] <= e[ok]).all() and ((loss - ref).abs()[ok] <= 2 * e[ok]).all() and (loss[~ok] == 0).all()
+    dx, dw = L.luq_cross_entropy_bwd(dloss, x, w, y, lse, 1.0, 0.1, dtable=torch.empty(V, D, dtype=DT[gt], device="cuda"))
+    g = torch.exp(z - lse.double()[:, None])
+    g -= 0.1 / V
+    g[row, at] -= 0.9
+    g *= (dloss.double() * ok)[:, None]
+    # every g by its logit's error and its roundings to terms
+    rel = (ez + 60 * 2.0 ** -24).amax()
+    rows, cols = (1 if xt == "bf16" else 3), (1 if gt == "bf16" else 2 if xt == "bf16" else 3)
+    for got, a, c, terms, k, bf16 in ((dx, g, w64, rows, V, xt == "bf16"), (dw, g.t(), x64 * ok[:, None], cols, T, gt == "bf16")):
+        tw = (2 if xt == "bf16" and nw == 3 else nw) if got is dx else (2 if gt == "bf16" and nx == 3 else nx)
+        tol = rel + 2.0 ** (-8 * terms) + 2.0 ** (-8 * (tw if (nw if got is dx else nx) > 1 else 9)) + S._chain(S._pairs(terms, tw), k) * 2.0 ** -23
+        mag = (a.abs() + 0.1 / V) @ c.abs()   # a g near 0 is off by its parts' errors
+        ref = a @ c
+        bound = tol * mag + (2.0 ** -8 * ref.abs() * (1 + tol) + 2.0 ** -8 * tol * mag if bf16 else 0)
+        assert ((got.double() - ref).abs() <= bound + 1e-30).all(), (got is dx, ((got.double() - ref).abs() / bound).max())
