@@ -314,8 +314,9 @@ size_t luq_adamw_plan_bytes(const int64_t* n, int64_t count);
 
 /*
  * luq_adamw_plan -- the work of a step, laid out once for tensors that keep their places.
- * `tensors` and `plan` are HOST memory; the caller copies the plan to the device.  Tensors
- * do not overlap; each is aligned to its elements.
+ * `tensors` and `plan` are HOST memory; the caller copies the plan to the device.  None that
+ * a step writes overlaps another (LUQ_ERR_PARAM; gradients may be shared); each is aligned to
+ * its elements.
  * Errors: LUQ_ERR_NULL, LUQ_ERR_SHAPE, LUQ_ERR_DTYPE, LUQ_ERR_PARAM, LUQ_ERR_ALIGN,
  * LUQ_ERR_WORKSPACE (plan_bytes is not luq_adamw_plan_bytes).
  */

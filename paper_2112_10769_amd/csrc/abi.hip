@@ -1,6 +1,10 @@
 // extern "C" entry points of libluq: argument validation on the host, then
 // launches on the caller's stream.  Nothing is enqueued when validation
 // fails.  See include/luq.h for the contract of every function.
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include <stdint.h>
 #include <stdio.h>
 #include <string.h>
@@ -751,7 +755,7 @@ luq_status luq_cross_entropy_bwd(const float* dloss, const void* x, luq_dtype xt
   if (!dtable || (T > 0 && (!dloss || !x || !table || !targets || !lse || !dx))) return fail(LUQ_ERR_NULL, "%s: NULL pointer", fn);
   if (!aligned16(x) || !aligned16(table)) return fail(LUQ_ERR_ALIGN, "%s: x and table must be 16-byte aligned", fn);
   if (!aligned_to(targets, it == LUQ_I64 ? 8 : 4) || !aligned4(dloss) || !aligned4(lse) || !aligned_to(dx, elem_size(xt)) ||
-      !aligned_to(dtable, T > 0 ? elem_size(gt) : 4))
+      !aligned_to(dtable, elem_size(gt)))
     return fail(LUQ_ERR_ALIGN, "%s: a tensor is misaligned", fn);
   st = check_workspace(fn, luq_cross_entropy_workspace(T, V, D, xt, tt, gt), ws, ws_bytes);
   if (st != LUQ_OK) return st;
@@ -785,6 +789,44 @@ size_t luq_adamw_plan_bytes(const int64_t* n, int64_t count) {
   return adamw_bytes(count, adamw_chunks(n, count, sizeof(int64_t)));
 }
 
+// Whether a tensor that a step writes overlaps another one of the plan: 1, or -1 without the memory to tell.
+static int adamw_overlap(const luq_adamw_tensor* tensors, int64_t count) {
+  struct Range {
+    uintptr_t begin, end;
+    bool written;
+  };
+  const std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[7 * (size_t)count]);
+  if (!ranges) return -1;
+  size_t used = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    const luq_adamw_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    auto add = [&](const void* p, int64_t bytes, bool written) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+      if (p) ranges[used++] = {at, at + (uintptr_t)bytes, written};
+    };
+    const int64_t state = t.state_bits == 8 ? 1 : 4, blocks = (t.n + 31) / 32;
+    add(t.p, 4 * t.n, true);
+    add(t.g, (t.gt == LUQ_F32 ? 4 : 2) * t.n, false);
+    add(t.m, state * t.n, true);
+    add(t.v, state * t.n, true);
+    add(t.copy, 2 * t.n, true);
+    if (state == 1) {
+      add(t.m_scale, blocks, true);
+      add(t.v_scale, blocks, true);
+    }
+  }
+  std::sort(ranges.get(), ranges.get() + used, [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t written = 0, any = 0;   // the furthest ends so far
+  for (size_t i = 0; i < used; ++i) {
+    const Range& r = ranges[i];
+    if (r.begin < (r.written ? any : written)) return 1;
+    any = std::max(any, r.end);
+    if (r.written) written = std::max(written, r.end);
+  }
+  return 0;
+}
+
 luq_status luq_adamw_plan(const luq_adamw_tensor* tensors, int64_t count, void* plan, size_t plan_bytes) {
   const char* fn = "luq_adamw_plan";
   g_last_error[0] = 0;
@@ -807,6 +849,8 @@ luq_status luq_adamw_plan(const luq_adamw_tensor* tensors, int64_t count, void* 
   }
   if (plan_bytes != adamw_bytes(count, chunks)) return fail(LUQ_ERR_WORKSPACE, "%s: plan_bytes is not luq_adamw_plan_bytes", fn);
   if (chunks == 0) return LUQ_OK;
+  const int overlap = adamw_overlap(tensors, count);
+  if (overlap) return fail(LUQ_ERR_PARAM, overlap > 0 ? "%s: a tensor that is written overlaps another" : "%s: out of memory", fn);
   if (!plan) return fail(LUQ_ERR_NULL, "%s: plan is NULL", fn);
   if (!aligned_to(plan, 8)) return fail(LUQ_ERR_ALIGN, "%s: plan must be 8-byte aligned", fn);
   luq::AdamwEntry* const entries = static_cast<luq::AdamwEntry*>(plan);

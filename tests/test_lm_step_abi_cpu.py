@@ -134,11 +134,32 @@ def test_adamw_plan_arguments():
     assert LIB.luq_adamw_plan_bytes(sizes, 3) == 0 and LIB.luq_adamw_plan_bytes(sizes, 1) > 0 and LIB.luq_adamw_plan_bytes(None, 3) == 0
 
 
+def _plan_of(tensors):
+    a = (luq._AdamwTensor * len(tensors))(*tensors)
+    n = luq.luq_adamw_plan_bytes([t.n for t in tensors])
+    plan = (ctypes.c_uint64 * (n // 8 + 1))()
+    return LIB.luq_adamw_plan(ctypes.addressof(a), len(tensors), ctypes.addressof(plan), n)
+
+
+def test_adamw_plan_refuses_overlaps():
+    """100 elements of 4 bytes from the addresses on: 0x190 bytes."""
+    other = dict(p=0x11000, g=0x12000, m=0x13000, v=0x14000)
+    assert _plan_of([_tensor(), _tensor(**other)]) == 0
+    assert _plan_of([_tensor(), _tensor(**dict(other, g=0x2000))]) == 0            # a shared gradient
+    assert _plan_of([_tensor(), _tensor(**dict(other, p=0x1190))]) == 0            # side by side
+    assert _plan_of([_tensor(), _tensor(n=0)]) == 0
+    for kw in (dict(p=0x1000), dict(p=0x118C), dict(m=0x1000), dict(v=0x3000), dict(g=0x1000), dict(p=0x2000), dict(copy=0x110FE),
+               dict(m=0x14000), dict(p=0x0FFC), dict(state_bits=8, m_scale=0x15000, v_scale=0x15003)):
+        assert _plan_of([_tensor(), _tensor(**dict(other, **kw))]) == PARAM, kw
+    assert _plan_of([_tensor(), _tensor(**dict(other, state_bits=8, m_scale=0x15000, v_scale=0x15004))]) == 0
+
+
 def test_adamw_plan_covers_every_element():
     """The plan's chunks: each of 4096 elements of a tensor, once, in order."""
     sizes = [1, 0, 4096, 4097, 20000]
     n = luq.luq_adamw_plan_bytes(sizes)
-    a = (luq._AdamwTensor * 5)(*[_tensor(n=k) for k in sizes])
+    a = (luq._AdamwTensor * 5)(*[_tensor(n=k, **{name: (4 * i + j + 1) << 20 for j, name in enumerate("pgmv")})
+                                 for i, k in enumerate(sizes)])
     plan = (ctypes.c_uint8 * n)()
     assert LIB.luq_adamw_plan(ctypes.addressof(a), 5, ctypes.addressof(plan), n) == 0
     chunks = [-(-k // 4096) for k in sizes]
