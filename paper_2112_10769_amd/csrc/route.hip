@@ -15,9 +15,10 @@
 // at again anyway) they hold the expert's place, in the row or in the lane: taking an expert out is
 // then a comparison for each key, without a branch.
 //
-// Bound by instructions, not by memory (16384 rows of 256 experts in 8 groups, top 8: 23 us, their
-// 16.8 MB would take 3.4; a wave a row with the choice in 64 bits took 57, in fp32 with the place
-// beside the key 27 to 32): many rows take as few lanes as 16 experts a lane allow, few rows as many.
+// Bound by instructions, not by memory (16384 rows of 256 experts in 8 groups, top 8: 15 us, their
+// 16.8 MB would take 3.4; a wave a row with the choice in 64 bits took 57, in fp32 with the largest of a
+// lane's keys looked for at each choice 23): many rows take as few lanes as 16 experts a lane allow, few
+// rows as many.  A row chosen again is waited for: 3.5 us at the end of a call that has one.
 #include <type_traits>
 
 #include "luq_launch.hpp"
@@ -174,7 +175,8 @@ __device__ void route_exact(const RouteArgs& a, int64_t row, uint64_t* keys, int
     const int step = whole ? lanes : 1, mine = lane / step;
     int before = 0;
     for (int g = 0; g < a.groups; ++g) {
-      const uint64_t r = __shfl((unsigned long long)rank, g * step, kWave);
+      const uint64_t r = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(rank >> 32), g * step) << 32 |
+                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)rank, g * step);
       before += r > rank || (r == rank && g < mine);
     }
     const uint64_t kept = __ballot(before < a.top_groups && mine < a.groups);
@@ -696,9 +698,9 @@ __global__ __launch_bounds__(kRouteWaves * kWave) void route_bwd_kernel(RouteArg
   if (left > 0) store_elements<NE>(dlogits + row * a.E + e0, left, out);
 }
 
-// Rows that fill the machine with 16 experts a lane (256 experts, 16384 rows: 23 us, 32 with 4 a lane;
-// 4 rows: 12.4 and 6.4 us a call).
-constexpr int64_t kManyRows = 4096;
+// Logits that fill the machine with 16 experts a lane (8192 rows of 256 experts: 11.2 us, 15.3 with 4 a
+// lane; 16384 of 128: 11.6 and 13.5; 4096 of 128: 10.3 and 8.2; 1024 of 256: 6.0 and 4.9).
+constexpr int64_t kManyLogits = 5 << 18;
 
 // Calls f with the lanes a row takes and the experts a lane.
 template <bool MANY, typename F>
@@ -742,7 +744,7 @@ hipError_t launch_route_fwd(const RouteArgs& a, int bf16, int32_t* chosen, float
     if (a.K < LPR) counted(std::true_type{});
     else counted(std::false_type{});
   };
-  if (a.T >= kManyRows) with_row_shape<true>(a.E, go);
+  if (a.T * a.E >= kManyLogits) with_row_shape<true>(a.E, go);
   else with_row_shape<false>(a.E, go);
   return hipGetLastError();
 }

@@ -246,3 +246,15 @@ def test_large_tiles(L, T, V, D, xt, tt, gt):
         ref = a @ c
         bound = tol * mag + (2.0 ** -8 * ref.abs() * (1 + tol) + 2.0 ** -8 * tol * mag if bf16 else 0)
         assert ((got.double() - ref).abs() <= bound + 1e-30).all(), (got is dx, ((got.double() - ref).abs() / bound).max())
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_no_tokens_leaves_a_table_of_zeros(L, accumulate):
+    """An odd number of bf16 elements on an address of two bytes; its neighbours stay."""
+    buf = torch.ones(3 * 5 + 2, dtype=torch.bfloat16, device="cuda")
+    dtable = buf[1:16].view(3, 5)
+    none = torch.empty(0, device="cuda")
+    announce("cross entropy backward without tokens", accumulate)
+    dx, _ = L.luq_cross_entropy_bwd(none, torch.empty(0, 5, dtype=torch.bfloat16, device="cuda"), torch.ones(3, 5, dtype=torch.bfloat16, device="cuda"),
+                                    torch.empty(0, dtype=torch.int32, device="cuda"), none, accumulate=accumulate, dtable=dtable)
+    assert dx.shape == (0, 5) and (dtable == (1 if accumulate else 0)).all() and buf[0] == buf[16] == 1

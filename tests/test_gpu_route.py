@@ -205,12 +205,13 @@ def test_many_rows(L, E, groups, top_groups):
     order of a sum of 500 terms."""
     for score, bias, best, dt in (("sigmoid", True, 2, "f32"), ("softmax", True, 1, "bf16"), ("softmax", False, 1, "f32"),
                                   ("sigmoid", False, 1, "bf16"), ("softmax", False, 2, "bf16")):
-        l, b, _ = _inputs(4099, E, dt, seed=3, bias=bias)
-        l[100, 3], l[4098, E - 1] = float("nan"), float("inf")
+        T = max(4099, 1400000 // E)
+        l, b, _ = _inputs(T, E, dt, seed=3, bias=bias)
+        l[100, 3], l[T - 1, E - 1] = float("nan"), float("inf")
         announce("route_fwd many rows", E, groups, score, bias, best, dt)
         for k, renorm in ((8, True), (min(20, top_groups * (E // groups)), False)):
             got = L.luq_route_fwd(l, k, score, b, groups, top_groups, best, renorm)
-            for r in (0, 1500, 3000, 4000):
+            for r in (0, 1500, 3000, T - 99):
                 part = L.luq_route_fwd(l[r:r + 99], k, score, b, groups, top_groups, best, renorm)
                 assert torch.equal(got[0][r:r + 99], part[0])
                 assert torch.allclose(got[1][r:r + 99], part[1], rtol=500 * 2.0 ** -24, atol=0, equal_nan=True)
