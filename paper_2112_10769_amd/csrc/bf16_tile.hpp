@@ -70,6 +70,16 @@ __device__ __forceinline__ void read_across(const uint32_t (&p)[2], v4h (&f)[4])
                : "memory");
 }
 template <int O1, int O2>
+__device__ __forceinline__ void read_across(const uint32_t (&p)[3], v4h (&f)[6]) {
+  asm volatile(LUQ_TR(0, 6) " offset:%9\n" LUQ_TR(1, 6) " offset:%10\n"
+               LUQ_TR(2, 7) " offset:%9\n" LUQ_TR(3, 7) " offset:%10\n"
+               LUQ_TR(4, 8) " offset:%9\n" LUQ_TR(5, 8) " offset:%10\n"
+               "s_waitcnt lgkmcnt(0)"
+               : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5])
+               : "v"(p[0]), "v"(p[1]), "v"(p[2]), "n"(O1), "n"(O2)
+               : "memory");
+}
+template <int O1, int O2>
 __device__ __forceinline__ void read_across(const uint32_t (&p)[4], v4h (&f)[8]) {
   asm volatile(LUQ_TR(0, 8) " offset:%12\n" LUQ_TR(1, 8) " offset:%13\n"
                LUQ_TR(2, 9) " offset:%12\n" LUQ_TR(3, 9) " offset:%13\n"

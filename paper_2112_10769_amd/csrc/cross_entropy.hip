@@ -62,7 +62,7 @@ struct PackArgs {
   int i64;
   int64_t vocab;
   uint16_t* out;
-  int64_t ld, plane;
+  int64_t width, ld, plane;   // width: cols, up to a multiple of eight
   __device__ __forceinline__ bool kept(int64_t row) const {
     if (!targets) return true;
     const int64_t y = target_of(targets, i64, row);
@@ -72,7 +72,7 @@ struct PackArgs {
 
 template <typename T, int N>
 __global__ __launch_bounds__(256) void pack_rows_kernel(PackArgs a) {
-  const int64_t pieces = a.ld / 8;
+  const int64_t pieces = a.width / 8;
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < a.rows * pieces; at += (int64_t)gridDim.x * 256) {
     const int64_t row = at / pieces, c = (at - row * pieces) * 8;
     float v[8];
@@ -93,6 +93,9 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackArgs a) {
 // 128 x 128 (1100; two a CU) where there are few tiles.
 using BigTile = Bf16Tile<2, 4, 4, 2, 64, 2>;
 using SmallTile = Bf16Tile<2, 2, 2, 2, 64, 2>;
+// The same alone on its CU: eight waves and three stages under way (the gradients of 300 tokens on 3000 x
+// 700 in fp32: 103 us, 112 with four waves and one stage, 111 with three).
+using DeepTile = Bf16Tile<4, 2, 1, 2, 64, 4>;
 // A few rows: bound by the read of the table, six stages of which are under way (two workgroups a CU).
 using ThinTile = Bf16Tile<1, 2, 1, 1, 64, 6>;
 
@@ -195,6 +198,7 @@ __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g
 // (hipcc leaves the host's side of the tiles' kernels out unless asked for)
 template __global__ void loss_tile_kernel<BigTile>(Bf16Product, LossArgs);
 template __global__ void loss_tile_kernel<SmallTile>(Bf16Product, LossArgs);
+template __global__ void loss_tile_kernel<DeepTile>(Bf16Product, LossArgs);
 template __global__ void loss_tile_kernel<ThinTile>(Bf16Product, LossArgs);
 
 // Parts of a row joined, one after the other.
@@ -403,6 +407,7 @@ __global__ __launch_bounds__(Tile::kThreads) void grad_tile_kernel(Bf16Product g
 
 template __global__ void grad_tile_kernel<BigTile>(Bf16Product, GradArgs);
 template __global__ void grad_tile_kernel<SmallTile>(Bf16Product, GradArgs);
+template __global__ void grad_tile_kernel<DeepTile>(Bf16Product, GradArgs);
 template __global__ void grad_tile_kernel<ThinTile>(Bf16Product, GradArgs);
 
 // Where a product's sums go: partial sums (fp32, one matrix a split, added to when `add`), or an
@@ -494,6 +499,8 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
 
 template __global__ void out_tile_kernel<BigTile, false>(Bf16Product, OutArgs);
 template __global__ void out_tile_kernel<SmallTile, false>(Bf16Product, OutArgs);
+template __global__ void out_tile_kernel<DeepTile, false>(Bf16Product, OutArgs);
+template __global__ void out_tile_kernel<DeepTile, true>(Bf16Product, OutArgs);
 template __global__ void out_tile_kernel<BigTile, true>(Bf16Product, OutArgs);
 template __global__ void out_tile_kernel<SmallTile, true>(Bf16Product, OutArgs);
 
@@ -518,6 +525,9 @@ __global__ __launch_bounds__(256) void out_join_kernel(OutArgs a, const float* _
 
 int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Elements from a laid out row to the next: whole 128-byte lines (the loss of 1000 tokens on 1000 x 1000 in
+// fp32: 64 us, 74 with rows of 2000 bytes).
+int64_t pitch(int64_t cols) { return ceil_div(cols, 64) * 64; }
 
 // All pairs of na and nb terms whose product is not below 2^-24 of the largest; the smallest
 // first, while the sums are small (509 tokens in fp32, gradient of the table: 1.5e-6 of its norm off,
@@ -538,7 +548,7 @@ PlanePairs pairs_of(int na, int nb) {
 // A product's tile and the splits of its reduction, by predicted time: a CU's one large tile takes
 // 1.65 us a stage of 64 k, its two small ones 1.0 (0.6 alone), and beginning and end 4 us; the splits'
 // sums are written and read again.
-enum class Edge { kThin, kSmall, kBig };
+enum class Edge { kThin, kSmall, kDeep, kBig };
 struct Choice {
   Edge edge;
   int splits;
@@ -555,7 +565,7 @@ Choice choose(int64_t M, int64_t N, int64_t stages, int most_splits) {
       if (s > 1) t += 3.0 + (double)s * M * N * 8.0 / 4.5e6;
       if (t < least) {
         least = t;
-        best = {big ? Edge::kBig : Edge::kSmall, s};
+        best = {big ? Edge::kBig : groups <= 256 ? Edge::kDeep : Edge::kSmall, s};
       }
     }
   }
@@ -573,7 +583,10 @@ Choice choose_logits(int64_t T, int64_t V, int64_t stages) {
 // Calls f with the tile.
 template <typename F>
 auto with_tile(Edge edge, F f) {
-  return edge == Edge::kBig ? f(BigTile{}) : edge == Edge::kSmall ? f(SmallTile{}) : f(ThinTile{});
+  return edge == Edge::kBig     ? f(BigTile{})
+         : edge == Edge::kSmall ? f(SmallTile{})
+         : edge == Edge::kDeep  ? f(DeepTile{})
+                                : f(ThinTile{});
 }
 static_assert(BigTile::BK == SmallTile::BK && BigTile::BK == ThinTile::BK, "one stage");
 constexpr int kStage = BigTile::BK;
@@ -589,7 +602,7 @@ struct Carver {
 
 // How a call is laid out; the same for its workspace query and its launches.
 struct Layout {
-  int64_t T, V, D, D8;
+  int64_t T, V, D, D8, ld;    // ld: of laid out rows
   int xn, tn;                 // terms of x and the table
   bool pack_x, pack_t;        // laid out in rows: fp32, or rows that are no whole 16-byte pieces
   size_t x_rows, t_rows;      // offsets in the workspace
@@ -607,13 +620,13 @@ struct Layout {
   size_t bytes;
   // x is laid out in the backward call too where it need not be: a row that is padding becomes
   // zeros, since 0 times what it holds need not be 0.
-  Layout(int64_t T_, int64_t V_, int64_t D_, int x_bf16, int t_bf16, bool back) : T(T_), V(V_), D(D_), D8(up8(D_)) {
+  Layout(int64_t T_, int64_t V_, int64_t D_, int x_bf16, int t_bf16, bool back) : T(T_), V(V_), D(D_), D8(up8(D_)), ld(pitch(D8)) {
     xn = x_bf16 ? 1 : 3;
     tn = t_bf16 ? 1 : 3;
     pack_x = back || !x_bf16 || (D & 7);
     pack_t = !t_bf16 || (D & 7);
-    x_rows = c.take(pack_x ? (size_t)xn * T * D8 * 2 : 0);
-    t_rows = c.take(pack_t ? (size_t)tn * V * D8 * 2 : 0);
+    x_rows = c.take(pack_x ? (size_t)xn * T * ld * 2 : 0);
+    t_rows = c.take(pack_t ? (size_t)tn * V * ld * 2 : 0);
   }
   void forward() {
     z = choose_logits(T, V, logits_stages());
@@ -655,7 +668,7 @@ struct Layout {
 };
 
 void pack_rows(const PackArgs& a, int bf16, hipStream_t st) {
-  const int64_t need = ceil_div(a.rows * (a.ld / 8), 256);
+  const int64_t need = ceil_div(a.rows * (a.width / 8), 256);
   const dim3 grid((unsigned)(need < 16384 ? need : 16384));
   if (bf16) hipLaunchKernelGGL((pack_rows_kernel<uint16_t, 1>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(256), 0, st, a);
@@ -668,13 +681,13 @@ Bf16Product logits_product(const CrossEntropyArgs& a, const Layout& l, bool back
   g.B = {static_cast<const uint16_t*>(a.table), a.V, a.D, 0};
   if (l.pack_x) {
     uint16_t* const out = reinterpret_cast<uint16_t*>(ws + l.x_rows);
-    pack_rows({a.x, a.T, a.D, back ? a.targets : nullptr, a.i64, a.V, out, l.D8, a.T * l.D8}, a.x_bf16, st);
-    g.A = {out, a.T, l.D8, a.T * l.D8};
+    pack_rows({a.x, a.T, a.D, back ? a.targets : nullptr, a.i64, a.V, out, l.D8, l.ld, a.T * l.ld}, a.x_bf16, st);
+    g.A = {out, a.T, l.ld, a.T * l.ld};
   }
   if (l.pack_t) {
     uint16_t* const out = reinterpret_cast<uint16_t*>(ws + l.t_rows);
-    pack_rows({a.table, a.V, a.D, nullptr, 0, 0, out, l.D8, a.V * l.D8}, a.t_bf16, st);
-    g.B = {out, a.V, l.D8, a.V * l.D8};
+    pack_rows({a.table, a.V, a.D, nullptr, 0, 0, out, l.D8, l.ld, a.V * l.ld}, a.t_bf16, st);
+    g.B = {out, a.V, l.ld, a.V * l.ld};
   }
   g.pairs = pairs_of(l.xn, l.tn);
   g.K = l.pack_x || l.pack_t ? l.D8 : a.D;
@@ -708,6 +721,7 @@ void out_product(Bf16Product g, OutArgs o, Choice c, hipStream_t st) {
   const int stages = g.pairs.count * (int)ceil_div(g.K, kStage);
   o.chunk = (int)ceil_div(stages, c.splits);
   if (c.edge == Edge::kBig) out_tiles<BigTile, CA>(g, o, c.splits, st);
+  else if (c.edge == Edge::kDeep) out_tiles<DeepTile, CA>(g, o, c.splits, st);
   else out_tiles<SmallTile, CA>(g, o, c.splits, st);
 }
 
@@ -746,6 +760,7 @@ hipError_t launch_cross_entropy_fwd(const CrossEntropyArgs& a, float* loss, floa
                     reinterpret_cast<float*>(w + l.at_target)};
   if (l.z.edge == Edge::kBig) loss_tiles<BigTile>(g, la, st);
   else if (l.z.edge == Edge::kSmall) loss_tiles<SmallTile>(g, la, st);
+  else if (l.z.edge == Edge::kDeep) loss_tiles<DeepTile>(g, la, st);
   else loss_tiles<ThinTile>(g, la, st);
   const LossOut out{a.smoothing, loss, lse};
   if (a.T <= kFewRows) hipLaunchKernelGGL(loss_join_few_kernel, dim3((unsigned)a.T), dim3(1024), 0, st, la, l.parts, out);
@@ -777,6 +792,7 @@ hipError_t launch_cross_entropy_bwd(const CrossEntropyArgs& a, const float* dlos
     const GradArgs ga{a.targets, a.i64, a.T, a.V, v0, cols, a.scale, a.smoothing, dloss, lse, half(l.g), l.piece, a.T * l.piece, l.g_terms()};
     if (l.z.edge == Edge::kBig) grad_tiles<BigTile>(z, ga, st);
     else if (l.z.edge == Edge::kSmall) grad_tiles<SmallTile>(z, ga, st);
+    else if (l.z.edge == Edge::kDeep) grad_tiles<DeepTile>(z, ga, st);
     else grad_tiles<ThinTile>(z, ga, st);
     const Bf16Planes grad{half(l.g), a.T, l.piece, a.T * l.piece};
     // dx += g W
