@@ -118,8 +118,19 @@ struct LossArgs {
   int64_t T, V;
   float scale;
   int smoothed;    // whether the sum of logits is asked for
-  float* part;     // [column parts][3][T]: maximum (times log2 e), sum of exponentials, sum of logits
+  float* part;     // [tiles of columns][3][T]: maximum (times log2 e), sum of exponentials, sum of logits
   float* at_target;
+};
+
+// Parts of a row joined, one after the other.
+struct RowSum {
+  float top = -3.0e38f, sum = 0.0f, all = 0.0f;
+  __device__ __forceinline__ void add(float m, float s, float z) {
+    const float next = fmaxf(top, m);
+    sum = sum * __builtin_amdgcn_exp2f(top - next) + s * __builtin_amdgcn_exp2f(m - next);
+    top = next;
+    all += z;
+  }
 };
 
 template <typename Tile>
@@ -145,7 +156,9 @@ __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g
         for (int e = 0; e < 16; ++e)
           if (at.col(j, e / 4) + e % 4 >= a.V) tile.acc[i][j][e] = none;
   }
-  const int64_t part = (int64_t)tn * Tile::WN + (threadIdx.x >> 6) % Tile::WN;
+  // a row's sums of each wave, joined at the end: [3][waves][rows of the tile]
+  float* const red = reinterpret_cast<float*>(lds) + (threadIdx.x >> 6) % Tile::WN * Tile::BM;
+  constexpr int kNext = Tile::WN * Tile::BM;
 #pragma unroll
   for (int i = 0; i < Tile::TM; ++i) {
     const int64_t row = at.row(i);
@@ -186,13 +199,25 @@ __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g
 #pragma unroll
       for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(tile.acc[i][j][e], c, -top));
     sum += __shfl_xor(sum, 32, kWave);
-    if (half == 0 && row < a.T) {
-      float* const out = a.part + part * 3 * a.T + row;
+    if (half == 0) {
+      float* const out = red + (row - m0);
       out[0] = top;
-      out[a.T] = sum;
-      out[2 * a.T] = all * a.scale;
+      out[kNext] = sum;
+      out[2 * kNext] = all * a.scale;
     }
   }
+  __syncthreads();
+  static_assert(Tile::BM <= Tile::kThreads, "a thread a row");
+  const int64_t row = m0 + threadIdx.x;
+  if (threadIdx.x >= Tile::BM || row >= a.T) return;
+  const float* const in = reinterpret_cast<const float*>(lds) + threadIdx.x;
+  RowSum r;
+#pragma unroll
+  for (int w = 0; w < Tile::WN; ++w) r.add(in[w * Tile::BM], in[kNext + w * Tile::BM], in[2 * kNext + w * Tile::BM]);
+  float* const out = a.part + (int64_t)tn * 3 * a.T + row;
+  out[0] = r.top;
+  out[a.T] = r.sum;
+  if (a.smoothed) out[2 * a.T] = r.all;
 }
 
 // (hipcc leaves the host's side of the tiles' kernels out unless asked for)
@@ -200,17 +225,6 @@ template __global__ void loss_tile_kernel<BigTile>(Bf16Product, LossArgs);
 template __global__ void loss_tile_kernel<SmallTile>(Bf16Product, LossArgs);
 template __global__ void loss_tile_kernel<DeepTile>(Bf16Product, LossArgs);
 template __global__ void loss_tile_kernel<ThinTile>(Bf16Product, LossArgs);
-
-// Parts of a row joined, one after the other.
-struct RowSum {
-  float top = -3.0e38f, sum = 0.0f, all = 0.0f;
-  __device__ __forceinline__ void add(float m, float s, float z) {
-    const float next = fmaxf(top, m);
-    sum = sum * __builtin_amdgcn_exp2f(top - next) + s * __builtin_amdgcn_exp2f(m - next);
-    top = next;
-    all += z;
-  }
-};
 
 // The outputs of a row from its sums.
 struct LossOut {
@@ -245,7 +259,7 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t par
         const float* const src = a.part + (q < parts ? q : p) * 3 * a.T + row;
         m[u] = q < parts ? src[0] : -3.0e38f;
         s[u] = q < parts ? src[a.T] : 0.0f;
-        z[u] = q < parts ? src[2 * a.T] : 0.0f;
+        z[u] = a.smoothed && q < parts ? src[2 * a.T] : 0.0f;
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) r.add(m[u], s[u], z[u]);
@@ -261,8 +275,8 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t par
   out.put(a, row, all);
 }
 
-// The same for few rows: a workgroup a row (the loss of 128 rows on 50021 x 1024: 32 us, 39 with 64 rows
-// a workgroup; its parts are read four bytes at a time, which many rows do not hide).
+// The same for few rows: a workgroup a row (the loss of 128 rows on 50021 x 1024: 30.3 us, 33.4 with 64
+// rows a workgroup; of 256 rows 40 with either: the parts are read four bytes at a time here).
 __global__ __launch_bounds__(1024) void loss_join_few_kernel(LossArgs a, int64_t parts, LossOut out) {
   __shared__ float red[3][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -270,7 +284,7 @@ __global__ __launch_bounds__(1024) void loss_join_few_kernel(LossArgs a, int64_t
   RowSum r;
   for (int64_t p = threadIdx.x; p < parts; p += 1024) {
     const float* const src = a.part + p * 3 * a.T + row;
-    r.add(src[0], src[a.T], src[2 * a.T]);
+    r.add(src[0], src[a.T], a.smoothed ? src[2 * a.T] : 0.0f);
   }
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) {
@@ -572,8 +586,9 @@ Choice choose(int64_t M, int64_t N, int64_t stages, int most_splits) {
   return best;
 }
 
-// The logits' tile: up to kThinRows rows are bound by the table's read (the loss of 32 rows on
-// 32000 x 4096: 62 us, 76 with the tile of 128 x 128; on 50021 x 1024 31 and 34; of 64 rows there 42 and 36).
+// The logits' tile: up to kThinRows rows are bound by the table's read (one row on 32000 x 4096: 58.6 us, 59.9
+// with the tile of 128 x 128; the gradients of 32 rows on 50021 x 1024 118 and 121; the loss of 64 there
+// 39 and 28).
 constexpr int64_t kThinRows = 32;
 Choice choose_logits(int64_t T, int64_t V, int64_t stages) {
   if (T <= kThinRows) return {Edge::kThin, 1};
@@ -630,7 +645,7 @@ struct Layout {
   }
   void forward() {
     z = choose_logits(T, V, logits_stages());
-    parts = with_tile(z.edge, [&](auto tile) { return ceil_div(V, decltype(tile)::BN) * decltype(tile)::WN; });
+    parts = with_tile(z.edge, [&](auto tile) { return ceil_div(V, decltype(tile)::BN); });
     part = c.take((size_t)parts * 3 * T * sizeof(float));
     at_target = c.take((size_t)T * sizeof(float));
     bytes = c.at;
