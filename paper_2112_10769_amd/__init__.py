@@ -808,7 +808,7 @@ def luq_adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copy=None, w
 def luq_adamw_step(plan, lr, step, betas=(0.9, 0.999), eps=1e-8, seed=0, grad_scale=None):
     """One AdamW step of the plan's tensors.  lr (float32), step (int64, from 1) and grad_scale (float32, or None for 1)
     hold one element on the device; a grad_scale that is not finite skips the step."""
-    gpu = plan.gpu
+    gpu = plan.gpu if plan.count else lr.get_device()
     if step.dtype is not torch.int64 or step.numel() != 1 or step.get_device() != gpu:
         raise ValueError("step must be one int64 on the plan's device")
     st = LIB.luq_adamw_step(plan.plan.data_ptr(), plan.bytes, plan.count, _scalar(lr, gpu, "lr"), step.data_ptr(), betas[0],

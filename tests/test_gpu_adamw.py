@@ -212,3 +212,12 @@ def test_plan_keeps_and_empty(L):
     plan = _plan(L, [t])
     want = [t["p"].data_ptr(), t["m"].data_ptr()]
     assert [plan.tensors[0][0].data_ptr(), plan.tensors[2][0].data_ptr()] == want
+
+
+def test_a_plan_of_nothing(L):
+    """No tensors, or tensors without elements: a step that does nothing."""
+    lr, step = torch.full((1,), 1e-3, device="cuda"), torch.ones(1, dtype=torch.int64, device="cuda")
+    none = [torch.empty(0, device="cuda") for _ in range(4)]
+    for lists in ([], [], [], []), [[t] for t in none]:
+        L.luq_adamw_step(L.luq_adamw_plan(*lists), lr, step)
+    torch.cuda.synchronize()
