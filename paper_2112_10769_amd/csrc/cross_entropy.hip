@@ -96,7 +96,7 @@ using SmallTile = Bf16Tile<2, 2, 2, 2, 64, 2>;
 // The same alone on its CU: eight waves and three stages under way (the gradients of 300 tokens on 3000 x
 // 700 in fp32: 103 us, 112 with four waves and one stage, 111 with three).
 using DeepTile = Bf16Tile<4, 2, 1, 2, 64, 4>;
-// A few rows: bound by the read of the table, six stages of which are under way (two workgroups a CU).
+// A few rows, bound by the read of the table, or a few tiles: six stages are under way (two workgroups a CU).
 using ThinTile = Bf16Tile<1, 2, 1, 1, 64, 6>;
 
 // Where a lane's sums lie: row `row(i)` of the matrix, columns col(j, q) .. + 3 in registers 4q .. 4q + 3.
@@ -566,10 +566,10 @@ enum class Edge { kThin, kSmall, kDeep, kBig };
 struct Choice {
   Edge edge;
   int splits;
+  double us;   // predicted
 };
 Choice choose(int64_t M, int64_t N, int64_t stages, int most_splits) {
-  Choice best{Edge::kSmall, 1};
-  double least = 1e300;
+  Choice best{Edge::kSmall, 1, 1e300};
   for (int big = 0; big < 2; ++big) {
     const int64_t edge = big ? 256 : 128, tiles = ceil_div(M, edge) * ceil_div(N, edge);
     for (int s = 1; s <= most_splits && (s == 1 || stages / s >= 2); ++s) {
@@ -577,10 +577,7 @@ Choice choose(int64_t M, int64_t N, int64_t stages, int most_splits) {
       const double stage = big ? 1.65 : groups <= 256 ? 0.6 : 1.0;
       double t = (double)ceil_div(groups, slots) * ((double)ceil_div(stages, s) * stage + 4.0);
       if (s > 1) t += 3.0 + (double)s * M * N * 8.0 / 4.5e6;
-      if (t < least) {
-        least = t;
-        best = {big ? Edge::kBig : groups <= 256 ? Edge::kDeep : Edge::kSmall, s};
-      }
+      if (t < best.us) best = {big ? Edge::kBig : groups <= 256 ? Edge::kDeep : Edge::kSmall, s, t};
     }
   }
   return best;
@@ -588,11 +585,16 @@ Choice choose(int64_t M, int64_t N, int64_t stages, int most_splits) {
 
 // The logits' tile: up to kThinRows rows are bound by the table's read (one row on 32000 x 4096: 58.6 us, 59.9
 // with the tile of 128 x 128; the gradients of 32 rows on 50021 x 1024 118 and 121; the loss of 64 there
-// 39 and 28).
+// 39 and 28).  So are few tiles with long rows, bound by a CU's loads (0.3 us a stage, 0.36 with two
+// tiles a CU): the loss of 1000 rows on 1000 x 1000 fp32 takes 48 us, 65 with 128 x 128, of 3812 on 206 x
+// 3144 121 and 176, but of 323 on 6004 x 3364 304 and 199.
 constexpr int64_t kThinRows = 32;
 Choice choose_logits(int64_t T, int64_t V, int64_t stages) {
-  if (T <= kThinRows) return {Edge::kThin, 1};
-  return choose(T, V, stages, 1);
+  const int64_t groups = ceil_div(T, ThinTile::BM) * ceil_div(V, ThinTile::BN);
+  const Choice thin{Edge::kThin, 1, (double)ceil_div(groups, 512) * ((double)stages * (groups <= 256 ? 0.3 : 0.36) + 4.0)};
+  if (T <= kThinRows) return thin;
+  const Choice other = choose(T, V, stages, 1);
+  return thin.us < other.us ? thin : other;
 }
 
 // Calls f with the tile.

@@ -258,3 +258,24 @@ def test_no_tokens_leaves_a_table_of_zeros(L, accumulate):
     dx, _ = L.luq_cross_entropy_bwd(none, torch.empty(0, 5, dtype=torch.bfloat16, device="cuda"), torch.ones(3, 5, dtype=torch.bfloat16, device="cuda"),
                                     torch.empty(0, dtype=torch.int32, device="cuda"), none, accumulate=accumulate, dtable=dtable)
     assert dx.shape == (0, 5) and (dtable == (1 if accumulate else 0)).all() and buf[0] == buf[16] == 1
+
+
+@pytest.mark.parametrize("T,V,D,xt,tt", [(1000, 129, 700, "f32", "f32"), (33, 1000, 1500, "bf16", "bf16"), (513, 65, 1033, "bf16", "f32")])
+def test_few_tiles(L, T, V, D, xt, tt):
+    """Sizes of few tiles with long reductions: the sums of a row against 64 bits, and the gradient of a row in the batch
+    against that of the row alone, whose tiles are others."""
+    x, w, y, dloss = _inputs(T, V, D, xt, tt)
+    announce("cross entropy, few tiles", T, V, D, xt, tt)
+    loss, lse = L.luq_cross_entropy_fwd(x, w, y, 1.0, 0.1)
+    z = x.double() @ w.double().t()
+    ok = y >= 0
+    want = torch.logsumexp(z, 1)
+    ez = (x.double().abs() @ w.double().abs().t()).amax(1) * (S._chain(S._pairs(1 if xt == "bf16" else 3, 1 if tt == "bf16" else 3), D) * 2 + 8) * 2.0 ** -24
+    assert ((lse - want).abs()[ok] <= (3 * ez + (200 + V / 128) * 2.0 ** -24 * (1 + want.abs()))[ok]).all()
+    dx, dw = L.luq_cross_entropy_bwd(dloss, x, w, y, lse, 1.0, 0.1)
+    for r in (0, T // 2, T - 1):
+        one, _ = L.luq_cross_entropy_bwd(dloss[r:r + 1], x[r:r + 1].clone(), w, y[r:r + 1], lse[r:r + 1], 1.0, 0.1)
+        far = (one.double() - dx[r:r + 1].double()).norm()
+        # two results, each off by a rounding of g and the output (2^-8 each in bf16) or by 3 ez of its g and 100 roundings
+        size = dx[r:r + 1].double().norm() + dloss[r].abs().double() * w.double().norm(dim=1).amax()
+        assert far <= size * (4 * 2.0 ** -8 if xt == "bf16" else 2 * (3 * ez[r] + 100 * 2.0 ** -24)), (r, far, size)
