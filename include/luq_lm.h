@@ -244,8 +244,8 @@ luq_status luq_route_bwd(const float* dweights, const void* logits, luq_dtype dt
  * Products are those of bf16 matrix instructions with fp32 sums.  An fp32 tensor is taken
  * as three bf16 terms (24 bits, fewer below 2^-110: a term is a multiple of 2^-133), of
  * whose products those above 2^-24 are formed.
- * In the backward call the logits' gradient is rounded to one bf16 term for a bf16 output,
- * to two (16 bits) for an fp32 gradient of bf16 activations, and to three otherwise.
+ * In the backward call the logits' gradient is rounded to one bf16 term for a bf16 output
+ * and to three (24 bits) for an fp32 one.
  */
 
 /* Bytes of the workspace of the forward call (gt = -1) or of the backward call (gt: type

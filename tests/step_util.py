@@ -164,7 +164,7 @@ def loss_grad(dloss, x, w, targets, lse, scale, eps, x_bf16, w_bf16, g_bf16, bef
     eg = np.abs(up) * (p * (ez + (np.abs(z) + 2 * np.abs(z - np.where(ok, lse, 0.0)[:, None]) + 8) * 2 * U)
                        + 4 * U * (p + hot + eps / V))
     nx, nw = (1 if x_bf16 else 3), (1 if w_bf16 else 3)
-    rows, cols = (1 if x_bf16 else 3), (1 if g_bf16 else 2 if x_bf16 else 3)
+    rows, cols = (1 if x_bf16 else 3), (1 if g_bf16 else 3)
     tx, xt = (2 if x_bf16 and nw > 2 else nw), (2 if g_bf16 and nx > 2 else nx)
     ag, ax, aw = np.abs(g), np.abs(x), np.abs(w)
 
