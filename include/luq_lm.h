@@ -190,7 +190,8 @@ luq_status luq_gemm_wgrad_grouped(const uint8_t* g_codes_t, const float* alpha, 
  * two largest (2; of those there are), and the experts of the top_groups first runs
  * remain; of these the top_k largest c are taken, the largest first.  Equal values:
  * the lower index first.  c is compared as if exact (in 64 bits where it is a sum), so
- * that a choice does not hang on the rounding of an exponential.
+ * that a choice does not hang on the rounding of an exponential: without a bias experts have
+ * the order of their logits, and only the ranks of groups by two are sums.
  *   w_k = scale * s_k, or with renorm scale * s_k / (sum of the row's chosen s)
  *
  * A logit or a bias of -inf bars an expert.  Where fewer than top_k remain, the places

@@ -184,6 +184,12 @@ __device__ void route_exact(const RouteArgs& a, int64_t row, uint64_t* keys, int
     for (int i = 0; i < NE; ++i)
       if (i < left && !(kept >> ((e0 + i) / size * step) & 1)) key[i] = 0;
   }
+  // without a bias the order within the groups is that of the logits, also where scores round to the same
+  // number (a sigmoid's above 37 to 1, a softmax's 745 below the largest to 0)
+  if (!a.bias) {
+#pragma unroll
+    for (int i = 0; i < NE; ++i) key[i] = key[i] ? key_of((double)l[i]) : 0;
+  }
   uint64_t best = 0;
   int at = 0;
   auto local = [&]() {

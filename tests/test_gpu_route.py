@@ -215,3 +215,33 @@ def test_many_rows(L, E, groups, top_groups):
                 part = L.luq_route_fwd(l[r:r + 99], k, score, b, groups, top_groups, best, renorm)
                 assert torch.equal(got[0][r:r + 99], part[0])
                 assert torch.allclose(got[1][r:r + 99], part[1], rtol=500 * 2.0 ** -24, atol=0, equal_nan=True)
+
+
+@pytest.mark.parametrize("E,groups,top_groups", [(16, 2, 1), (64, 8, 4), (72, 4, 3), (256, 8, 4), (520, 8, 4), (1100, 10, 5)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_saturated_scores_keep_the_logits_order(L, E, groups, top_groups, score):
+    """Without a bias the experts of the groups that remain are ordered by their logits, also where scores of 64 bits are
+    equal: sigmoids of logits above 37 are 1, softmaxes of logits 745 below the largest are 0, and logits of 10^-20 and of
+    twice that have the same scores of either kind."""
+    size, k = E // groups, 6
+    rng = np.random.default_rng(E)
+    for spread, dt in ((60.0, "f32"), (3000.0, "f32"), (3000.0, "bf16"), (1e-20, "f32")):
+        rows = rng.permuted(np.tile(np.arange(E), (37, 1)), axis=1) * (spread / E) + (40.0 if spread == 60.0 else 0.0)
+        l = torch.tensor(rows, dtype=torch.float32, device="cuda").to(DT[dt])
+        announce("route_fwd saturated", E, groups, score, spread, dt)
+        experts, weights = L.luq_route_fwd(l, k, score, None, groups, top_groups, 2)
+        s, l64, at = S.scores(S.f64(l), score), S.f64(l), host(experts)
+        for t in range(37):
+            rank = np.sort(s[t].reshape(groups, size), 1)[:, -2:].sum(1)
+            kept = sorted(range(groups), key=lambda g: (-rank[g], g))[:top_groups]
+            order = sorted((e for e in range(E) if e // size in kept), key=lambda e: (-l64[t, e], e))
+            assert at[t].tolist() == order[:k], (t, l64[t, at[t]], l64[t, order[:k]])
+        assert torch.isfinite(weights).all() and (weights.diff(dim=1) <= 0).all()
+
+
+def test_saturated_scores_of_a_pair(L):
+    """Logits of 40 and 50: both sigmoids are 1 in 64 bits, and the second is the larger."""
+    l = torch.full((1, 8), -1.0, device="cuda")
+    l[0, 1], l[0, 3] = 40.0, 50.0
+    for best in (1, 2):
+        assert L.luq_route_fwd(l, 2, "sigmoid", None, 2, 1, best)[0].tolist() == [[3, 1]]
