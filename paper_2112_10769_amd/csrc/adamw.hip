@@ -70,7 +70,8 @@ __device__ __forceinline__ float finite_or_zero(float a) { return a < __builtin_
 
 // The e4m3 code of magnitude a: of a over the block's power of two and over 2^120, so that e4m3's
 // subnormal numbers are fp32's, the sign-less upper twelve bits; or the code above if the fraction
-// between the two plus u / 2^16 reaches 1.  What is not finite becomes NaN.
+// between the two plus u / 2^16 reaches 1.  What is not finite becomes NaN; a NaN too comes in without
+// its sign, whose bit the addition would carry out of the word.
 __device__ __forceinline__ uint32_t encode(float a, int scale, uint32_t u) {
   const uint32_t bits = __float_as_uint(__builtin_amdgcn_ldexpf(a, 7 - scale));
   return min((bits + (u << 4)) >> 20, 0x7Fu);
@@ -245,7 +246,7 @@ __device__ __forceinline__ void chunk_u8(const AdamwEntry& e, const Common& c, i
     for (int k = 0; k < 4; ++k) {
       const uint32_t a = encode(fabsf(mk[k]), m_scale, u[k] & 0xFFFFu) | (__float_as_uint(mk[k]) >> 24 & 0x80u);
       // a root above 0 does not become 0: it divides
-      const uint32_t b = max(encode(r[k], r_scale, u[k] >> 16), min(__float_as_uint(r[k]), 1u));
+      const uint32_t b = max(encode(fabsf(r[k]), r_scale, u[k] >> 16), min(__float_as_uint(r[k]), 1u));
       mc |= a << (8 * k);
       rc |= b << (8 * k);
     }

@@ -221,3 +221,27 @@ def test_a_plan_of_nothing(L):
     for lists in ([], [], [], []), [[t] for t in none]:
         L.luq_adamw_step(L.luq_adamw_plan(*lists), lr, step)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("gt", ["f32", "bf16"])
+def test_every_nan_becomes_one(L, gt):
+    """NaN of both signs, with the smallest and the largest payloads, quiet and signalling, over many uniforms."""
+    words = [0x7FC00000, 0xFFC00000, 0x7FFFFFFF, 0xFFFFFFFF, 0x7F800001, 0xFF800001] if gt == "f32" else [0x7FC0, 0xFFC0, 0x7FFF, 0xFFFF, 0x7F81, 0xFF81]
+    kind = np.uint32 if gt == "f32" else np.uint16
+    nans = torch.from_numpy(np.array(words, dtype=kind).view(np.int32 if gt == "f32" else np.int16)).cuda().view(DT[gt])
+    n = 32 * 600
+    t, other = _one(n, gt, 8), _one(n, gt, 8)
+    bad = torch.arange(5, n, 32, device="cuda")           # one in each block
+    t["g"][bad] = nans[torch.arange(bad.numel(), device="cuda") % len(words)]
+    other["g"][bad] = 0.0
+    announce("adamw, every NaN", gt)
+    for x in (t, other):
+        L.luq_adamw_step(_plan(L, [x]), *_scalars(), seed=9)
+    assert torch.isnan(t["p"][bad]).all() and (t["m"][bad] % 128 == 127).all() and (t["v"][bad] == 127).all()
+    # the others of a block are as without the NaN, where its element is not the block's largest there
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[bad] = False
+    same = ((t["ms"] == other["ms"]) & (t["vs"] == other["vs"])).repeat_interleave(32)
+    assert same.float().mean() > 0.5
+    assert all(torch.equal(t[k][keep & same], other[k][keep & same]) for k in ("p", "m", "v"))
+    assert torch.isfinite(t["p"][keep]).all() and not (t["m"][keep] % 128 == 127).any() and not (t["v"][keep] == 127).any()
