@@ -482,6 +482,7 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
         const float v[4] = {tile.acc[i][j][4 * q], tile.acc[i][j][4 * q + 1], tile.acc[i][j][4 * q + 2], tile.acc[i][j][4 * q + 3]};
         slab.put(j, q, v);
       }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // the other lanes' parts of the slab
 #pragma unroll
     for (int u = 0; u < Slab<Tile>::kItems; ++u) {
       const int item = lane + u * 64, r = item / (Slab<Tile>::kCols / 8), c = item % (Slab<Tile>::kCols / 8) * 8;
@@ -510,6 +511,7 @@ __global__ __launch_bounds__(Tile::kThreads) void out_tile_kernel(Bf16Product g,
         a.put<float>(row, col, v);
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // read before the next rows are put there
   }
 }
 
