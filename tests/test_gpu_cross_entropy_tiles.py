@@ -1,6 +1,6 @@
 """Every kernel of the cross entropy (its logits' tiles, the tiles of both gradients with a whole and a split
 reduction and their epilogues, one and several pieces of the vocabulary, the joins of few and of many parts) against
-the plain form in 64 bits on the GPU."""
+the plain form in 64 bits on the GPU.  test_cross_entropy_plan_cpu.py holds that the shapes reach them."""
 import pytest
 
 torch = pytest.importorskip("torch")
