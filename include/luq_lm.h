@@ -255,7 +255,8 @@ size_t luq_cross_entropy_workspace(int64_t T, int64_t V, int64_t D, luq_dtype xt
 
 /*
  * luq_cross_entropy_fwd -- the loss of every token.
- *  loss, lse  out: [T] fp32; lse is 0 where the target is no row of the table.
+ *  loss, lse  out: [T] fp32; lse is 0 where the target is no row of the table.  The loss is summed from
+ *             differences to the row's largest logit: without smoothing it is not below 0.
  */
 luq_status luq_cross_entropy_fwd(const void* x, luq_dtype xt, const void* table, luq_dtype tt, const void* targets,
                                  luq_index it, int64_t T, int64_t V, int64_t D, float scale, float smoothing,

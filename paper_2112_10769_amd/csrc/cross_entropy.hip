@@ -21,7 +21,7 @@ namespace luq {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr float kLog2e = 1.44269504088896341f, kMost = 3.40282347e38f;   // kMost: fp32's largest number
 
 __device__ __forceinline__ int64_t target_of(const void* targets, int i64, int64_t t) {
   return i64 ? static_cast<const int64_t*>(targets)[t] : static_cast<const int32_t*>(targets)[t];
@@ -110,16 +110,17 @@ struct LossArgs {
   int64_t T, V;
   float scale;
   int smoothed;    // whether the sum of logits is asked for
-  float* part;     // [tiles of columns][3][T]: maximum (times log2 e), sum of exponentials, sum of logits
+  float* part;     // [tiles of columns][3][T]: maximum, sum of exponentials (over its own), sum of logits
   float* at_target;
 };
 
-// Parts of a row joined, one after the other.
+// Parts of a row joined, one after the other.  The maximum is a logit as it is rounded for the target too, and
+// its exponential is 1: the sum is no less than 1, and a loss without smoothing no less than 0.
 struct RowSum {
-  float top = -3.0e38f, sum = 0.0f, all = 0.0f;
+  float top = -kMost, sum = 0.0f, all = 0.0f;
   __device__ __forceinline__ void add(float m, float s, float z) {
     const float next = fmaxf(top, m);
-    sum = sum * __builtin_amdgcn_exp2f(top - next) + s * __builtin_amdgcn_exp2f(m - next);
+    sum = sum * __builtin_amdgcn_exp2f((top - next) * kLog2e) + s * __builtin_amdgcn_exp2f((m - next) * kLog2e);
     top = next;
     all += z;
   }
@@ -183,17 +184,18 @@ __global__ __launch_bounds__(Tile::kThreads) void loss_tile_kernel(Bf16Product g
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, tile.acc[i][j][e]);
     }
-    top = fmaxf(top * c, -3.0e38f);
-    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    const float other = __shfl_xor(top, 32, kWave);
+    top = c < 0.0f ? fminf(fminf(top, other), kMost) : fmaxf(fmaxf(top, other), -kMost);   // (columns beyond the table)
     float sum = 0.0f;
+    // differences of products, before the scale: exact near the maximum, and 0 there, however large it is
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(tile.acc[i][j][e], c, -top));
+      for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((tile.acc[i][j][e] - top) * c);
     sum += __shfl_xor(sum, 32, kWave);
     if (half == 0) {
       float* const out = red + (row - m0);
-      out[0] = top;
+      out[0] = top * a.scale;
       out[kNext] = sum;
       out[2 * kNext] = all * a.scale;
     }
@@ -226,12 +228,14 @@ struct LossOut {
   __device__ __forceinline__ void put(const LossArgs& a, int64_t row, const RowSum& r) const {
     const int64_t y = target_of(a.targets, a.i64, row);
     const bool kept = y >= 0 && y < a.V;
-    const float l = r.top * kLn2 + logf(r.sum);
-    lse[row] = kept ? l : 0.0f;
+    const float rest = logf(r.sum);
+    lse[row] = kept ? r.top + rest : 0.0f;
+    // differences to the maximum first: the loss keeps its bits however far from 0 the logits are
+    const float behind = kept ? r.top - a.at_target[row] : 0.0f;
     loss[row] = y < 0              ? 0.0f
                 : !kept            ? __builtin_nanf("")
-                : smoothing > 0.0f ? l - (1.0f - smoothing) * a.at_target[row] - smoothing / (float)a.V * r.all
-                                   : l - a.at_target[row];
+                : smoothing > 0.0f ? rest + (1.0f - smoothing) * behind + smoothing * (r.top - r.all / (float)a.V)
+                                   : rest + behind;
   }
 };
 
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int64_t par
       for (int u = 0; u < U; ++u) {
         const int64_t q = p + 16 * u;
         const float* const src = a.part + (q < parts ? q : p) * 3 * a.T + row;
-        m[u] = q < parts ? src[0] : -3.0e38f;
+        m[u] = q < parts ? src[0] : -kMost;
         s[u] = q < parts ? src[a.T] : 0.0f;
         z[u] = a.smoothed && q < parts ? src[2 * a.T] : 0.0f;
       }

@@ -279,3 +279,42 @@ def test_few_tiles(L, T, V, D, xt, tt):
         # two results, each off by a rounding of g and the output (2^-8 each in bf16) or by 3 ez of its g and 100 roundings
         size = dx[r:r + 1].double().norm() + dloss[r].abs().double() * w.double().norm(dim=1).amax()
         assert far <= size * (4 * 2.0 ** -8 if xt == "bf16" else 2 * (3 * ez[r] + 100 * 2.0 ** -24)), (r, far, size)
+
+
+@pytest.mark.parametrize("scale", [1.0, -0.7, 3.0])
+@pytest.mark.parametrize("xt,tt", [("bf16", "bf16"), ("f32", "f32")])
+def test_one_class_loses_nothing(L, xt, tt, scale):
+    """A table of one row: the loss is 0, not the rounding of its logit."""
+    x, w, _, _ = _inputs(300, 1, 72, xt, tt)
+    loss, lse = L.luq_cross_entropy_fwd(x * 50.0, w, torch.zeros(300, dtype=torch.int64, device="cuda"), scale)
+    assert (loss == 0).all() and (lse.abs() > 1).any()
+
+
+@pytest.mark.parametrize("T,V,D,xt,tt", [(40, 300, 64, "f32", "f32"), (40, 300, 64, "bf16", "bf16"), (509, 8000, 510, "f32", "f32"),
+                                         (1500, 9100, 72, "bf16", "bf16")])
+def test_losses_of_far_logits(L, T, V, D, xt, tt):
+    """Rows predicted well, their target's logit far above the others or not so far: the loss is not below 0, and the
+    rounding of the logits' common size is not in it."""
+    gen = torch.Generator(device="cuda").manual_seed(T + V)
+    w = torch.randn(V, D, device="cuda", generator=gen).to(DT[tt])
+    y = torch.randint(0, V, (T,), device="cuda", generator=gen)
+    x = w.float()[y] / (w.float()[y] ** 2).sum(1, keepdim=True)
+    for size in (5.0, 12.0, 30.0, 1000.0, 1e6, 1e9, 1e30):
+        for scale in (1.0, -3.0):
+            xs = (x * (size / scale)).to(DT[xt])
+            announce("cross entropy, far logits", T, V, D, xt, tt, size, scale)
+            loss, lse = L.luq_cross_entropy_fwd(xs, w, y, scale)
+            z = scale * (xs.double() @ w.double().t())
+            top = z.amax(1)
+            row = torch.arange(T, device="cuda")
+            rest = torch.logsumexp(z - top[:, None], 1)
+            want = rest + (top - z[row, y])
+            # every logit is off by its products' additions and its rounding, a row's loss by as much of the others' share twice;
+            # the sum, which is 1 at least, and its logarithm by their roundings
+            chain = S._chain(S._pairs(1 if xt == "bf16" else 3, 1 if tt == "bf16" else 3), D) * 2 + 8
+            ez = abs(scale) * (xs.double().abs() @ w.double().abs().t()).amax(1) * chain * 2.0 ** -24
+            off = 1 - torch.exp(z[row, y] - top - rest)
+            bound = 2 * ez * torch.clamp(off * torch.exp(torch.clamp(2 * ez, max=700.0)), max=1.0) + (96 + V / 512) * 2.0 ** -24 * (1 + want)
+            assert (loss >= 0).all(), (size, scale, loss.min())
+            assert ((loss.double() - want).abs() <= bound).all(), (size, scale, ((loss.double() - want).abs() / bound).max())
+            assert ((lse.double() - (top + rest)).abs() <= 2 * ez + (96 + V / 512) * 2.0 ** -24 + 2.0 ** -23 * top.abs()).all(), (size, scale)
