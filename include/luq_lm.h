@@ -245,8 +245,9 @@ luq_status luq_route_bwd(const float* dweights, const void* logits, luq_dtype dt
  * Products are those of bf16 matrix instructions with fp32 sums.  An fp32 tensor is taken
  * as three bf16 terms (24 bits, fewer below 2^-110: a term is a multiple of 2^-133), of
  * whose products those above 2^-24 are formed.
- * In the backward call the logits' gradient is rounded to one bf16 term for a bf16 output
- * and to three (24 bits) for an fp32 one.
+ * In the backward call's products with the logits' gradient, an fp32 output is formed from three
+ * terms of it (24 bits) and as many of an fp32 tensor; a bf16 output from one term of it (8 bits: the
+ * output is off by 1.4 times its own rounding, in the norm) and two of an fp32 tensor (16 bits).
  */
 
 /* Bytes of the workspace of the forward call (gt = -1) or of the backward call (gt: type
