@@ -776,7 +776,10 @@ def luq_adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copy=None, w
     """The plan of a step over params (float32), whose gradients (float32 or bfloat16) and states keep their places.
     m and v of a tensor are float32, or uint8 codes with m_scale and v_scale (uint8, one for 32 elements); they begin as
     zeros.  copy: bfloat16 tensors that get the new weights too.  weight_decay and lr_scale: one for all, or a list;
-    the other lists may hold None where a tensor has none."""
+    the other lists may hold None where a tensor has none.
+    The plan holds addresses, and keeps the tensors alive: gradients that are written to the same buffers every step
+    (zeroed or overwritten, not set to None) need one plan.  Where they are new tensors every step, the plan is made
+    again before each (220 us of host work for 97 tensors), or a step takes the old ones."""
     count = len(params)
     gpu = params[0].get_device() if count else -1
     lists = [_each(t, count, name) for t, name in ((grads, "grads"), (m, "m"), (v, "v"), (m_scale, "m_scale"),

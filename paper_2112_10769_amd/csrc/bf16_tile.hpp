@@ -40,8 +40,8 @@ struct PlanePairs {
 struct Bf16Product {
   Bf16Planes A, B;
   PlanePairs pairs;
-  int64_t K;           // a multiple of 8
-  int tiles_m, tiles_n, splits;
+  int64_t K;           // a multiple of 8 where an operand lies along it
+  int tiles_m, tiles_n;
 };
 
 // Tile of a workgroup: each XCD takes a run of tiles, eight rows of tiles at a time.

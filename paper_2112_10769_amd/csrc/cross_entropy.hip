@@ -6,13 +6,15 @@
 //
 // Forward: a tile of products leaves each row's maximum, sum of exponentials and sum of logits over
 // its columns; a second launch joins them.  Backward: a piece of the vocabulary at a time, the
-// products again, their gradient g in bf16, and the two products with it, whose operands lie
+// products again, their gradient g in bf16 terms, and the two products with it, whose operands lie
 // across the reduction: they are transposed on the way out of LDS (written a second time, transposed,
 // g took 130 of 447 us for 4096 x 32000 of it, and the table's and x's transposes 50).
 //
-// g in bf16 is what a bf16 product takes; its rounding is of the size of a bf16 output's own.  An
-// fp32 output takes three bf16 terms of g (4096 tokens on 32000 x 1024 bf16, fp32 gradient of the table:
-// 4.6e-7 of its norm off in 1405 us for both gradients, with two terms 2.6e-6 in 1147; the exact g in an
+// A bf16 output takes g in one bf16 term, whose rounding is of the size of the output's own: 2.4e-3 of the
+// norm off where the output's rounding alone leaves 1.7e-3; a second term would double the products with g
+// and its writes.  An fp32 tensor in such a product is cut to two terms (16 bits: 2^-8 of the output's
+// rounding).  An fp32 output takes three bf16 terms of g (4096 tokens on 32000 x 1024 bf16, fp32 gradient of the table:
+// 4.5e-7 of its norm off in 1400 us for both gradients, with two terms 2.6e-6 in 1147; the exact g in an
 // fp32 library product 1.1e-6).
 #include "cross_entropy_plan.hpp"
 #include "luq_launch.hpp"
@@ -302,8 +304,7 @@ constexpr int64_t kFewRows = 128;
 
 // ---- backward
 
-// A slab of a wave's sums in LDS: 32 rows of its columns in fp32, from which both orders are read
-// in pieces of eight.
+// A slab of a wave's sums in LDS: 32 rows of its columns in fp32, read in pieces of eight along the rows.
 template <typename Tile>
 struct Slab {
   static constexpr int kCols = Tile::TN * 32, kPitch = kCols + 4, kItems = 32 * kCols / 8 / 64;
@@ -559,7 +560,6 @@ Bf16Product logits_product(const CrossEntropyArgs& a, const Layout& l, bool back
   }
   g.pairs = pairs_of(l.xn, l.tn);
   g.K = l.pack_x || l.pack_t ? l.D8 : a.D;
-  g.splits = 1;
   return g;
 }
 
